@@ -11,7 +11,9 @@
  * kernels, as the comparison path.  Beyond that core: hag_max_* / csr_max_* (the
  * element-wise max Aggregate of Table 1's GraphSAGE-P row over the same HAG) and
  * hag_graph_pool_* (the mean-pooling read-out of Section 5.1 over the graphs of
- * a batch).
+ * a batch); and what a training step needs around the aggregation: hag_embedding_*
+ * (learned rows selected by node types or ids), hag_layer_norm_* and
+ * hag_clip_grad_norm.
  *
  * Conventions
  *   ids        graph nodes 0..N-1; aggregation nodes N..N+|V_A|-1, sorted by level
@@ -456,6 +458,75 @@ int32_t hag_test_range_predicates(int32_t id, int32_t lo, int32_t hi, int64_t i,
  * negative value switches the hook off.  The failing call frees what it had built and returns the status;
  * nothing is left half-made, and no GPU work is involved.  Errors: ARG (kind). */
 hag_status hag_test_fail_allocation(int32_t kind, int32_t countdown);
+
+/* ---- Around the aggregation: embedding, layer norm, clipping by the global norm ----
+ * These calls have no handle: device pointers, sizes and a stream, on the current device, no allocation.  Unlike the
+ * aggregation they take any width D (1 .. 2^30), row strides and element-aligned pointers; the widest loads that the
+ * width, the strides and the pointers allow are used (16 bytes where D, the strides and the pointers are multiples
+ * of 16 bytes).  `ld_*` is the distance between the starts of consecutive rows in elements: at least D for what is
+ * written (unless it has one row), any value >= 0 for what is read (0: the same row every time).  Sums and statistics
+ * are fp32, or fp64 where said; each result is rounded once, when it is stored.  No floating-point atomics and a
+ * fixed order of additions: the same inputs give the same bits.  Matrices that are written must not overlap anything
+ * else the call reads or writes, except where "in place" is mentioned. */
+
+typedef enum { HAG_ID32 = 0, HAG_ID64 = 1 } hag_id_type; /* int32_t / int64_t ids */
+
+/* Embedding: rows of a table (n_rows x D of table_dtype) selected by ids and scaled.
+ *   forward : out_i = scale * table[ids[i]], n x D of `dtype`.
+ *   backward: grad_table_v = scale * sum over i with ids[i] == v of grad_out_i; every row of grad_table is written,
+ *             rows that no id names with zeros.  The ids are sorted in the workspace (stable, so that the terms of a
+ *             row are added in the same order every time).
+ * An id outside 0 .. n_rows-1 (-1, say) stands for no token: a zero row forward, nothing backward.
+ * hag_embedding_bwd_workspace_bytes: 16-byte aligned scratch of the backward call (0 when n is 0); it carries
+ * nothing between calls.
+ * ids, out / grad_out may be NULL when n = 0, the table when n_rows = 0.
+ * Errors: NULL, ARG (D <= 0, n < 0, n_rows < 0, a stride, out == table), DTYPE (also id_type), ALIGN (pointer not on
+ * its element), WORKSPACE, TOO_LARGE (D > 2^30, n_rows >= 2^31 - 1; backward: n >= 2^31 - 4096), CUDA. */
+hag_status hag_embedding_fwd(const void *ids, hag_id_type id_type, int64_t n, int64_t n_rows, const void *table,
+                             hag_dtype table_dtype, int64_t ld_table, hag_dtype dtype, int32_t D, float scale, void *out,
+                             int64_t ld_out, void *cuda_stream);
+size_t hag_embedding_bwd_workspace_bytes(int64_t n, int64_t n_rows, int32_t D);
+hag_status hag_embedding_bwd(const void *ids, hag_id_type id_type, int64_t n, int64_t n_rows, hag_dtype dtype, int32_t D,
+                             const void *grad_out, int64_t ld_grad_out, float scale, void *grad_table,
+                             hag_dtype table_dtype, int64_t ld_grad_table, void *workspace, void *cuda_stream);
+
+/* Layer norm over the D columns of each of n rows.
+ *   forward : mean = sum x / D, rstd = 1 / sqrt(sum (x - mean)^2 / D + eps), y = (x - mean) * rstd * weight + bias.
+ *             mean and rstd (n fp32 values each; may be NULL) are what the backward call needs.
+ *   backward: with xh = (x - mean) * rstd and q = grad_y * weight:
+ *             grad_x = rstd * (q - sum q / D - xh * sum(q * xh) / D), grad_weight = sum over rows of grad_y * xh,
+ *             grad_bias = sum over rows of grad_y.  grad_weight and grad_bias may each be NULL (not wanted); with
+ *             n = 0 they are zeros.
+ * x, y, grad_y, grad_x: `dtype`; weight, bias and their gradients: D values of weight_dtype; weight NULL stands for
+ * ones, bias NULL for zeros.  In place: y may be x, grad_x may be grad_y or x (with the same row stride).
+ * hag_layer_norm_bwd_workspace_bytes: 16-byte aligned scratch, needed when grad_weight or grad_bias is wanted; it
+ * carries nothing between calls.
+ * Errors: NULL, ARG (n < 0, D <= 0, eps negative or no number, a stride), DTYPE, ALIGN (pointer not on its element),
+ * WORKSPACE, TOO_LARGE (D > 2^30), CUDA. */
+hag_status hag_layer_norm_fwd(int64_t n, int32_t D, hag_dtype dtype, const void *x, int64_t ld_x, const void *weight,
+                              const void *bias, hag_dtype weight_dtype, float eps, void *y, int64_t ld_y, float *mean,
+                              float *rstd, void *cuda_stream);
+size_t hag_layer_norm_bwd_workspace_bytes(int64_t n, int32_t D);
+hag_status hag_layer_norm_bwd(int64_t n, int32_t D, hag_dtype dtype, const void *grad_y, int64_t ld_grad_y, const void *x,
+                              int64_t ld_x, const float *mean, const float *rstd, const void *weight,
+                              hag_dtype weight_dtype, void *grad_x, int64_t ld_grad_x, void *grad_weight, void *grad_bias,
+                              void *workspace, void *cuda_stream);
+
+/* The global norm of a list of tensors, and the list scaled so that its norm does not exceed max_norm:
+ *   N = sqrt(sum over all tensors and elements of g^2), c = min(1, max_norm / (N + 1e-6)), out_t = c * grads_t.
+ * grads, out, lengths, dtypes: HOST arrays of `count` entries (read during the call, not kept); grads[t] and out[t]
+ * are DEVICE pointers to lengths[t] contiguous elements of dtypes[t].  In place: out[t] may be grads[t] (it is then
+ * left untouched when c = 1); a tensor must not be named twice.  out NULL: the norm alone.  total_norm: DEVICE
+ * pointer to one float that receives N (may be NULL if out is not).  Tensors of length 0 are skipped and may be NULL.
+ * Squares are fp32 and are added in fp32 over 16 KB at most, then in fp64; a value whose square overflows fp32 gives N = inf.  The formula
+ * is applied as it stands: N = inf gives c = 0 (and inf * 0 = NaN), N = NaN gives NaN everywhere.
+ * workspace: hag_clip_grad_norm_workspace_bytes(count) bytes, 16-byte aligned; carries nothing between calls.
+ * Errors: NULL, ARG (count < 0, a negative length, max_norm negative or no number), DTYPE, ALIGN (pointer not on its
+ * element), WORKSPACE, TOO_LARGE (about 2^44 elements), CUDA. */
+size_t hag_clip_grad_norm_workspace_bytes(int32_t count);
+hag_status hag_clip_grad_norm(int32_t count, const void *const *grads, void *const *out, const int64_t *lengths,
+                              const hag_dtype *dtypes, float max_norm, float *total_norm, void *workspace,
+                              void *cuda_stream);
 
 /* Number of kernels the last aggregate call on this handle enqueued. */
 int32_t hag_last_launch_count(const hag_t *h);

@@ -22,6 +22,7 @@ LIB_PATH = os.path.join(_HERE, "libhag_b200.so")
 
 HAG_SUM, HAG_MEAN, HAG_GCN = 0, 1, 2
 HAG_F32, HAG_BF16 = 0, 1
+HAG_ID32, HAG_ID64 = 0, 1
 (HAG_OK, HAG_ERR_NULL, HAG_ERR_ARG, HAG_ERR_GRAPH, HAG_ERR_OOM_HOST, HAG_ERR_OOM_DEVICE, HAG_ERR_CUDA, HAG_ERR_DTYPE,
  HAG_ERR_ALIGN, HAG_ERR_WORKSPACE, HAG_ERR_TIMEOUT, HAG_ERR_NOT_ON_DEVICE, HAG_ERR_TOO_LARGE) = range(13)
 
@@ -31,6 +32,9 @@ EXPORTED_SYMBOLS = [
     "hag_aggregate_host", "hag_aggregate_fwd_static", "hag_graph_pool_fwd", "hag_graph_pool_bwd",
     "hag_max_workspace_bytes", "hag_max_fwd", "hag_max_bwd", "csr_max_fwd", "csr_max_bwd", "hag_profile_enable", "hag_profile_read", "hag_last_launch_count", "hag_status_str",
     "hag_set_schedule", "hag_device_status", "hag_selftest_wait_limit", "hag_export_pass", "hag_test_fail_allocation",
+    "hag_embedding_fwd", "hag_embedding_bwd_workspace_bytes", "hag_embedding_bwd",
+    "hag_layer_norm_fwd", "hag_layer_norm_bwd_workspace_bytes", "hag_layer_norm_bwd",
+    "hag_clip_grad_norm_workspace_bytes", "hag_clip_grad_norm",
 ]
 
 
@@ -150,6 +154,23 @@ def load_library():
     lib.hag_export_pass.restype = ctypes.c_int
     lib.hag_test_fail_allocation.argtypes = [i32, i32]
     lib.hag_test_fail_allocation.restype = ctypes.c_int
+    i64, f32, size, code = ctypes.c_int64, ctypes.c_float, ctypes.c_size_t, ctypes.c_int
+    lib.hag_embedding_fwd.argtypes = [vp, code, i64, i64, vp, code, i64, code, i32, f32, vp, i64, vp]
+    lib.hag_embedding_fwd.restype = code
+    lib.hag_embedding_bwd_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.hag_embedding_bwd_workspace_bytes.restype = size
+    lib.hag_embedding_bwd.argtypes = [vp, code, i64, i64, code, i32, vp, i64, f32, vp, code, i64, vp, vp]
+    lib.hag_embedding_bwd.restype = code
+    lib.hag_layer_norm_fwd.argtypes = [i64, i32, code, vp, i64, vp, vp, code, f32, vp, i64, vp, vp, vp]
+    lib.hag_layer_norm_fwd.restype = code
+    lib.hag_layer_norm_bwd_workspace_bytes.argtypes = [i64, i32]
+    lib.hag_layer_norm_bwd_workspace_bytes.restype = size
+    lib.hag_layer_norm_bwd.argtypes = [i64, i32, code, vp, i64, vp, i64, vp, vp, vp, code, vp, i64, vp, vp, vp, vp]
+    lib.hag_layer_norm_bwd.restype = code
+    lib.hag_clip_grad_norm_workspace_bytes.argtypes = [i32]
+    lib.hag_clip_grad_norm_workspace_bytes.restype = size
+    lib.hag_clip_grad_norm.argtypes = [i32, vp, vp, vp, vp, f32, vp, vp, vp]
+    lib.hag_clip_grad_norm.restype = code
     lib.hag_status_str.argtypes = [ctypes.c_int]
     lib.hag_status_str.restype = ctypes.c_char_p
     _lib = lib
@@ -545,3 +566,210 @@ def graph_pool_bwd(seg_ptr, grad_out, n_rows: int, reduce="mean", out=None):
                                                torch.cuda.current_stream().cuda_stream)
     _check(st, "hag_graph_pool_bwd")
     return out
+
+
+# -- around the aggregation: embedding, layer norm, clipping by the global norm -------------------------------------- #
+def _code(dtype) -> int:
+    import torch
+    if dtype is torch.float32:
+        return HAG_F32
+    if dtype is torch.bfloat16:
+        return HAG_BF16
+    raise TypeError(f"values must be float32 or bfloat16, got {dtype}")
+
+
+def _rows(t, what, like=None, device=None, dtype=None):
+    """A 2-D device tensor whose rows are contiguous (any row stride); returns the row stride in elements."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what} must be a 2-D device tensor")
+    if like is not None and t.shape != like:
+        raise ValueError(f"{what} must have shape {tuple(like)}, got {tuple(t.shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{what} must live on {device}")
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    rs, cs = t.stride()
+    if cs != 1 and t.shape[1] > 1:
+        raise ValueError(f"the rows of {what} must be contiguous")
+    return rs
+
+
+def _vector(t, what, count, device, dtype=None):
+    """A contiguous 1-D device tensor of `count` values."""
+    if t.dim() != 1 or t.shape[0] != count or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what} must be a contiguous tensor of {count} values on {device}")
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    return t.data_ptr()
+
+
+def _scratch_for(workspace, need, device):
+    import torch
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    if not workspace.is_contiguous() or workspace.device != device or workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"workspace must be a contiguous tensor of at least {need} bytes on {device}")
+    return workspace
+
+
+def _call(name, device, *args):
+    """One C call on the device's current stream."""
+    import torch
+    fn = getattr(load_library(), name)
+    index = device.index
+    if torch.cuda.current_device() == index:
+        st = fn(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(index):
+            st = fn(*args, torch.cuda.current_stream().cuda_stream)
+    if st != 0:
+        _check(st, name)
+
+
+def _ids(ids, device, n=None):
+    import torch
+    if ids.dim() != 1 or not ids.is_contiguous() or ids.device != device or (n is not None and ids.shape[0] != n):
+        raise ValueError(f"ids must be a contiguous 1-D tensor{'' if n is None else f' of {n} values'} on {device}")
+    if ids.dtype is torch.int64:
+        return HAG_ID64
+    if ids.dtype is torch.int32:
+        return HAG_ID32
+    raise TypeError(f"ids must be int32 or int64, got {ids.dtype}")
+
+
+def embedding_fwd(ids, table, scale=1.0, out=None, dtype=None):
+    """``hag_embedding_fwd``: scale * table[ids], one row per id; an id outside the table gives a zero row.  The rows are
+    of ``dtype`` (default: the table's)."""
+    import torch
+    ld = _rows(table, "table")
+    device, n, (v, d) = table.device, ids.shape[0] if ids.dim() == 1 else -1, table.shape
+    id_type = _ids(ids, device)
+    if out is None:
+        out = torch.empty((n, d), dtype=dtype or table.dtype, device=device)
+        ld_out = d
+    else:
+        ld_out = _rows(out, "out", (n, d), device, dtype)
+    _call("hag_embedding_fwd", device, ids.data_ptr(), id_type, n, v, table.data_ptr(), _code(table.dtype), ld, _code(out.dtype), d,
+          scale, out.data_ptr(), ld_out)
+    return out
+
+
+def embedding_bwd(ids, grad_out, n_rows: int, scale=1.0, out=None, dtype=None, workspace=None):
+    """``hag_embedding_bwd``: the gradient of ``embedding_fwd`` with respect to a table of n_rows rows, of ``dtype``
+    (default: grad_out's)."""
+    import torch
+    ld = _rows(grad_out, "grad_out")
+    device, (n, d) = grad_out.device, grad_out.shape
+    id_type = _ids(ids, device, n)
+    if out is None:
+        out = torch.empty((n_rows, d), dtype=dtype or grad_out.dtype, device=device)
+        ld_out = d
+    else:
+        ld_out = _rows(out, "out", (n_rows, d), device, dtype)
+    ws = _scratch_for(workspace, load_library().hag_embedding_bwd_workspace_bytes(n, n_rows, d), device)
+    _call("hag_embedding_bwd", device, ids.data_ptr(), id_type, n, n_rows, _code(grad_out.dtype), d, grad_out.data_ptr(), ld, scale,
+          out.data_ptr(), _code(out.dtype), ld_out, None if ws is None else ws.data_ptr())
+    return out
+
+
+def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None, stats=True):
+    """``hag_layer_norm_fwd`` over the columns of x.  Returns (y, mean, rstd); mean and rstd are None where ``stats`` is
+    false (no gradient wanted).  ``out`` may be x."""
+    import torch
+    ld = _rows(x, "x")
+    device, (n, d) = x.device, x.shape
+    wdt = weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
+    w = None if weight is None else _vector(weight, "weight", d, device)
+    b = None if bias is None else _vector(bias, "bias", d, device, wdt)
+    if out is None:
+        out = torch.empty((n, d), dtype=x.dtype, device=device)
+        ld_out = d
+    else:
+        ld_out = _rows(out, "out", x.shape, device, x.dtype)
+    mean = rstd = None
+    if stats:
+        mean, rstd = torch.empty((2, n), dtype=torch.float32, device=device).unbind()
+    _call("hag_layer_norm_fwd", device, n, d, _code(x.dtype), x.data_ptr(), ld, w, b, _code(wdt), eps, out.data_ptr(), ld_out,
+          None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr())
+    return out, mean, rstd
+
+
+def layer_norm_bwd(grad_out, x, mean, rstd, weight=None, out=None, param_grads=True, param_dtype=None, workspace=None):
+    """``hag_layer_norm_bwd``: (grad_x, grad_weight, grad_bias) from what ``layer_norm_fwd`` took and returned; the last
+    two are of the weight's type (without a weight: ``param_dtype``, default float32), and None where ``param_grads``
+    is false.  ``out`` may be grad_out or x."""
+    import torch
+    ld = _rows(x, "x")
+    device, (n, d) = x.device, x.shape
+    ld_g = _rows(grad_out, "grad_out", x.shape, device, x.dtype)
+    w = None if weight is None else _vector(weight, "weight", d, device, param_dtype)
+    wdt = weight.dtype if weight is not None else param_dtype or torch.float32
+    m, r = _vector(mean, "mean", n, device, torch.float32), _vector(rstd, "rstd", n, device, torch.float32)
+    if out is None:
+        out = torch.empty((n, d), dtype=x.dtype, device=device)
+        ld_out = d
+    else:
+        ld_out = _rows(out, "out", x.shape, device, x.dtype)
+    gw = gb = ws = None
+    if param_grads:
+        gw, gb = torch.empty((2, d), dtype=wdt, device=device).unbind()
+        ws = _scratch_for(workspace, load_library().hag_layer_norm_bwd_workspace_bytes(n, d), device)
+    _call("hag_layer_norm_bwd", device, n, d, _code(x.dtype), grad_out.data_ptr(), ld_g, x.data_ptr(), ld, m, r, w, _code(wdt),
+          out.data_ptr(), ld_out, None if gw is None else gw.data_ptr(), None if gb is None else gb.data_ptr(),
+          None if ws is None else ws.data_ptr())
+    return out, gw, gb
+
+
+def _tensor_list(tensors, device):
+    """Pointers, lengths and type codes of a list of contiguous device tensors."""
+    import torch
+    codes = {torch.float32: HAG_F32, torch.bfloat16: HAG_BF16}
+    try:
+        kinds = [codes[t.dtype] for t in tensors]
+    except KeyError as e:
+        raise TypeError(f"gradients must be float32 or bfloat16, got {e.args[0]}") from None
+    if not all(t.is_contiguous() and t.device == device for t in tensors):
+        raise ValueError(f"gradients must be contiguous tensors on {device}")
+    return [t.data_ptr() for t in tensors], [t.numel() for t in tensors], kinds
+
+
+def clip_grad_norm(grads, max_norm, out=None, workspace=None):
+    """``hag_clip_grad_norm``: (the gradients scaled so that their global norm is at most max_norm, that norm as it was).
+    ``out`` is a list of tensors like ``grads``, or ``grads`` itself (in place); default: new tensors."""
+    import torch
+    grads = list(grads)
+    if not grads:
+        raise ValueError("the list of gradients is empty")
+    device, count = grads[0].device, len(grads)
+    if not grads[0].is_cuda:
+        raise ValueError("gradients must be device tensors")
+    ptrs, lens, kinds = _tensor_list(grads, device)
+    if len(set(ptrs)) != count and len({p for p, m in zip(ptrs, lens) if m}) != sum(m > 0 for m in lens):
+        raise ValueError("a gradient is named twice")
+    if out is None:
+        out = [torch.empty_like(g) for g in grads]
+    elif len(out) != count or not all(o is g or (o.shape == g.shape and o.dtype is g.dtype) for o, g in zip(out, grads)):
+        raise ValueError("out must be tensors like the gradients")
+    return out, _clip(device, count, ptrs, _tensor_list(out, device)[0], lens, kinds, max_norm, workspace)
+
+
+def grad_norm(grads, workspace=None):
+    """The global norm alone (``hag_clip_grad_norm`` without outputs): a float32 tensor of one value."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("the list of gradients is empty")
+    device = grads[0].device
+    if not grads[0].is_cuda:
+        raise ValueError("gradients must be device tensors")
+    ptrs, lens, kinds = _tensor_list(grads, device)
+    return _clip(device, len(grads), ptrs, None, lens, kinds, float("inf"), workspace)
+
+
+def _clip(device, count, ptrs, out_ptrs, lens, kinds, max_norm, workspace):
+    import torch
+    pointers = ctypes.c_void_p * count
+    ws = _scratch_for(workspace, load_library().hag_clip_grad_norm_workspace_bytes(count), device)
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    _call("hag_clip_grad_norm", device, count, pointers(*ptrs), None if out_ptrs is None else pointers(*out_ptrs),
+          (ctypes.c_int64 * count)(*lens), (ctypes.c_int * count)(*kinds), max_norm, norm.data_ptr(), ws.data_ptr())
+    return norm

@@ -9,9 +9,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhag_b200.so")
-SOURCES = ["hag_build.cpp", "hag_cuda.cu", "hag_pool.cu", "hag_max.cu"]
+SOURCES = ["hag_build.cpp", "hag_cuda.cu", "hag_pool.cu", "hag_max.cu", "hag_embed.cu", "hag_norm.cu", "hag_clip.cu"]
 HEADERS = [os.path.join(ROOT, "include", "hag.h"), os.path.join(CSRC, "hag_internal.h"),
-           os.path.join(CSRC, "hag_kernels.cuh"), os.path.join(CSRC, "hag_launch.h")]
+           os.path.join(CSRC, "hag_kernels.cuh"), os.path.join(CSRC, "hag_launch.h"), os.path.join(CSRC, "hag_rows.cuh")]
 
 
 def _stale() -> bool:

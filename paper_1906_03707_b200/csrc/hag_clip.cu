@@ -1,0 +1,238 @@
+// The global norm of a list of tensors, and the list scaled so that its norm does not exceed a limit.
+//   N = sqrt(sum over all tensors and elements of g^2),  c = min(1, max_norm / (N + 1e-6)),  out_t = c * g_t
+// Two launches: every block sums the squares of its pieces of the list; then every block adds up those sums (the
+// same order everywhere: the same bits everywhere) and scales its pieces.  The list travels as a kernel parameter,
+// so no descriptor is copied to the device first and the calls can be captured in a graph.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "hag.h"
+#include "hag_kernels.cuh"
+#include "hag_launch.h"
+#include "hag_rows.cuh"
+
+namespace {
+
+constexpr int kClipThreads = 256;
+constexpr int kClipList = 128;                 // tensors per launch: the list must fit in 4 KB of parameters
+constexpr int kPieceBytes = 16384;             // a piece of a tensor: four 16-byte loads per thread
+constexpr int kClipBlocks = 148 * 8;
+
+struct ClipArgs {
+    int32_t tensors;
+    uint32_t pieces;                           // of this launch's tensors
+    double *sums;                              // [launches][kClipBlocks]
+    int32_t first_sum, n_sums;                 // where this launch's blocks put theirs; how many there are in all
+    float max_norm;
+    float *norm;
+    const void *in[kClipList];
+    void *out[kClipList];
+    int64_t len[kClipList];
+    uint32_t first_piece[kClipList];
+    uint8_t bf16[kClipList];
+    uint8_t vec[kClipList];                    // both pointers on 16 bytes
+};
+static_assert(sizeof(ClipArgs) <= 4096, "the list must fit in the parameters of a launch");
+
+__device__ __forceinline__ double block_sum(double v, double *slot) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double s = 0.0;
+#pragma unroll
+    for (int w = 0; w < kClipThreads / 32; ++w) s += slot[w];
+    return s;
+}
+
+// Calls f(tensor, first element, end element) for the pieces of this block, which ascend.
+template <typename F>
+__device__ __forceinline__ void for_pieces(const ClipArgs &p, F f) {
+    int t = 0;
+    for (uint32_t k = blockIdx.x; k < p.pieces; k += gridDim.x) {
+        while (t + 1 < p.tensors && p.first_piece[t + 1] <= k) ++t;
+        const int64_t per = kPieceBytes / (p.bf16[t] ? 2 : 4), b = int64_t(k - p.first_piece[t]) * per;
+        f(t, b, min(p.len[t], b + per));
+    }
+}
+
+template <typename T, int V>
+__device__ __forceinline__ float piece_squares(const void *in, int64_t b, int64_t e) {
+    constexpr int U = kPieceBytes / kClipThreads / (V * int(sizeof(T)));
+    const char *at = static_cast<const char *>(in) + b * sizeof(T);
+    const int32_t len = int32_t(e - b), full = len / V;
+    float s = 0.0f;
+#pragma unroll(U > 4 ? 4 : U)
+    for (int u = 0; u < U; ++u) {
+        const int32_t i = u * kClipThreads + threadIdx.x;
+        if (i >= full) continue;
+        hagr::Vec<T, V> v;
+        v.template load<hagr::kKeep>(at, i);
+#pragma unroll
+        for (int j = 0; j < V; ++j) s += v.get(j) * v.get(j);
+    }
+    if (V > 1 && int32_t(threadIdx.x) < len - full * V) {
+        hagr::Vec<T, 1> v;
+        v.template load<hagr::kKeep>(at, full * V + threadIdx.x);
+        s += v.get(0) * v.get(0);
+    }
+    return s;
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void piece_scale(const void *in, void *out, int64_t b, int64_t e, float c) {
+    constexpr int U = kPieceBytes / kClipThreads / (V * int(sizeof(T)));
+    const char *at = static_cast<const char *>(in) + b * sizeof(T);
+    char *to = static_cast<char *>(out) + b * sizeof(T);
+    const int32_t len = int32_t(e - b), full = len / V;
+#pragma unroll(U > 4 ? 4 : U)
+    for (int u = 0; u < U; ++u) {
+        const int32_t i = u * kClipThreads + threadIdx.x;
+        if (i >= full) continue;
+        hagr::Vec<T, V> v;
+        v.template load<hagr::kOnce>(at, i);
+        float f[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = v.get(j) * c;
+        v.set(f);
+        v.store(to, i);
+    }
+    if (V > 1 && int32_t(threadIdx.x) < len - full * V) {
+        hagr::Vec<T, 1> v;
+        v.template load<hagr::kOnce>(at, full * V + threadIdx.x);
+        const float f = v.get(0) * c;
+        v.set(&f);
+        v.store(to, full * V + threadIdx.x);
+    }
+}
+
+__global__ void __launch_bounds__(kClipThreads) norm_sums_kernel(const __grid_constant__ ClipArgs p) {
+    hagk::pdl_launch_dependents();
+    __shared__ double slot[kClipThreads / 32];
+    double s = 0.0;       // squares are added in fp32 within a piece, in fp64 from piece to piece
+    hagk::pdl_wait();
+    for_pieces(p, [&](int t, int64_t b, int64_t e) {
+        if (p.bf16[t])
+            s += p.vec[t] ? piece_squares<__nv_bfloat16, 8>(p.in[t], b, e) : piece_squares<__nv_bfloat16, 1>(p.in[t], b, e);
+        else
+            s += p.vec[t] ? piece_squares<float, 4>(p.in[t], b, e) : piece_squares<float, 1>(p.in[t], b, e);
+    });
+    s = block_sum(s, slot);
+    if (threadIdx.x == 0) p.sums[p.first_sum + blockIdx.x] = s;
+}
+
+// The norm from the blocks' sums; called by whole blocks.
+__device__ __forceinline__ float total_norm(const ClipArgs &p, double *slot) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < p.n_sums; i += kClipThreads) s += __ldcg(p.sums + i);
+    return float(sqrt(block_sum(s, slot)));
+}
+
+__global__ void __launch_bounds__(kClipThreads) norm_join_kernel(const __grid_constant__ ClipArgs p) {
+    hagk::pdl_launch_dependents();
+    __shared__ double slot[kClipThreads / 32];
+    hagk::pdl_wait();
+    const float norm = total_norm(p, slot);
+    if (threadIdx.x == 0 && p.norm) *p.norm = norm;
+}
+
+__global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_constant__ ClipArgs p) {
+    hagk::pdl_launch_dependents();
+    __shared__ double slot[kClipThreads / 32];
+    hagk::pdl_wait();
+    const float norm = total_norm(p, slot);
+    if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
+    const float ratio = p.max_norm / (norm + 1e-6f);
+    const float c = ratio >= 1.0f ? 1.0f : ratio;          // a norm that is no number gives a factor that is none
+    for_pieces(p, [&](int t, int64_t b, int64_t e) {
+        if (c == 1.0f && p.in[t] == p.out[t]) return;      // in place and nothing to change
+        if (p.bf16[t]) {
+            if (p.vec[t]) piece_scale<__nv_bfloat16, 8>(p.in[t], p.out[t], b, e, c);
+            else piece_scale<__nv_bfloat16, 1>(p.in[t], p.out[t], b, e, c);
+        } else {
+            if (p.vec[t]) piece_scale<float, 4>(p.in[t], p.out[t], b, e, c);
+            else piece_scale<float, 1>(p.in[t], p.out[t], b, e, c);
+        }
+    });
+}
+
+int launches_of(int32_t count) { return std::max(1, (count + kClipList - 1) / kClipList); }
+
+// The part of the list that launch `k` handles; false: it has more pieces than a launch can count.
+bool fill(ClipArgs &p, int k, int32_t count, const void *const *in, void *const *out, const int64_t *len, const hag_dtype *dtype) {
+    p.tensors = 0;
+    int64_t pieces = 0;
+    for (int32_t t = k * kClipList; t < std::min(count, (k + 1) * kClipList); ++t) {
+        if (len[t] == 0) continue;
+        const int i = p.tensors++;
+        const int64_t per = kPieceBytes / (dtype[t] == HAG_BF16 ? 2 : 4);
+        p.in[i] = in[t];
+        p.out[i] = out ? out[t] : nullptr;
+        p.len[i] = len[t];
+        p.first_piece[i] = uint32_t(pieces);
+        p.bf16[i] = dtype[t] == HAG_BF16;
+        p.vec[i] = hagl::aligned16(in[t]) && (!out || hagl::aligned16(out[t]));
+        pieces += (len[t] + per - 1) / per;
+        if (pieces > 0x7fffffffLL) return false;
+    }
+    p.pieces = uint32_t(pieces);
+    return true;
+}
+
+}  // namespace
+
+extern "C" size_t hag_clip_grad_norm_workspace_bytes(int32_t count) {
+    return count < 0 ? 0 : size_t(launches_of(count)) * kClipBlocks * sizeof(double);
+}
+
+extern "C" hag_status hag_clip_grad_norm(int32_t count, const void *const *grads, void *const *out, const int64_t *lengths,
+                                         const hag_dtype *dtypes, float max_norm, float *total_norm, void *workspace,
+                                         void *cuda_stream) {
+    if (count < 0 || !(max_norm >= 0.0f)) return HAG_ERR_ARG;
+    if (count > 0 && (!grads || !lengths || !dtypes)) return HAG_ERR_NULL;
+    if (!out && !total_norm) return HAG_ERR_NULL;
+    for (int32_t t = 0; t < count; ++t) {
+        if (dtypes[t] != HAG_F32 && dtypes[t] != HAG_BF16) return HAG_ERR_DTYPE;
+        if (lengths[t] < 0) return HAG_ERR_ARG;
+        if (lengths[t] == 0) continue;
+        if (!grads[t] || (out && !out[t])) return HAG_ERR_NULL;
+        const int elem = dtypes[t] == HAG_F32 ? 4 : 2;
+        if (!hagr::element_aligned(grads[t], elem) || (out && !hagr::element_aligned(out[t], elem))) return HAG_ERR_ALIGN;
+    }
+    if (!hagr::element_aligned(total_norm, 4)) return HAG_ERR_ALIGN;
+    if (!workspace) return HAG_ERR_WORKSPACE;
+    if (!hagl::aligned16(workspace)) return HAG_ERR_ALIGN;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const int launches = launches_of(count);
+    ClipArgs p{};
+    p.sums = static_cast<double *>(workspace);
+    p.max_norm = max_norm;
+    for (int k = 0; k < launches; ++k)      // before the first launch: an error leaves everything as it was
+        if (!fill(p, k, count, grads, out, lengths, dtypes)) return HAG_ERR_TOO_LARGE;
+    cudaError_t err = cudaSuccess;
+    int32_t sums = 0;
+    for (int k = 0; k < launches && err == cudaSuccess; ++k) {
+        if (launches > 1) fill(p, k, count, grads, out, lengths, dtypes);
+        const unsigned grid = unsigned(std::min<int64_t>(std::max<uint32_t>(p.pieces, 1), kClipBlocks));
+        p.first_sum = sums;
+        sums += int32_t(grid);
+        err = hagl::launch_pdl<ClipArgs>(norm_sums_kernel, grid, unsigned(kClipThreads), p, s);
+    }
+    p.n_sums = sums;
+    if (err == cudaSuccess && !out) {
+        p.norm = total_norm;
+        err = hagl::launch_pdl<ClipArgs>(norm_join_kernel, 1u, unsigned(kClipThreads), p, s);
+    }
+    for (int k = 0; out && k < launches && err == cudaSuccess; ++k) {
+        if (launches > 1) fill(p, k, count, grads, out, lengths, dtypes);
+        p.norm = k == 0 ? total_norm : nullptr;
+        const unsigned grid = unsigned(std::min<int64_t>(std::max<uint32_t>(p.pieces, 1), kClipBlocks));
+        err = hagl::launch_pdl<ClipArgs>(clip_scale_kernel, grid, unsigned(kClipThreads), p, s);
+    }
+    if (err != cudaSuccess) { cudaGetLastError(); return HAG_ERR_CUDA; }
+    return HAG_OK;
+}

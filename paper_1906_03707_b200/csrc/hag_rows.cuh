@@ -1,0 +1,148 @@
+// Row vectors shared by the kernels around the aggregation (embedding, layer norm, clipping): V elements of
+// type T as one load or store of V * sizeof(T) bytes (two of 16 bytes where that is 32), kept as raw words
+// while in flight and widened to fp32 when used.  V is the largest power of two that the width, the row
+// strides and the pointers of a call allow (vector_elems), so any width and any element-aligned pointer works.
+// Loads are coherent (ld.global, never .nc): under programmatic dependent launch the kernel that wrote the
+// data may still be alive when the reader starts.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace hagr {
+
+template <int B> struct Words;      // B bytes
+template <> struct Words<2> { uint16_t w[1]; };
+template <> struct Words<4> { uint32_t w[1]; };
+template <> struct Words<8> { uint32_t w[2]; };
+template <> struct Words<16> { uint32_t w[4]; };
+template <> struct Words<32> { uint32_t w[8]; };
+
+// Cache operator of a load: kKeep leaves the line where later reads find it, kOnce marks it evict-first (data that
+// is read once must not push out rows that are read again).
+enum CacheOp { kKeep, kOnce };
+
+template <CacheOp OP, int B>
+__device__ __forceinline__ Words<B> load_words(const void *p) {
+    Words<B> r;
+    if constexpr (B == 2) {
+        r.w[0] = OP == kOnce ? __ldcs(static_cast<const uint16_t *>(p)) : __ldcg(static_cast<const uint16_t *>(p));
+    } else if constexpr (B == 4) {
+        r.w[0] = OP == kOnce ? __ldcs(static_cast<const uint32_t *>(p)) : __ldcg(static_cast<const uint32_t *>(p));
+    } else if constexpr (B == 8) {
+        const uint2 q = OP == kOnce ? __ldcs(static_cast<const uint2 *>(p)) : __ldcg(static_cast<const uint2 *>(p));
+        r.w[0] = q.x; r.w[1] = q.y;
+    } else {
+#pragma unroll
+        for (int h = 0; h < B / 16; ++h) {
+            const uint4 *s = static_cast<const uint4 *>(p) + h;
+            const uint4 q = OP == kOnce ? __ldcs(s) : __ldcg(s);
+            r.w[4 * h] = q.x; r.w[4 * h + 1] = q.y; r.w[4 * h + 2] = q.z; r.w[4 * h + 3] = q.w;
+        }
+    }
+    return r;
+}
+
+template <int B>
+__device__ __forceinline__ void store_words(void *p, const Words<B> &r) {
+    if constexpr (B == 2) {
+        *static_cast<uint16_t *>(p) = r.w[0];
+    } else if constexpr (B == 4) {
+        *static_cast<uint32_t *>(p) = r.w[0];
+    } else if constexpr (B == 8) {
+        *static_cast<uint2 *>(p) = make_uint2(r.w[0], r.w[1]);
+    } else {
+#pragma unroll
+        for (int h = 0; h < B / 16; ++h)
+            static_cast<uint4 *>(p)[h] = make_uint4(r.w[4 * h], r.w[4 * h + 1], r.w[4 * h + 2], r.w[4 * h + 3]);
+    }
+}
+
+template <typename T, int V>
+struct Vec {
+    static constexpr int kBytes = V * int(sizeof(T));
+    Words<kBytes> raw;
+
+    template <CacheOp OP>
+    __device__ __forceinline__ void load(const void *row, size_t i) {        // elements i * V .. of the row
+        raw = load_words<OP, kBytes>(static_cast<const char *>(row) + i * kBytes);
+    }
+    __device__ __forceinline__ void store(void *row, size_t i) const {
+        store_words<kBytes>(static_cast<char *>(row) + i * kBytes, raw);
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int k = 0; k < int(sizeof(raw.w) / sizeof(raw.w[0])); ++k) raw.w[k] = 0;
+    }
+    __device__ __forceinline__ float get(int j) const {
+        if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(raw.w[j]);
+        } else if constexpr (V == 1) {
+            return __uint_as_float(uint32_t(raw.w[0]) << 16);
+        } else {
+            return (j & 1) ? __uint_as_float(raw.w[j / 2] & 0xffff0000u) : __uint_as_float(raw.w[j / 2] << 16);
+        }
+    }
+    __device__ __forceinline__ void set(const float *v) {                    // one round-to-nearest per element
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) raw.w[j] = __float_as_uint(v[j]);
+        } else if constexpr (V == 1) {
+            raw.w[0] = __bfloat16_as_ushort(__float2bfloat16_rn(v[0]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; j += 2) {
+                const __nv_bfloat162 q = __floats2bfloat162_rn(v[j], v[j + 1]);
+                raw.w[j / 2] = *reinterpret_cast<const uint32_t *>(&q);
+            }
+        }
+    }
+};
+
+// Quotients by a divisor fixed per launch: multiply-high, add and shift (Granlund and Montgomery 1994), for
+// dividends below 2^31.
+struct Divisor {
+    uint32_t d, mul, shift;
+};
+inline Divisor make_divisor(uint32_t d) {
+    uint32_t s = 0;
+    while ((uint64_t(1) << s) < d) ++s;
+    const uint64_t m = ((uint64_t(1) << 32) * ((uint64_t(1) << s) - d)) / d + 1;
+    return Divisor{d, uint32_t(m), s};
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t n, const Divisor &v) { return (__umulhi(n, v.mul) + n) >> v.shift; }
+
+// One matrix of a call, as far as the vector width goes.
+struct Operand {
+    const void *p;
+    int64_t ld;
+    int elem;        // bytes per element
+};
+
+// The largest power of two V <= limit such that every operand can be read V elements at a time: V divides the width
+// and the row strides, and the pointer is aligned to the V elements or to 16 bytes, whichever is less.
+template <int N>
+inline int vector_elems(int limit, int32_t D, const Operand (&ops)[N]) {
+    int v = limit;
+    auto fits = [&](int v_) {
+        if (D % v_ != 0) return false;
+        for (const Operand &o : ops) {
+            if (!o.p) continue;
+            const int bytes = v_ * o.elem < 16 ? v_ * o.elem : 16;
+            if (o.ld % v_ != 0 || reinterpret_cast<uintptr_t>(o.p) % uintptr_t(bytes) != 0) return false;
+        }
+        return true;
+    };
+    while (v > 1 && !fits(v)) v /= 2;
+    return v;
+}
+
+inline bool element_aligned(const void *p, int elem) { return reinterpret_cast<uintptr_t>(p) % uintptr_t(elem) == 0; }
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+}  // namespace hagr
