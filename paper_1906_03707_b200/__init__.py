@@ -615,13 +615,13 @@ def _scratch_for(workspace, need, device):
 def _call(name, device, *args):
     """One C call on the device's current stream."""
     import torch
-    fn = getattr(load_library(), name)
+    fn = getattr(_lib or load_library(), name)
     index = device.index
     if torch.cuda.current_device() == index:
-        st = fn(*args, torch.cuda.current_stream().cuda_stream)
+        st = fn(*args, torch.cuda.current_stream(index).cuda_stream)
     else:
         with torch.cuda.device(index):
-            st = fn(*args, torch.cuda.current_stream().cuda_stream)
+            st = fn(*args, torch.cuda.current_stream(index).cuda_stream)
     if st != 0:
         _check(st, name)
 
