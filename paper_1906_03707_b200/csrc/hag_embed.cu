@@ -98,6 +98,51 @@ cudaError_t launch_lookup_v(LookupArgs &p, int64_t n, int32_t D, cudaStream_t s)
 }
 
 // ---------------------------------------------------------------------------------------------------------------
+// Zeros for the rows of the gradient, written by blocks of their own next to the sort's in the sort's launches: the
+// sort waits for latencies and leaves the memory idle.  The rows that some id names are written again afterwards.
+struct FillArgs {
+    char *out;
+    int64_t row_bytes, ld_bytes;
+    int32_t rows_begin, rows_end;      // of this launch
+    int32_t elem;                      // bytes
+    int32_t blocks;
+};
+constexpr int kFillThreads = 256;
+
+// Threads tid, tid + step, ... clear `bytes` bytes at p (a multiple of the element, 2 or 4).
+__device__ __forceinline__ void clear_span(char *p, int64_t bytes, int elem, int64_t tid, int64_t step) {
+    int64_t head = int64_t((16 - (reinterpret_cast<uintptr_t>(p) & 15u)) & 15u);
+    if (head > bytes) head = bytes;
+    const int64_t body = (bytes - head) / 16, tail = head + body * 16;
+    for (int64_t i = tid; i < body; i += step) *reinterpret_cast<uint4 *>(p + head + i * 16) = make_uint4(0, 0, 0, 0);
+    // the ragged ends: at most 7 elements each
+    for (int64_t i = tid * elem; i < head; i += step * elem) {
+        if (elem == 4) *reinterpret_cast<uint32_t *>(p + i) = 0; else *reinterpret_cast<uint16_t *>(p + i) = 0;
+    }
+    for (int64_t i = tail + tid * elem; i < bytes; i += step * elem) {
+        if (elem == 4) *reinterpret_cast<uint32_t *>(p + i) = 0; else *reinterpret_cast<uint16_t *>(p + i) = 0;
+    }
+}
+
+__device__ __forceinline__ void fill_rows(const FillArgs &f, int block) {
+    if (f.ld_bytes == f.row_bytes) {
+        clear_span(f.out + f.rows_begin * f.row_bytes, (f.rows_end - f.rows_begin) * f.row_bytes, f.elem,
+                   int64_t(block) * kFillThreads + threadIdx.x, int64_t(f.blocks) * kFillThreads);
+    } else {
+        const int lane = threadIdx.x & 31;
+        for (int64_t r = f.rows_begin + int64_t(block) * (kFillThreads / 32) + (threadIdx.x >> 5); r < f.rows_end;
+             r += int64_t(f.blocks) * (kFillThreads / 32))
+            clear_span(f.out + r * f.ld_bytes, f.row_bytes, f.elem, lane, 32);
+    }
+}
+
+__global__ void __launch_bounds__(kFillThreads) fill_kernel(const FillArgs f) {
+    hagk::pdl_launch_dependents();
+    hagk::pdl_wait();
+    fill_rows(f, blockIdx.x);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
 // Stable radix sort of (key, place) by key; key = the id, or V for a place without a token (those come last).
 // Each pass: every block counts the digits of its own stretch of the list (sort_count_kernel); then every block
 // adds up the counts before it, and moves its stretch to the places found (sort_move_kernel).
@@ -118,6 +163,8 @@ struct SortArgs {
     int32_t n;
     int32_t stretch;         // keys per block, a multiple of the tile
     int32_t shift, bits;
+    int32_t blocks;          // that sort; the blocks after them clear rows of the gradient
+    FillArgs fill;
 };
 
 __device__ __forceinline__ uint32_t sort_key(const SortArgs &p, int32_t i) {
@@ -132,8 +179,12 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
     bin[threadIdx.x] = 0;
     __syncthreads();
     const uint32_t mask = (1u << p.bits) - 1u;
-    const int32_t begin = blockIdx.x * p.stretch, end = int32_t(min(int64_t(p.n), int64_t(begin) + p.stretch));
     hagk::pdl_wait();
+    if (int(blockIdx.x) >= p.blocks) {
+        fill_rows(p.fill, blockIdx.x - p.blocks);
+        return;
+    }
+    const int32_t begin = blockIdx.x * p.stretch, end = int32_t(min(int64_t(p.n), int64_t(begin) + p.stretch));
     for (int32_t i = begin + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&bin[(sort_key(p, i) >> p.shift) & mask], 1u);
     __syncthreads();
     p.count[blockIdx.x * kSortBins + threadIdx.x] = bin[threadIdx.x];
@@ -147,9 +198,14 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const uint32_t mask = (1u << p.bits) - 1u;
     hagk::pdl_wait();
+    if (int(blockIdx.x) >= p.blocks) {
+        fill_rows(p.fill, blockIdx.x - p.blocks);
+        return;
+    }
     {   // base[d] = keys with a smaller digit + keys of digit d in the blocks before this one
         uint32_t before = 0, total = 0;
-        for (int b = 0; b < int(gridDim.x); ++b) {
+        #pragma unroll 8
+        for (int b = 0; b < p.blocks; ++b) {
             const uint32_t c = __ldcg(p.count + b * kSortBins + t);
             if (b < int(blockIdx.x)) before += c;
             total += c;
@@ -211,8 +267,13 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
 }
 
 // ---------------------------------------------------------------------------------------------------------------
+// The sums.  The sorted list is cut into equal stretches, one per worker (a group of lanes that covers a row, or 32
+// vectors of it, with one load per lane), so the work does not depend on how often an id occurs.  A worker adds up
+// run after run of equal ids; a run that lies inside its stretch is a finished row.  A run that crosses into or out of
+// the stretch leaves a partial row: the one that was open at the stretch's start in `head`, the one that is open at its
+// end in `tail`; embedding_join_kernel adds those up in the order of the stretches.
 struct SumArgs {
-    const uint32_t *key, *place;     // sorted
+    const uint32_t *key, *place;     // sorted; readable in whole groups of kSumBatch
     int32_t n;
     int32_t n_rows;                  // V
     const void *grad;
@@ -221,53 +282,198 @@ struct SumArgs {
     int64_t ld_out;
     int32_t D;
     float scale;
+    int32_t stretch;                 // places per worker, a multiple of kSumBatch
+    int32_t workers;
+    int32_t lanes;                   // per worker: 4, 8, 16 or 32
+    float *head, *tail;              // [workers][D up to a multiple of 4]
 };
+constexpr int kSumThreads = 256;
+constexpr int kSumBatch = 8;         // rows in flight per worker
 
-__device__ __forceinline__ int32_t lower_bound(const uint32_t *key, int32_t n, uint32_t v) {
-    int32_t lo = 0, hi = n;
-    while (lo < hi) {
-        const int32_t mid = lo + (hi - lo) / 2;
-        if (__ldcg(key + mid) < v) lo = mid + 1; else hi = mid;
-    }
-    return lo;
+template <typename TO, int V>
+__device__ __forceinline__ void store_row(const SumArgs &p, uint32_t key, int vec, const float *acc) {
+    float v[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = acc[j] * p.scale;
+    hagr::Vec<TO, V> o;
+    o.set(v);
+    o.store(static_cast<TO *>(p.out) + int64_t(key) * p.ld_out, vec);
 }
 
-// One warp per row of the table.
 template <typename TG, typename TO, int V>
-__global__ void __launch_bounds__(hagk::kThreads) embedding_sum_kernel(const SumArgs p) {
+__global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArgs p) {
     hagk::pdl_launch_dependents();
-    const int lane = threadIdx.x & 31;
-    const int64_t row = int64_t(blockIdx.x) * hagk::kWarps + (threadIdx.x >> 5);
+    const int worker = (blockIdx.x * kSumThreads + threadIdx.x) / p.lanes;
+    const int vec = blockIdx.y * 32 + (threadIdx.x & (p.lanes - 1));
+    const bool column = vec < p.D / V;                         // lanes beyond the row only keep step
+    const int32_t t0 = worker < p.workers ? worker * p.stretch : p.n;
+    const int32_t t1 = int32_t(min(int64_t(p.n), int64_t(t0) + p.stretch));
     hagk::pdl_wait();
-    if (row >= p.n_rows) return;
-    const int32_t b = lower_bound(p.key, p.n, uint32_t(row)), e = lower_bound(p.key, p.n, uint32_t(row) + 1u);
-    const int n_vec = p.D / V;
-    for (int c = lane; c < n_vec; c += 32) {
-        float acc[V];
+    if (t0 >= t1) return;
+    const uint32_t none = 0xffffffffu, rows = uint32_t(p.n_rows);
+    const uint32_t before = t0 > 0 ? __ldcg(p.key + t0 - 1) : none, after = t1 < p.n ? __ldcg(p.key + t1) : none;
+    const int64_t part = int64_t(worker) * ((p.D + 3) & ~3) + int64_t(vec) * V;
+    auto leave = [&](float *at, const float *acc) {
+        if (!column) return;
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] = 0.0f;
-        for (int32_t i = b; i < e; ++i) {
-            hagr::Vec<TG, V> g;
-            g.template load<hagr::kOnce>(static_cast<const TG *>(p.grad) + int64_t(__ldcg(p.place + i)) * p.ld_grad, c);
+        for (int j = 0; j < V; ++j) at[part + j] = acc[j];
+    };
+    uint32_t key[kSumBatch], place[kSumBatch];
+    auto fetch = [&](int32_t t) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] += g.get(j);
+        for (int h = 0; h < kSumBatch; h += 4) {
+            const uint4 k = __ldcg(reinterpret_cast<const uint4 *>(p.key + t + h)), q = __ldcg(reinterpret_cast<const uint4 *>(p.place + t + h));
+            key[h] = k.x; key[h + 1] = k.y; key[h + 2] = k.z; key[h + 3] = k.w;
+            place[h] = q.x; place[h + 1] = q.y; place[h + 2] = q.z; place[h + 3] = q.w;
+        }
+    };
+    fetch(t0);
+    uint32_t cur = key[0];
+    bool from_left = cur == before;                            // the current run began in an earlier stretch
+    float acc[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] = 0.0f;
+    for (int32_t t = t0; t < t1; t += kSumBatch) {
+        hagr::Vec<TG, V> g[kSumBatch];
+        uint32_t k[kSumBatch];
+#pragma unroll
+        for (int u = 0; u < kSumBatch; ++u) {
+            k[u] = t + u < t1 ? key[u] : none;
+            g[u].zero();
+            if (k[u] < rows && column) g[u].template load<hagr::kOnce>(static_cast<const TG *>(p.grad) + int64_t(place[u]) * p.ld_grad, vec);
+        }
+        if (t + kSumBatch < t1) fetch(t + kSumBatch);          // the next ids while the rows are on their way
+        if (k[kSumBatch - 1] == cur) {                         // sorted: the whole batch belongs to the run
+            float v[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                v[j] = (g[0].get(j) + g[4].get(j)) + (g[2].get(j) + g[6].get(j));
+                v[j] += (g[1].get(j) + g[5].get(j)) + (g[3].get(j) + g[7].get(j));
+                acc[j] += v[j];
+            }
+            continue;
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] *= p.scale;
-        hagr::Vec<TO, V> o;
-        o.set(acc);
-        o.store(static_cast<TO *>(p.out) + row * p.ld_out, c);
+        for (int u = 0; u < kSumBatch; ++u) {
+            if (t + u < t1 && k[u] != cur) {
+                if (from_left) leave(p.head, acc);
+                else if (column && cur < rows) store_row<TO, V>(p, cur, vec, acc);
+                from_left = false;
+                cur = k[u];
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] = 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] += g[u].get(j);
+        }
+    }
+    if (from_left) leave(p.head, acc);
+    else if (cur == after) leave(p.tail, acc);
+    else if (column && cur < rows) store_row<TO, V>(p, cur, vec, acc);
+}
+
+// Rows whose runs cross stretches: the tail of the stretch where the run begins and the heads of the following
+// stretches that begin with it.  A warp takes one stretch; chains of more than kLongChain heads (an id that fills
+// many stretches) are taken by all the warps of the block together.
+constexpr int kJoinWarps = 8;
+constexpr int kLongChain = 16;
+
+template <typename TO>
+__device__ __forceinline__ void join_store(const SumArgs &p, uint32_t key, int c, float v) {
+    hagr::Vec<TO, 1> o;
+    v *= p.scale;
+    o.set(&v);
+    o.store(static_cast<TO *>(p.out) + int64_t(key) * p.ld_out, c);
+}
+
+template <typename TO>
+__global__ void __launch_bounds__(32 * kJoinWarps) embedding_join_kernel(const SumArgs p) {
+    hagk::pdl_launch_dependents();
+    __shared__ int chain[kJoinWarps];
+    __shared__ float sum[kJoinWarps][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int w0 = blockIdx.x * kJoinWarps, w = w0 + warp;
+    const int64_t width = (p.D + 3) & ~3;
+    hagk::pdl_wait();
+    // heads that continue the run open at the end of stretch `w`; 0: none begins there
+    int heads = 0;
+    uint32_t key = 0;
+    const int64_t t1 = (int64_t(w) + 1) * p.stretch;
+    if (w < p.workers && t1 < p.n) {
+        key = __ldcg(p.key + t1 - 1);
+        const int64_t t0 = t1 - p.stretch;
+        const bool begins = !(__ldcg(p.key + t0) == key && t0 > 0 && __ldcg(p.key + t0 - 1) == key);
+        if (begins && key < uint32_t(p.n_rows)) {
+            for (int j = w + 1;; j += 32) {
+                const bool in = j + lane < p.workers && __ldcg(p.key + int64_t(j + lane) * p.stretch) == key;
+                const int c = __popc(__ballot_sync(0xffffffffu, in));
+                heads += c;
+                if (c < 32) break;
+            }
+        }
+    }
+    if (lane == 0) chain[warp] = heads;
+    __syncthreads();
+    if (heads > 0 && heads <= kLongChain)
+        for (int c = lane; c < p.D; c += 32) {
+            float v = __ldcg(p.tail + w * width + c);
+#pragma unroll 4
+            for (int j = 1; j <= heads; ++j) v += __ldcg(p.head + (w + j) * width + c);
+            join_store<TO>(p, key, c, v);
+        }
+    for (int q = 0; q < kJoinWarps; ++q) {
+        const int count = chain[q];                            // the same for all threads
+        if (count <= kLongChain) continue;
+        const uint32_t k = __ldcg(p.key + (int64_t(w0 + q) + 1) * p.stretch - 1);
+        for (int c0 = 0; c0 < p.D; c0 += 32) {
+            const int c = c0 + lane;
+            float v = 0.0f;
+            if (c < p.D) {
+                if (warp == 0) v = __ldcg(p.tail + (w0 + q) * width + c);
+#pragma unroll 8
+                for (int j = 1 + warp; j <= count; j += kJoinWarps) v += __ldcg(p.head + (w0 + q + j) * width + c);
+            }
+            __syncthreads();
+            sum[warp][lane] = v;
+            __syncthreads();
+            if (warp == 0 && c < p.D) {
+#pragma unroll
+                for (int x = 1; x < kJoinWarps; ++x) v += sum[x][lane];
+                join_store<TO>(p, k, c, v);
+            }
+        }
     }
 }
 
+// Warps for the sums: 16 per SM with kSumBatch 16-byte loads per lane in flight keep 64 KB per SM on their way.
+constexpr int kSumWarps = 148 * 16;
+
 template <typename TG, typename TO, int V>
-cudaError_t launch_sum(const SumArgs &p, cudaStream_t s) {
-    const int64_t blocks = (int64_t(p.n_rows) + hagk::kWarps - 1) / hagk::kWarps;
-    return hagl::launch_pdl(embedding_sum_kernel<TG, TO, V>, unsigned(blocks), unsigned(hagk::kThreads), p, s);
+cudaError_t launch_sum(SumArgs &p, cudaStream_t s) {
+    const int n_vec = p.D / V;
+    p.lanes = hagl::lanes_per_row(n_vec);
+    const int column_blocks = (n_vec + 31) / 32;
+    const int64_t most = std::max<int64_t>(int64_t(kSumWarps) / column_blocks, 1) * (32 / p.lanes);
+    const int64_t batches = (int64_t(p.n) + kSumBatch - 1) / kSumBatch;
+    p.stretch = int32_t((batches + most - 1) / most * kSumBatch);
+    p.workers = int32_t((int64_t(p.n) + p.stretch - 1) / p.stretch);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned((int64_t(p.workers) * p.lanes + kSumThreads - 1) / kSumThreads), unsigned(column_blocks));
+    cfg.blockDim = dim3(kSumThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaError_t err = cudaLaunchKernelEx(&cfg, embedding_sum_kernel<TG, TO, V>, p);
+    if (err == cudaSuccess && p.workers > 1)
+        err = hagl::launch_pdl(embedding_join_kernel<TO>, unsigned((p.workers + kJoinWarps - 1) / kJoinWarps), unsigned(32 * kJoinWarps), p, s);
+    return err;
 }
 
 template <typename TG, typename TO>
-cudaError_t launch_sum_v(const SumArgs &p, cudaStream_t s) {
+cudaError_t launch_sum_v(SumArgs &p, cudaStream_t s) {
     constexpr int kMost = sizeof(TG) == 4 && sizeof(TO) == 4 ? 4 : 8;
     const hagr::Operand ops[] = {{p.grad, p.ld_grad, int(sizeof(TG))}, {p.out, p.ld_out, int(sizeof(TO))}};
     switch (hagr::vector_elems(kMost, p.D, ops)) {
@@ -276,6 +482,15 @@ cudaError_t launch_sum_v(const SumArgs &p, cudaStream_t s) {
         case 2: return launch_sum<TG, TO, 2>(p, s);
         default: return launch_sum<TG, TO, 1>(p, s);
     }
+}
+
+// Floats of `head` (and of `tail`), at most: workers * columns is bounded by the lanes times the vector, for any width.
+int64_t partial_floats(int64_t n, int32_t D) {
+    const int64_t width = (int64_t(D) + 3) / 4 * 4, batches = (n + kSumBatch - 1) / kSumBatch;
+    // at V elements per lane a worker covers up to 32 V columns: workers <= kSumWarps * 32 V / D (and twice that where D
+    // does not fill its lanes), at least 8 per column block
+    const int64_t workers = std::max<int64_t>(2 * (int64_t(kSumWarps) * 32 * 8 + D - 1) / D, 8);
+    return std::min(workers, batches) * width;
 }
 
 int key_bits(int32_t n_rows) {          // of the largest key, V
@@ -301,6 +516,13 @@ SortPlan sort_plan(int32_t n, int32_t n_rows) {
 }
 
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+size_t list_bytes(int64_t n) { return up256((size_t(n) + kSumBatch) * 4); }
+
+// Blocks that clear a launch's share of the rows: 32 KB each, four per SM at most.
+int fill_blocks(const FillArgs &f) {
+    const int64_t bytes = (int64_t(f.rows_end) - f.rows_begin) * f.row_bytes;
+    return int(std::min<int64_t>((bytes + 32767) / 32768, 148 * 4));
+}
 
 bool dtype_ok(hag_dtype d) { return d == HAG_F32 || d == HAG_BF16; }
 int elem_size(hag_dtype d) { return d == HAG_F32 ? 4 : 2; }
@@ -310,7 +532,7 @@ hag_status embed_check(const void *ids, hag_id_type id_type, int64_t n, const vo
     if (!dtype_ok(dtype) || !dtype_ok(table_dtype)) return HAG_ERR_DTYPE;
     if (id_type != HAG_ID32 && id_type != HAG_ID64) return HAG_ERR_DTYPE;
     if (D <= 0 || n < 0 || n_rows < 0) return HAG_ERR_ARG;
-    if (D > (1 << 30) || n_rows > 0x7ffffffeLL) return HAG_ERR_TOO_LARGE;
+    if (D > (1 << 20) || n_rows > 0x7ffffffeLL) return HAG_ERR_TOO_LARGE;
     if (is_bwd && n > 0x7fffffffLL - kSortTile) return HAG_ERR_TOO_LARGE;
     const int64_t ld_out = is_bwd ? ld_table : ld_rows, ld_in = is_bwd ? ld_rows : ld_table, n_out = is_bwd ? n_rows : n;
     if (ld_in < 0 || ld_out < 0 || (n_out > 1 && ld_out < D)) return HAG_ERR_ARG;
@@ -343,7 +565,7 @@ extern "C" hag_status hag_embedding_fwd(const void *ids, hag_id_type id_type, in
 
 extern "C" size_t hag_embedding_bwd_workspace_bytes(int64_t n, int64_t n_rows, int32_t D) {
     if (n <= 0 || n > 0x7fffffffLL - kSortTile || n_rows < 0 || D <= 0) return 0;
-    return 4 * up256(size_t(n) * 4) + up256(size_t(kSortMaxBlocks) * kSortBins * 4);
+    return 4 * list_bytes(n) + up256(size_t(kSortMaxBlocks) * kSortBins * 4) + 2 * up256(size_t(partial_floats(n, D)) * 4);
 }
 
 extern "C" hag_status hag_embedding_bwd(const void *ids, hag_id_type id_type, int64_t n, int64_t n_rows, hag_dtype dtype, int32_t D,
@@ -356,23 +578,36 @@ extern "C" hag_status hag_embedding_bwd(const void *ids, hag_id_type id_type, in
     if (!hagl::aligned16(workspace)) return HAG_ERR_ALIGN;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     char *w = static_cast<char *>(workspace);
-    const size_t part = up256(size_t(n) * 4);
+    const int elem = elem_size(table_dtype);
+    FillArgs fill{static_cast<char *>(grad_table), int64_t(D) * elem, ld_grad_table * elem, 0, int32_t(n_rows), elem, 0};
+    if (n_rows == 1) fill.ld_bytes = fill.row_bytes;
+    cudaError_t err = cudaSuccess;
+    if (n == 0) {
+        fill.blocks = fill_blocks(fill);
+        err = hagl::launch_pdl(fill_kernel, unsigned(fill.blocks), unsigned(kFillThreads), fill, s);
+        if (err != cudaSuccess) { cudaGetLastError(); return HAG_ERR_CUDA; }
+        return HAG_OK;
+    }
+    const size_t part = list_bytes(n);
     uint32_t *key[2] = {reinterpret_cast<uint32_t *>(w), reinterpret_cast<uint32_t *>(w + part)};
     uint32_t *place[2] = {reinterpret_cast<uint32_t *>(w + 2 * part), reinterpret_cast<uint32_t *>(w + 3 * part)};
     uint32_t *count = reinterpret_cast<uint32_t *>(w + 4 * part);
-    cudaError_t err = cudaSuccess;
+    char *partials = w + 4 * part + up256(size_t(kSortMaxBlocks) * kSortBins * 4);
     int side = 0;
-    if (n > 0) {
-        const SortPlan plan = sort_plan(int32_t(n), int32_t(n_rows));
-        for (int pass = 0; pass < plan.passes && err == cudaSuccess; ++pass) {
-            SortArgs a{ids, id_type == HAG_ID64, int32_t(n_rows), pass ? key[side] : nullptr, pass ? place[side] : nullptr,
-                       key[side ^ 1], place[side ^ 1], count, int32_t(n), plan.stretch, pass * plan.bits, plan.bits};
-            err = hagl::launch_pdl(sort_count_kernel, unsigned(plan.blocks), unsigned(kSortThreads), a, s);
-            if (err == cudaSuccess) err = hagl::launch_pdl(sort_move_kernel, unsigned(plan.blocks), unsigned(kSortThreads), a, s);
-            side ^= 1;
-        }
+    const SortPlan plan = sort_plan(int32_t(n), int32_t(n_rows));
+    const int launches = 2 * plan.passes;
+    for (int k = 0; k < launches && err == cudaSuccess; ++k) {
+        const int pass = k / 2;
+        fill.rows_begin = int32_t(n_rows * k / launches);
+        fill.rows_end = int32_t(n_rows * (k + 1) / launches);
+        fill.blocks = fill_blocks(fill);
+        const SortArgs a{ids, id_type == HAG_ID64, int32_t(n_rows), pass ? key[side] : nullptr, pass ? place[side] : nullptr,
+                         key[side ^ 1], place[side ^ 1], count, int32_t(n), plan.stretch, pass * plan.bits, plan.bits, plan.blocks, fill};
+        err = hagl::launch_pdl(k % 2 ? sort_move_kernel : sort_count_kernel, unsigned(plan.blocks + fill.blocks), unsigned(kSortThreads), a, s);
+        if (k % 2) side ^= 1;
     }
-    SumArgs q{key[side], place[side], int32_t(n), int32_t(n_rows), grad_out, ld_grad_out, grad_table, ld_grad_table, D, scale};
+    SumArgs q{key[side], place[side], int32_t(n), int32_t(n_rows), grad_out, ld_grad_out, grad_table, ld_grad_table, D, scale, 0, 0, 0,
+              reinterpret_cast<float *>(partials), reinterpret_cast<float *>(partials + up256(size_t(partial_floats(n, D)) * 4))};
     if (err == cudaSuccess) {
         if (dtype == HAG_F32)
             err = table_dtype == HAG_F32 ? launch_sum_v<float, float>(q, s) : launch_sum_v<float, __nv_bfloat16>(q, s);
