@@ -19,7 +19,8 @@
 namespace {
 
 constexpr int kCopyThreads = 256;
-constexpr int kCopyUnroll = 4;
+// Vectors per thread: 64 bytes of the wider type in flight, narrow vectors at most 8.
+template <int BYTES> constexpr int kCopyUnroll = BYTES >= 16 ? 4 : 8;
 
 struct LookupArgs {
     const void *ids;
@@ -35,7 +36,7 @@ struct LookupArgs {
 };
 
 __device__ __forceinline__ int64_t load_id(const void *ids, int ids64, int64_t i) {
-    return ids64 ? __ldcg(static_cast<const long long *>(ids) + i) : int64_t(__ldcg(static_cast<const int *>(ids) + i));
+    return ids64 ? __ldca(static_cast<const long long *>(ids) + i) : int64_t(__ldca(static_cast<const int *>(ids) + i));
 }
 
 // One vector per thread and step over the flat list of all output vectors, so that any mix of few wide or many
@@ -43,29 +44,30 @@ __device__ __forceinline__ int64_t load_id(const void *ids, int ids64, int64_t i
 template <typename TT, typename TO, int V>
 __global__ void __launch_bounds__(kCopyThreads) embedding_fwd_kernel(const LookupArgs p) {
     hagk::pdl_launch_dependents();
-    const int64_t first = int64_t(blockIdx.x) * (kCopyThreads * kCopyUnroll);
+    constexpr int U = kCopyUnroll<V * int(sizeof(TT))>;
+    const int64_t first = int64_t(blockIdx.x) * (kCopyThreads * U);
     const int64_t row0 = first < (int64_t(1) << 31) ? int64_t(hagr::quotient(uint32_t(first), p.per_row)) : first / p.per_row.d;
     const uint32_t col0 = uint32_t(first - row0 * p.per_row.d);
-    int64_t row[kCopyUnroll], id[kCopyUnroll];
-    uint32_t col[kCopyUnroll];
+    int64_t row[U], id[U];
+    uint32_t col[U];
     hagk::pdl_wait();
 #pragma unroll
-    for (int u = 0; u < kCopyUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
         const uint32_t k = u * kCopyThreads + threadIdx.x;
         const uint32_t r = hagr::quotient(col0 + k, p.per_row);
         row[u] = row0 + r;
         col[u] = col0 + k - r * p.per_row.d;
         id[u] = first + k < p.items ? load_id(p.ids, p.ids64, row[u]) : -1;
     }
-    hagr::Vec<TT, V> in[kCopyUnroll];
+    hagr::Vec<TT, V> in[U];
 #pragma unroll
-    for (int u = 0; u < kCopyUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
         in[u].zero();
         if (uint64_t(id[u]) < uint64_t(p.n_rows))
-            in[u].template load<hagr::kKeep>(static_cast<const TT *>(p.table) + id[u] * p.ld_table, col[u]);
+            in[u].template load<hagr::kNear>(static_cast<const TT *>(p.table) + id[u] * p.ld_table, col[u]);
     }
 #pragma unroll
-    for (int u = 0; u < kCopyUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
         if (first + u * kCopyThreads + threadIdx.x >= p.items) continue;
         float v[V];
 #pragma unroll
@@ -80,7 +82,8 @@ template <typename TT, typename TO, int V>
 cudaError_t launch_lookup(LookupArgs &p, int64_t n, int32_t D, cudaStream_t s) {
     p.per_row = hagr::make_divisor(uint32_t(D / V));
     p.items = n * (D / V);
-    const int64_t blocks = (p.items + kCopyThreads * kCopyUnroll - 1) / (kCopyThreads * kCopyUnroll);
+    constexpr int U = kCopyUnroll<V * int(sizeof(TT))>;
+    const int64_t blocks = (p.items + kCopyThreads * U - 1) / (kCopyThreads * U);
     if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
     return hagl::launch_pdl(embedding_fwd_kernel<TT, TO, V>, unsigned(blocks), unsigned(kCopyThreads), p, s);
 }
@@ -107,7 +110,7 @@ struct FillArgs {
     int32_t elem;                      // bytes
     int32_t blocks;
 };
-constexpr int kFillThreads = 256;
+constexpr int kFillThreads = 512;      // those of the sort's launches
 
 // Threads tid, tid + step, ... clear `bytes` bytes at p (a multiple of the element, 2 or 4).
 __device__ __forceinline__ void clear_span(char *p, int64_t bytes, int elem, int64_t tid, int64_t step) {
@@ -143,22 +146,24 @@ __global__ void __launch_bounds__(kFillThreads) fill_kernel(const FillArgs f) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Stable radix sort of (key, place) by key; key = the id, or V for a place without a token (those come last).
-// Each pass: every block counts the digits of its own stretch of the list (sort_count_kernel); then every block
-// adds up the counts before it, and moves its stretch to the places found (sort_move_kernel).
-constexpr int kSortThreads = 256;
+// Stable radix sort of (key, place) pairs by key; key = the id, or V for a place without a token (those come last).
+// Each pass is two launches: every block counts the digits of its own stretch of the list (sort_count_kernel); then
+// every block adds up the counts of all blocks and moves its stretch to the places found (sort_move_kernel).  Within a
+// block a key's place comes from the lanes of its warp that hold the same digit (match), the warp's count so far and
+// the counts of the warps before it: keys keep their order, and nothing depends on the order of atomics.
+constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortItems = 16;                                // keys per thread and tile
+constexpr int kSortItems = 8;                                 // keys per thread and tile
 constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kSortBins = 256;
-constexpr int kSortMaxBlocks = 296;                           // two per SM
+constexpr int kSortMaxBlocks = 148;                           // every block reads the counts of all blocks
 
 struct SortArgs {
     const void *ids;         // first pass: the caller's ids
     int32_t ids64;
     int32_t n_rows;          // V
-    const uint32_t *key_in, *place_in;       // later passes
-    uint32_t *key_out, *place_out;
+    const uint2 *in;         // later passes: {key, place}
+    uint2 *out;
     uint32_t *count;         // [blocks][bins]
     int32_t n;
     int32_t stretch;         // keys per block, a multiple of the tile
@@ -167,16 +172,18 @@ struct SortArgs {
     FillArgs fill;
 };
 
-__device__ __forceinline__ uint32_t sort_key(const SortArgs &p, int32_t i) {
-    if (p.key_in) return __ldcg(p.key_in + i);
+__device__ __forceinline__ uint2 sort_pair(const SortArgs &p, int32_t i) {
+    if (p.in) return __ldcg(p.in + i);
     const int64_t id = load_id(p.ids, p.ids64, i);
-    return uint64_t(id) < uint64_t(p.n_rows) ? uint32_t(id) : uint32_t(p.n_rows);
+    return make_uint2(uint64_t(id) < uint64_t(p.n_rows) ? uint32_t(id) : uint32_t(p.n_rows), uint32_t(i));
 }
 
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs p) {
     hagk::pdl_launch_dependents();
-    __shared__ uint32_t bin[kSortBins];
-    bin[threadIdx.x] = 0;
+    constexpr int kCopies = 4;                                // of the counters: fewer warps on one address
+    __shared__ uint32_t bin[kCopies][kSortBins];
+    const int t = threadIdx.x;
+    for (int i = t; i < kCopies * kSortBins; i += kSortThreads) (&bin[0][0])[i] = 0;
     __syncthreads();
     const uint32_t mask = (1u << p.bits) - 1u;
     hagk::pdl_wait();
@@ -185,16 +192,24 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
         return;
     }
     const int32_t begin = blockIdx.x * p.stretch, end = int32_t(min(int64_t(p.n), int64_t(begin) + p.stretch));
-    for (int32_t i = begin + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&bin[(sort_key(p, i) >> p.shift) & mask], 1u);
+    uint32_t *mine = bin[(t >> 5) % kCopies];
+    for (int32_t tile = begin; tile < end; tile += kSortTile) {
+        uint32_t key[kSortItems];
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) key[k] = tile + k * kSortThreads + t < end ? sort_pair(p, tile + k * kSortThreads + t).x : 0;
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k)
+            if (tile + k * kSortThreads + t < end) atomicAdd(&mine[(key[k] >> p.shift) & mask], 1u);
+    }
     __syncthreads();
-    p.count[blockIdx.x * kSortBins + threadIdx.x] = bin[threadIdx.x];
+    if (t < kSortBins) p.count[blockIdx.x * kSortBins + t] = bin[0][t] + bin[1][t] + bin[2][t] + bin[3][t];
 }
 
 __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs p) {
     hagk::pdl_launch_dependents();
     __shared__ uint32_t base[kSortBins];                      // next place of each digit for this block
-    __shared__ uint32_t seen[kSortWarps][kSortBins];          // per warp: keys of the digit so far in this tile
-    __shared__ uint32_t scan[kSortWarps];
+    __shared__ __align__(16) uint32_t seen[kSortWarps][kSortBins];       // per warp: keys of the digit so far in this tile
+    __shared__ uint32_t scan[kSortBins / 32];
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const uint32_t mask = (1u << p.bits) - 1u;
     hagk::pdl_wait();
@@ -203,38 +218,56 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
         return;
     }
     {   // base[d] = keys with a smaller digit + keys of digit d in the blocks before this one
-        uint32_t before = 0, total = 0;
-        #pragma unroll 8
-        for (int b = 0; b < p.blocks; ++b) {
-            const uint32_t c = __ldcg(p.count + b * kSortBins + t);
-            if (b < int(blockIdx.x)) before += c;
-            total += c;
+        constexpr int kQuads = kSortBins / 4, kGroups = kSortThreads / kQuads;           // 64 threads read the counts of one block
+        const int quad = t % kQuads, group = t / kQuads;
+        uint4 before = make_uint4(0, 0, 0, 0), total = before;
+#pragma unroll 10
+        for (int b = group; b < p.blocks; b += kGroups) {
+            const uint4 c = __ldcg(reinterpret_cast<const uint4 *>(p.count + b * kSortBins) + quad);
+            const uint32_t in = b < int(blockIdx.x) ? 0xffffffffu : 0u;
+            total.x += c.x; total.y += c.y; total.z += c.z; total.w += c.w;
+            before.x += c.x & in; before.y += c.y & in; before.z += c.z & in; before.w += c.w & in;
         }
-        uint32_t x = total;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
-        }
-        if (lane == 31) scan[warp] = x;
+        static_assert(2 * kGroups <= kSortWarps, "the sums of the groups share the counters' space");
+        reinterpret_cast<uint4 *>(seen[group])[quad] = total;
+        reinterpret_cast<uint4 *>(seen[kGroups + group])[quad] = before;
         __syncthreads();
-        uint32_t lower = 0;
-        for (int w = 0; w < warp; ++w) lower += scan[w];
-        base[t] = lower + x - total + before;
+        uint32_t all = 0, mine = 0, x = 0;
+        if (t < kSortBins) {
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                all += seen[g][t];
+                mine += seen[kGroups + g][t];
+            }
+            x = all;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+                if (lane >= o) x += y;
+            }
+            if (lane == 31) scan[warp] = x;
+        }
+        __syncthreads();
+        if (t < kSortBins) {
+            uint32_t lower = 0;
+            for (int w = 0; w < warp; ++w) lower += scan[w];
+            base[t] = lower + x - all + mine;
+        }
     }
     const int32_t begin = blockIdx.x * p.stretch, end = int32_t(min(int64_t(p.n), int64_t(begin) + p.stretch));
     for (int32_t tile = begin; tile < end; tile += kSortTile) {
-#pragma unroll
-        for (int w = 0; w < kSortWarps; ++w) seen[w][t] = 0;
-        __syncthreads();
-        uint32_t key[kSortItems], rank[kSortItems];
+        uint2 pair[kSortItems];
+        uint32_t rank[kSortItems];
         const int32_t mine = tile + warp * (32 * kSortItems) + lane;      // a warp's keys are consecutive: stable
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) key[k] = mine + 32 * k < end ? sort_key(p, mine + 32 * k) : 0xffffffffu;
+        for (int k = 0; k < kSortItems; ++k) pair[k] = mine + 32 * k < end ? sort_pair(p, mine + 32 * k) : make_uint2(0xffffffffu, 0);
+        __syncthreads();
+        for (int i = t; i < kSortWarps * kSortBins / 4; i += kSortThreads) reinterpret_cast<uint4 *>(&seen[0][0])[i] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k) {
             const bool live = mine + 32 * k < end;
-            const uint32_t digit = (key[k] >> p.shift) & mask;
+            const uint32_t digit = (pair[k].x >> p.shift) & mask;
             const uint32_t same = __match_any_sync(0xffffffffu, live ? digit : 0xffffffffu);
             const uint32_t old = live ? seen[warp][digit] : 0;
             rank[k] = old + __popc(same & ((1u << lane) - 1u));
@@ -243,7 +276,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
             __syncwarp();
         }
         __syncthreads();
-        {   // per digit: the counts of the warps become their first places; base moves on
+        if (t < kSortBins) {   // per digit: the counts of the warps become their first places; base moves on
             uint32_t at = base[t];
 #pragma unroll
             for (int w = 0; w < kSortWarps; ++w) {
@@ -255,14 +288,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) {
-            const int32_t i = mine + 32 * k;
-            if (i >= end) continue;
-            const uint32_t to = seen[warp][(key[k] >> p.shift) & mask] + rank[k];
-            p.key_out[to] = key[k];
-            p.place_out[to] = p.place_in ? __ldcg(p.place_in + i) : uint32_t(i);
-        }
-        __syncthreads();
+        for (int k = 0; k < kSortItems; ++k)
+            if (mine + 32 * k < end) p.out[seen[warp][(pair[k].x >> p.shift) & mask] + rank[k]] = pair[k];
     }
 }
 
@@ -273,7 +300,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
 // the stretch leaves a partial row: the one that was open at the stretch's start in `head`, the one that is open at its
 // end in `tail`; embedding_join_kernel adds those up in the order of the stretches.
 struct SumArgs {
-    const uint32_t *key, *place;     // sorted; readable in whole groups of kSumBatch
+    const uint2 *list;               // {key, place} sorted; readable in whole groups of kSumBatch
     int32_t n;
     int32_t n_rows;                  // V
     const void *grad;
@@ -289,6 +316,8 @@ struct SumArgs {
 };
 constexpr int kSumThreads = 256;
 constexpr int kSumBatch = 8;         // rows in flight per worker
+
+__device__ __forceinline__ uint32_t list_key(const SumArgs &p, int64_t i) { return __ldcg(&p.list[i].x); }
 
 template <typename TO, int V>
 __device__ __forceinline__ void store_row(const SumArgs &p, uint32_t key, int vec, const float *acc) {
@@ -311,7 +340,7 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
     hagk::pdl_wait();
     if (t0 >= t1) return;
     const uint32_t none = 0xffffffffu, rows = uint32_t(p.n_rows);
-    const uint32_t before = t0 > 0 ? __ldcg(p.key + t0 - 1) : none, after = t1 < p.n ? __ldcg(p.key + t1) : none;
+    const uint32_t before = t0 > 0 ? list_key(p, t0 - 1) : none, after = t1 < p.n ? list_key(p, t1) : none;
     const int64_t part = int64_t(worker) * ((p.D + 3) & ~3) + int64_t(vec) * V;
     auto leave = [&](float *at, const float *acc) {
         if (!column) return;
@@ -321,10 +350,9 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
     uint32_t key[kSumBatch], place[kSumBatch];
     auto fetch = [&](int32_t t) {
 #pragma unroll
-        for (int h = 0; h < kSumBatch; h += 4) {
-            const uint4 k = __ldcg(reinterpret_cast<const uint4 *>(p.key + t + h)), q = __ldcg(reinterpret_cast<const uint4 *>(p.place + t + h));
-            key[h] = k.x; key[h + 1] = k.y; key[h + 2] = k.z; key[h + 3] = k.w;
-            place[h] = q.x; place[h + 1] = q.y; place[h + 2] = q.z; place[h + 3] = q.w;
+        for (int h = 0; h < kSumBatch; h += 2) {
+            const uint4 q = __ldcg(reinterpret_cast<const uint4 *>(p.list + t + h));
+            key[h] = q.x; place[h] = q.y; key[h + 1] = q.z; place[h + 1] = q.w;
         }
     };
     fetch(t0);
@@ -374,72 +402,89 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
 
 // Rows whose runs cross stretches: the tail of the stretch where the run begins and the heads of the following
 // stretches that begin with it.  A warp takes one stretch; chains of more than kLongChain heads (an id that fills
-// many stretches) are taken by all the warps of the block together.
-constexpr int kJoinWarps = 8;
-constexpr int kLongChain = 16;
+// many stretches) are taken by all the warps of the block together, every group of lanes a share of the heads.
+constexpr int kJoinThreads = 512;
+constexpr int kJoinWarps = kJoinThreads / 32;
+constexpr int kLongChain = 12;
 
-template <typename TO>
-__device__ __forceinline__ void join_store(const SumArgs &p, uint32_t key, int c, float v) {
-    hagr::Vec<TO, 1> o;
-    v *= p.scale;
-    o.set(&v);
-    o.store(static_cast<TO *>(p.out) + int64_t(key) * p.ld_out, c);
+__device__ __forceinline__ float4 add4(float4 a, float4 b) {
+    const float2 lo = __fadd2_rn(make_float2(a.x, a.y), make_float2(b.x, b.y)), hi = __fadd2_rn(make_float2(a.z, a.w), make_float2(b.z, b.w));
+    return make_float4(lo.x, lo.y, hi.x, hi.y);
 }
 
 template <typename TO>
-__global__ void __launch_bounds__(32 * kJoinWarps) embedding_join_kernel(const SumArgs p) {
+__device__ __forceinline__ void join_store(const SumArgs &p, uint32_t key, int quad, float4 v) {
+    const float f[4] = {v.x * p.scale, v.y * p.scale, v.z * p.scale, v.w * p.scale};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (quad * 4 + j >= p.D) break;
+        hagr::Vec<TO, 1> o;
+        o.set(f + j);
+        o.store(static_cast<TO *>(p.out) + int64_t(key) * p.ld_out, quad * 4 + j);
+    }
+}
+
+template <typename TO>
+__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const SumArgs p) {
     hagk::pdl_launch_dependents();
     __shared__ int chain[kJoinWarps];
-    __shared__ float sum[kJoinWarps][32];
+    __shared__ float4 sum[kJoinThreads];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int w0 = blockIdx.x * kJoinWarps, w = w0 + warp;
-    const int64_t width = (p.D + 3) & ~3;
+    const int quads = (p.D + 3) / 4;                           // of a partial row
+    const float4 *head = reinterpret_cast<const float4 *>(p.head), *tail = reinterpret_cast<const float4 *>(p.tail);
     hagk::pdl_wait();
     // heads that continue the run open at the end of stretch `w`; 0: none begins there
     int heads = 0;
     uint32_t key = 0;
     const int64_t t1 = (int64_t(w) + 1) * p.stretch;
     if (w < p.workers && t1 < p.n) {
-        key = __ldcg(p.key + t1 - 1);
+        key = list_key(p, t1 - 1);
         const int64_t t0 = t1 - p.stretch;
-        const bool begins = !(__ldcg(p.key + t0) == key && t0 > 0 && __ldcg(p.key + t0 - 1) == key);
+        const bool begins = !(list_key(p, t0) == key && t0 > 0 && list_key(p, t0 - 1) == key);
         if (begins && key < uint32_t(p.n_rows)) {
-            for (int j = w + 1;; j += 32) {
-                const bool in = j + lane < p.workers && __ldcg(p.key + int64_t(j + lane) * p.stretch) == key;
-                const int c = __popc(__ballot_sync(0xffffffffu, in));
+            for (int j = w + 1;; j += 128) {
+                int c = 0;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int i = j + 32 * u + lane;
+                    c += __popc(__ballot_sync(0xffffffffu, i < p.workers && list_key(p, int64_t(i) * p.stretch) == key));
+                }
                 heads += c;
-                if (c < 32) break;
+                if (c < 128) break;
             }
         }
     }
     if (lane == 0) chain[warp] = heads;
     __syncthreads();
     if (heads > 0 && heads <= kLongChain)
-        for (int c = lane; c < p.D; c += 32) {
-            float v = __ldcg(p.tail + w * width + c);
+        for (int q = lane; q < quads; q += 32) {
+            float4 v = __ldcg(tail + int64_t(w) * quads + q);
 #pragma unroll 4
-            for (int j = 1; j <= heads; ++j) v += __ldcg(p.head + (w + j) * width + c);
-            join_store<TO>(p, key, c, v);
+            for (int j = 1; j <= heads; ++j) v = add4(v, __ldcg(head + int64_t(w + j) * quads + q));
+            join_store<TO>(p, key, q, v);
         }
-    for (int q = 0; q < kJoinWarps; ++q) {
-        const int count = chain[q];                            // the same for all threads
+    int lanes = 4;                                             // that cover a partial row, or 128 quads of it
+    while (lanes < 128 && lanes < quads) lanes *= 2;
+    const int group = threadIdx.x / lanes, groups = kJoinThreads / lanes;
+    for (int x = 0; x < kJoinWarps; ++x) {
+        const int count = chain[x];                            // the same for all threads
         if (count <= kLongChain) continue;
-        const uint32_t k = __ldcg(p.key + (int64_t(w0 + q) + 1) * p.stretch - 1);
-        for (int c0 = 0; c0 < p.D; c0 += 32) {
-            const int c = c0 + lane;
-            float v = 0.0f;
-            if (c < p.D) {
-                if (warp == 0) v = __ldcg(p.tail + (w0 + q) * width + c);
+        const uint32_t k = list_key(p, (int64_t(w0 + x) + 1) * p.stretch - 1);
+        for (int q0 = 0; q0 < quads; q0 += lanes) {
+            const int q = q0 + threadIdx.x % lanes;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (q < quads) {
+                if (group == 0) v = __ldcg(tail + int64_t(w0 + x) * quads + q);
 #pragma unroll 8
-                for (int j = 1 + warp; j <= count; j += kJoinWarps) v += __ldcg(p.head + (w0 + q + j) * width + c);
+                for (int j = 1 + group; j <= count; j += groups) v = add4(v, __ldcg(head + int64_t(w0 + x + j) * quads + q));
             }
             __syncthreads();
-            sum[warp][lane] = v;
+            sum[threadIdx.x] = v;
             __syncthreads();
-            if (warp == 0 && c < p.D) {
-#pragma unroll
-                for (int x = 1; x < kJoinWarps; ++x) v += sum[x][lane];
-                join_store<TO>(p, k, c, v);
+            if (group == 0 && q < quads) {
+                for (int g = 1; g < groups; ++g) v = add4(v, sum[g * lanes + threadIdx.x]);
+                join_store<TO>(p, k, q, v);
             }
         }
     }
@@ -468,7 +513,7 @@ cudaError_t launch_sum(SumArgs &p, cudaStream_t s) {
     cfg.numAttrs = 1;
     cudaError_t err = cudaLaunchKernelEx(&cfg, embedding_sum_kernel<TG, TO, V>, p);
     if (err == cudaSuccess && p.workers > 1)
-        err = hagl::launch_pdl(embedding_join_kernel<TO>, unsigned((p.workers + kJoinWarps - 1) / kJoinWarps), unsigned(32 * kJoinWarps), p, s);
+        err = hagl::launch_pdl(embedding_join_kernel<TO>, unsigned((p.workers + kJoinWarps - 1) / kJoinWarps), unsigned(kJoinThreads), p, s);
     return err;
 }
 
@@ -516,7 +561,7 @@ SortPlan sort_plan(int32_t n, int32_t n_rows) {
 }
 
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
-size_t list_bytes(int64_t n) { return up256((size_t(n) + kSumBatch) * 4); }
+size_t list_bytes(int64_t n) { return up256((size_t(n) + kSumBatch) * sizeof(uint2)); }
 
 // Blocks that clear a launch's share of the rows: 32 KB each, four per SM at most.
 int fill_blocks(const FillArgs &f) {
@@ -565,7 +610,7 @@ extern "C" hag_status hag_embedding_fwd(const void *ids, hag_id_type id_type, in
 
 extern "C" size_t hag_embedding_bwd_workspace_bytes(int64_t n, int64_t n_rows, int32_t D) {
     if (n <= 0 || n > 0x7fffffffLL - kSortTile || n_rows < 0 || D <= 0) return 0;
-    return 4 * list_bytes(n) + up256(size_t(kSortMaxBlocks) * kSortBins * 4) + 2 * up256(size_t(partial_floats(n, D)) * 4);
+    return 2 * list_bytes(n) + up256(size_t(kSortMaxBlocks) * kSortBins * 4) + 2 * up256(size_t(partial_floats(n, D)) * 4);
 }
 
 extern "C" hag_status hag_embedding_bwd(const void *ids, hag_id_type id_type, int64_t n, int64_t n_rows, hag_dtype dtype, int32_t D,
@@ -589,10 +634,9 @@ extern "C" hag_status hag_embedding_bwd(const void *ids, hag_id_type id_type, in
         return HAG_OK;
     }
     const size_t part = list_bytes(n);
-    uint32_t *key[2] = {reinterpret_cast<uint32_t *>(w), reinterpret_cast<uint32_t *>(w + part)};
-    uint32_t *place[2] = {reinterpret_cast<uint32_t *>(w + 2 * part), reinterpret_cast<uint32_t *>(w + 3 * part)};
-    uint32_t *count = reinterpret_cast<uint32_t *>(w + 4 * part);
-    char *partials = w + 4 * part + up256(size_t(kSortMaxBlocks) * kSortBins * 4);
+    uint2 *list[2] = {reinterpret_cast<uint2 *>(w), reinterpret_cast<uint2 *>(w + part)};
+    uint32_t *count = reinterpret_cast<uint32_t *>(w + 2 * part);
+    char *partials = w + 2 * part + up256(size_t(kSortMaxBlocks) * kSortBins * 4);
     int side = 0;
     const SortPlan plan = sort_plan(int32_t(n), int32_t(n_rows));
     const int launches = 2 * plan.passes;
@@ -601,12 +645,11 @@ extern "C" hag_status hag_embedding_bwd(const void *ids, hag_id_type id_type, in
         fill.rows_begin = int32_t(n_rows * k / launches);
         fill.rows_end = int32_t(n_rows * (k + 1) / launches);
         fill.blocks = fill_blocks(fill);
-        const SortArgs a{ids, id_type == HAG_ID64, int32_t(n_rows), pass ? key[side] : nullptr, pass ? place[side] : nullptr,
-                         key[side ^ 1], place[side ^ 1], count, int32_t(n), plan.stretch, pass * plan.bits, plan.bits, plan.blocks, fill};
+        const SortArgs a{ids, id_type == HAG_ID64, int32_t(n_rows), pass ? list[side] : nullptr, list[side ^ 1], count, int32_t(n), plan.stretch, pass * plan.bits, plan.bits, plan.blocks, fill};
         err = hagl::launch_pdl(k % 2 ? sort_move_kernel : sort_count_kernel, unsigned(plan.blocks + fill.blocks), unsigned(kSortThreads), a, s);
         if (k % 2) side ^= 1;
     }
-    SumArgs q{key[side], place[side], int32_t(n), int32_t(n_rows), grad_out, ld_grad_out, grad_table, ld_grad_table, D, scale, 0, 0, 0,
+    SumArgs q{list[side], int32_t(n), int32_t(n_rows), grad_out, ld_grad_out, grad_table, ld_grad_table, D, scale, 0, 0, 0,
               reinterpret_cast<float *>(partials), reinterpret_cast<float *>(partials + up256(size_t(partial_floats(n, D)) * 4))};
     if (err == cudaSuccess) {
         if (dtype == HAG_F32)

@@ -18,25 +18,32 @@ template <> struct Words<8> { uint32_t w[2]; };
 template <> struct Words<16> { uint32_t w[4]; };
 template <> struct Words<32> { uint32_t w[8]; };
 
-// Cache operator of a load: kKeep leaves the line where later reads find it, kOnce marks it evict-first (data that
-// is read once must not push out rows that are read again).
-enum CacheOp { kKeep, kOnce };
+// Cache operator of a load: kKeep leaves the line in the L2, kOnce marks it evict-first (data that is read once must
+// not push out rows that are read again), kNear also keeps it in the SM's own L1 (rows that the same SM reads again).
+enum CacheOp { kKeep, kOnce, kNear };
+
+template <CacheOp OP, typename W>
+__device__ __forceinline__ W load_word(const W *p) {
+    if constexpr (OP == kOnce) return __ldcs(p);
+    else if constexpr (OP == kNear) return __ldca(p);
+    else return __ldcg(p);
+}
 
 template <CacheOp OP, int B>
 __device__ __forceinline__ Words<B> load_words(const void *p) {
     Words<B> r;
     if constexpr (B == 2) {
-        r.w[0] = OP == kOnce ? __ldcs(static_cast<const uint16_t *>(p)) : __ldcg(static_cast<const uint16_t *>(p));
+        r.w[0] = load_word<OP>(static_cast<const uint16_t *>(p));
     } else if constexpr (B == 4) {
-        r.w[0] = OP == kOnce ? __ldcs(static_cast<const uint32_t *>(p)) : __ldcg(static_cast<const uint32_t *>(p));
+        r.w[0] = load_word<OP>(static_cast<const uint32_t *>(p));
     } else if constexpr (B == 8) {
-        const uint2 q = OP == kOnce ? __ldcs(static_cast<const uint2 *>(p)) : __ldcg(static_cast<const uint2 *>(p));
+        const uint2 q = load_word<OP>(static_cast<const uint2 *>(p));
         r.w[0] = q.x; r.w[1] = q.y;
     } else {
 #pragma unroll
         for (int h = 0; h < B / 16; ++h) {
             const uint4 *s = static_cast<const uint4 *>(p) + h;
-            const uint4 q = OP == kOnce ? __ldcs(s) : __ldcg(s);
+            const uint4 q = load_word<OP>(s);
             r.w[4 * h] = q.x; r.w[4 * h + 1] = q.y; r.w[4 * h + 2] = q.z; r.w[4 * h + 3] = q.w;
         }
     }
