@@ -110,7 +110,7 @@ struct FillArgs {
     int32_t elem;                      // bytes
     int32_t blocks;
 };
-constexpr int kFillThreads = 512;      // those of the sort's launches
+constexpr int kFillThreads = 1024;     // those of the sort's launches
 
 // Threads tid, tid + step, ... clear `bytes` bytes at p (a multiple of the element, 2 or 4).
 __device__ __forceinline__ void clear_span(char *p, int64_t bytes, int elem, int64_t tid, int64_t step) {
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kFillThreads) fill_kernel(const FillArgs f) {
 // every block adds up the counts of all blocks and moves its stretch to the places found (sort_move_kernel).  Within a
 // block a key's place comes from the lanes of its warp that hold the same digit (match), the warp's count so far and
 // the counts of the warps before it: keys keep their order, and nothing depends on the order of atomics.
-constexpr int kSortThreads = 512;
+constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortItems = 8;                                 // keys per thread and tile
 constexpr int kSortTile = kSortThreads * kSortItems;
@@ -264,15 +264,17 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
         __syncthreads();
         for (int i = t; i < kSortWarps * kSortBins / 4; i += kSortThreads) reinterpret_cast<uint4 *>(&seen[0][0])[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
+        // places beyond the end hold the largest key: they count after all others of the tile, which is the last one
+        uint32_t same[kSortItems];
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) same[k] = __match_any_sync(0xffffffffu, (pair[k].x >> p.shift) & mask);
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k) {
-            const bool live = mine + 32 * k < end;
-            const uint32_t digit = (pair[k].x >> p.shift) & mask;
-            const uint32_t same = __match_any_sync(0xffffffffu, live ? digit : 0xffffffffu);
-            const uint32_t old = live ? seen[warp][digit] : 0;
-            rank[k] = old + __popc(same & ((1u << lane) - 1u));
+            uint32_t *count = &seen[warp][(pair[k].x >> p.shift) & mask];
+            const uint32_t below = __popc(same[k] & ((1u << lane) - 1u));
+            rank[k] = *count + below;
             __syncwarp();
-            if (live && (same >> lane) == 1u) seen[warp][digit] = old + __popc(same);      // the highest lane of the digit
+            if ((same[k] >> lane) == 1u) *count = rank[k] + 1;            // the highest lane of the digit
             __syncwarp();
         }
         __syncthreads();
