@@ -18,6 +18,28 @@
 
 namespace {
 
+template <typename Args>
+cudaError_t launch_with(void (*kernel)(Args), dim3 grid, unsigned threads, size_t shared, const Args &args, cudaStream_t s) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args);
+}
+
+template <typename Args>
+bool allow_shared(void (*kernel)(Args), size_t bytes) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) == cudaSuccess) return true;
+    cudaGetLastError();
+    return false;
+}
+
 constexpr int kCopyThreads = 256;
 // Vectors per thread: 64 bytes of the wider type in flight, narrow vectors at most 8.
 template <int BYTES> constexpr int kCopyUnroll = BYTES >= 16 ? 4 : 8;
@@ -149,7 +171,7 @@ __global__ void __launch_bounds__(kFillThreads) fill_kernel(const FillArgs f) {
 // Stable radix sort of (key, place) pairs by key; key = the id, or V for a place without a token (those come last).
 // Each pass is two launches: every block counts the digits of its own stretch of the list (sort_count_kernel); then
 // every block adds up the counts of all blocks and moves its stretch to the places found (sort_move_kernel).  Within a
-// block a key's place comes from the lanes of its warp that hold the same digit (match), the warp's count so far and
+// block a key's place comes from the lanes of its warp that hold the same digit, the warp's count so far and
 // the counts of the warps before it: keys keep their order, and nothing depends on the order of atomics.
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
@@ -168,6 +190,7 @@ struct SortArgs {
     int32_t n;
     int32_t stretch;         // keys per block, a multiple of the tile
     int32_t shift, bits;
+    int32_t passes;          // of the single-launch form
     int32_t blocks;          // that sort; the blocks after them clear rows of the gradient
     FillArgs fill;
 };
@@ -205,11 +228,89 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
     if (t < kSortBins) p.count[blockIdx.x * kSortBins + t] = bin[0][t] + bin[1][t] + bin[2][t] + bin[3][t];
 }
 
+// What a block needs to order a tile of pairs by one digit.
+struct SortShared {
+    uint2 pair[kSortTile];
+    uint32_t seen[kSortWarps][kSortBins];      // per warp: keys of the digit so far; then the first place of the warp's keys in the tile
+    uint32_t base[kSortBins];                  // next place in the list of each digit of this block
+    uint32_t shift_by[kSortBins];              // place in the list minus place in the tile
+    uint32_t scan[kSortBins / 32];
+};
+
+// Exclusive sums over the bins, for the first kSortBins threads; all threads call it.
+__device__ __forceinline__ uint32_t bin_scan(uint32_t count, uint32_t *scan) {
+    const int t = threadIdx.x, lane = t & 31;
+    uint32_t x = count;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (t < kSortBins && lane == 31) scan[t >> 5] = x;
+    __syncthreads();
+    uint32_t lower = 0;
+#pragma unroll
+    for (int w = 0; w < kSortBins / 32; ++w)
+        if (w < (t >> 5)) lower += scan[w];
+    return lower + x - count;
+}
+
+// Orders a tile by the digit at `shift`: the pairs (in registers, a warp's are consecutive in the list) end in
+// sm.pair.  Returns, for threads below kSortBins, how many keys have digit t; sm.shift_by[t] is set from `base`.
+__device__ __forceinline__ uint32_t sort_tile(SortShared &sm, const uint2 (&pair)[kSortItems], int shift, uint32_t mask, uint32_t base) {
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    for (int i = t; i < kSortWarps * kSortBins / 4; i += kSortThreads) reinterpret_cast<uint4 *>(&sm.seen[0][0])[i] = make_uint4(0, 0, 0, 0);
+    uint32_t same[kSortItems], rank[kSortItems];
+    // lanes with the same digit, bit by bit: a vote per bit costs about a fifth of what the match instruction takes on
+    // digits that mostly differ (10 000 cycles per tile there)
+#pragma unroll
+    for (int k = 0; k < kSortItems; ++k) same[k] = 0xffffffffu;
+#pragma unroll
+    for (int bit = 0; bit < 8; ++bit) {
+        if ((mask >> bit) == 0) break;
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) {
+            const bool set = (pair[k].x >> (shift + bit)) & 1u;
+            const uint32_t votes = __ballot_sync(0xffffffffu, set);
+            same[k] &= set ? votes : ~votes;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSortItems; ++k) {
+        uint32_t *count = &sm.seen[warp][(pair[k].x >> shift) & mask];
+        rank[k] = *count + __popc(same[k] & ((1u << lane) - 1u));
+        __syncwarp();
+        if ((same[k] >> lane) == 1u) *count = rank[k] + 1;                // the highest lane of the digit
+        __syncwarp();
+    }
+    __syncthreads();
+    uint32_t all = 0, c[kSortWarps];
+    if (t < kSortBins) {
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) {
+            c[w] = all;
+            all += sm.seen[w][t];
+        }
+    }
+    const uint32_t first = bin_scan(all, sm.scan);
+    if (t < kSortBins) {
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) sm.seen[w][t] = first + c[w];
+        sm.shift_by[t] = base - first;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSortItems; ++k) sm.pair[sm.seen[warp][(pair[k].x >> shift) & mask] + rank[k]] = pair[k];
+    __syncthreads();
+    return all;
+}
+
 __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs p) {
     hagk::pdl_launch_dependents();
-    __shared__ uint32_t base[kSortBins];                      // next place of each digit for this block
-    __shared__ __align__(16) uint32_t seen[kSortWarps][kSortBins];       // per warp: keys of the digit so far in this tile
-    __shared__ uint32_t scan[kSortBins / 32];
+    extern __shared__ __align__(16) char raw[];
+    SortShared &sm = *reinterpret_cast<SortShared *>(raw);
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const uint32_t mask = (1u << p.bits) - 1u;
     hagk::pdl_wait();
@@ -217,7 +318,18 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
         fill_rows(p.fill, blockIdx.x - p.blocks);
         return;
     }
-    {   // base[d] = keys with a smaller digit + keys of digit d in the blocks before this one
+    const int32_t begin = blockIdx.x * p.stretch, end = int32_t(min(int64_t(p.n), int64_t(begin) + p.stretch));
+    uint2 pair[kSortItems];
+    // a warp's keys are consecutive: stable.  Places beyond the end hold the largest key and come after all others of
+    // the tile, which is the list's last.
+    auto load = [&](int32_t tile) {
+        const int32_t mine = tile + warp * (32 * kSortItems) + lane;
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) pair[k] = mine + 32 * k < end ? sort_pair(p, mine + 32 * k) : make_uint2(0xffffffffu, 0);
+    };
+    load(begin);
+    uint32_t base = 0;       // for t < kSortBins: keys with a smaller digit + keys of digit t in the blocks before this one
+    {
         constexpr int kQuads = kSortBins / 4, kGroups = kSortThreads / kQuads;           // 64 threads read the counts of one block
         const int quad = t % kQuads, group = t / kQuads;
         uint4 before = make_uint4(0, 0, 0, 0), total = before;
@@ -229,70 +341,59 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
             before.x += c.x & in; before.y += c.y & in; before.z += c.z & in; before.w += c.w & in;
         }
         static_assert(2 * kGroups <= kSortWarps, "the sums of the groups share the counters' space");
-        reinterpret_cast<uint4 *>(seen[group])[quad] = total;
-        reinterpret_cast<uint4 *>(seen[kGroups + group])[quad] = before;
+        reinterpret_cast<uint4 *>(sm.seen[group])[quad] = total;
+        reinterpret_cast<uint4 *>(sm.seen[kGroups + group])[quad] = before;
         __syncthreads();
-        uint32_t all = 0, mine = 0, x = 0;
+        uint32_t all = 0;
         if (t < kSortBins) {
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
-                all += seen[g][t];
-                mine += seen[kGroups + g][t];
+                all += sm.seen[g][t];
+                base += sm.seen[kGroups + g][t];
             }
-            x = all;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-            }
-            if (lane == 31) scan[warp] = x;
         }
-        __syncthreads();
-        if (t < kSortBins) {
-            uint32_t lower = 0;
-            for (int w = 0; w < warp; ++w) lower += scan[w];
-            base[t] = lower + x - all + mine;
-        }
+        base += bin_scan(all, sm.scan);
     }
-    const int32_t begin = blockIdx.x * p.stretch, end = int32_t(min(int64_t(p.n), int64_t(begin) + p.stretch));
     for (int32_t tile = begin; tile < end; tile += kSortTile) {
-        uint2 pair[kSortItems];
-        uint32_t rank[kSortItems];
-        const int32_t mine = tile + warp * (32 * kSortItems) + lane;      // a warp's keys are consecutive: stable
-#pragma unroll
-        for (int k = 0; k < kSortItems; ++k) pair[k] = mine + 32 * k < end ? sort_pair(p, mine + 32 * k) : make_uint2(0xffffffffu, 0);
+        if (tile != begin) load(tile);
         __syncthreads();
-        for (int i = t; i < kSortWarps * kSortBins / 4; i += kSortThreads) reinterpret_cast<uint4 *>(&seen[0][0])[i] = make_uint4(0, 0, 0, 0);
-        __syncthreads();
-        // places beyond the end hold the largest key: they count after all others of the tile, which is the last one
-        uint32_t same[kSortItems];
-#pragma unroll
-        for (int k = 0; k < kSortItems; ++k) same[k] = __match_any_sync(0xffffffffu, (pair[k].x >> p.shift) & mask);
+        base += sort_tile(sm, pair, p.shift, mask, base);
+        const int32_t len = min(end - tile, kSortTile);
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k) {
-            uint32_t *count = &seen[warp][(pair[k].x >> p.shift) & mask];
-            const uint32_t below = __popc(same[k] & ((1u << lane) - 1u));
-            rank[k] = *count + below;
-            __syncwarp();
-            if ((same[k] >> lane) == 1u) *count = rank[k] + 1;            // the highest lane of the digit
-            __syncwarp();
+            const int i = k * kSortThreads + t;
+            if (i >= len) continue;
+            const uint2 q = sm.pair[i];
+            p.out[sm.shift_by[(q.x >> p.shift) & mask] + i] = q;          // neighbours mostly go to neighbouring places
         }
-        __syncthreads();
-        if (t < kSortBins) {   // per digit: the counts of the warps become their first places; base moves on
-            uint32_t at = base[t];
-#pragma unroll
-            for (int w = 0; w < kSortWarps; ++w) {
-                const uint32_t c = seen[w][t];
-                seen[w][t] = at;
-                at += c;
-            }
-            base[t] = at;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kSortItems; ++k)
-            if (mine + 32 * k < end) p.out[seen[warp][(pair[k].x >> p.shift) & mask] + rank[k]] = pair[k];
     }
+}
+
+// A list of one tile: all passes in one launch, the pairs stay in shared memory.
+__global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const SortArgs p) {
+    hagk::pdl_launch_dependents();
+    extern __shared__ __align__(16) char raw[];
+    SortShared &sm = *reinterpret_cast<SortShared *>(raw);
+    const int t = threadIdx.x;
+    const uint32_t mask = (1u << p.bits) - 1u;
+    hagk::pdl_wait();
+    if (blockIdx.x >= 1) {
+        fill_rows(p.fill, blockIdx.x - 1);
+        return;
+    }
+    const int mine = (t >> 5) * (32 * kSortItems) + (t & 31);
+    uint2 pair[kSortItems];
+#pragma unroll
+    for (int k = 0; k < kSortItems; ++k) pair[k] = mine + 32 * k < p.n ? sort_pair(p, mine + 32 * k) : make_uint2(0xffffffffu, 0);
+    for (int pass = 0; pass < p.passes; ++pass) {
+        sort_tile(sm, pair, pass * p.bits, mask, 0);
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) pair[k] = sm.pair[mine + 32 * k];
+        __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < kSortItems; ++k)
+        if (mine + 32 * k < p.n) p.out[mine + 32 * k] = pair[k];
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -408,6 +509,7 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
 constexpr int kJoinThreads = 512;
 constexpr int kJoinWarps = kJoinThreads / 32;
 constexpr int kLongChain = 12;
+constexpr int kJoinQuads = 32;          // a block's columns, in fours
 
 __device__ __forceinline__ float4 add4(float4 a, float4 b) {
     const float2 lo = __fadd2_rn(make_float2(a.x, a.y), make_float2(b.x, b.y)), hi = __fadd2_rn(make_float2(a.z, a.w), make_float2(b.z, b.w));
@@ -430,7 +532,7 @@ template <typename TO>
 __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const SumArgs p) {
     hagk::pdl_launch_dependents();
     __shared__ int chain[kJoinWarps];
-    __shared__ float4 sum[kJoinThreads];
+    __shared__ float4 sum[kJoinWarps][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int w0 = blockIdx.x * kJoinWarps, w = w0 + warp;
     const int quads = (p.D + 3) / 4;                           // of a partial row
@@ -460,34 +562,36 @@ __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const SumA
     if (lane == 0) chain[warp] = heads;
     __syncthreads();
     if (heads > 0 && heads <= kLongChain)
-        for (int q = lane; q < quads; q += 32) {
+        if (const int q = blockIdx.y * kJoinQuads + lane; q < quads) {
             float4 v = __ldcg(tail + int64_t(w) * quads + q);
 #pragma unroll 4
             for (int j = 1; j <= heads; ++j) v = add4(v, __ldcg(head + int64_t(w + j) * quads + q));
             join_store<TO>(p, key, q, v);
         }
-    int lanes = 4;                                             // that cover a partial row, or 128 quads of it
-    while (lanes < 128 && lanes < quads) lanes *= 2;
+    int lanes = 4;                                             // that cover the columns of this block
+    while (lanes < kJoinQuads && lanes < quads) lanes *= 2;
     const int group = threadIdx.x / lanes, groups = kJoinThreads / lanes;
     for (int x = 0; x < kJoinWarps; ++x) {
         const int count = chain[x];                            // the same for all threads
         if (count <= kLongChain) continue;
         const uint32_t k = list_key(p, (int64_t(w0 + x) + 1) * p.stretch - 1);
-        for (int q0 = 0; q0 < quads; q0 += lanes) {
-            const int q = q0 + threadIdx.x % lanes;
-            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (q < quads) {
-                if (group == 0) v = __ldcg(tail + int64_t(w0 + x) * quads + q);
+        const int q = blockIdx.y * kJoinQuads + threadIdx.x % lanes;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (q < quads) {
+            if (group == 0) v = __ldcg(tail + int64_t(w0 + x) * quads + q);
 #pragma unroll 8
-                for (int j = 1 + group; j <= count; j += groups) v = add4(v, __ldcg(head + int64_t(w0 + x + j) * quads + q));
-            }
-            __syncthreads();
-            sum[threadIdx.x] = v;
-            __syncthreads();
-            if (group == 0 && q < quads) {
-                for (int g = 1; g < groups; ++g) v = add4(v, sum[g * lanes + threadIdx.x]);
-                join_store<TO>(p, k, q, v);
-            }
+            for (int j = 1 + group; j <= count; j += groups) v = add4(v, __ldcg(head + int64_t(w0 + x + j) * quads + q));
+        }
+        for (int o = lanes; o < 32; o *= 2)                    // the groups of a warp, then the warps
+            v = add4(v, make_float4(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o),
+                                    __shfl_xor_sync(0xffffffffu, v.z, o), __shfl_xor_sync(0xffffffffu, v.w, o)));
+        __syncthreads();
+        if (lane < lanes) sum[warp][lane] = v;
+        __syncthreads();
+        if (group == 0 && q < quads) {
+#pragma unroll
+            for (int y = 1; y < kJoinWarps; ++y) v = add4(v, sum[y][lane]);
+            join_store<TO>(p, k, q, v);
         }
     }
 }
@@ -504,18 +608,13 @@ cudaError_t launch_sum(SumArgs &p, cudaStream_t s) {
     const int64_t batches = (int64_t(p.n) + kSumBatch - 1) / kSumBatch;
     p.stretch = int32_t((batches + most - 1) / most * kSumBatch);
     p.workers = int32_t((int64_t(p.n) + p.stretch - 1) / p.stretch);
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(unsigned((int64_t(p.workers) * p.lanes + kSumThreads - 1) / kSumThreads), unsigned(column_blocks));
-    cfg.blockDim = dim3(kSumThreads);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaError_t err = cudaLaunchKernelEx(&cfg, embedding_sum_kernel<TG, TO, V>, p);
+    cudaError_t err = launch_with(embedding_sum_kernel<TG, TO, V>,
+                                  dim3(unsigned((int64_t(p.workers) * p.lanes + kSumThreads - 1) / kSumThreads), unsigned(column_blocks)),
+                                  kSumThreads, 0, p, s);
     if (err == cudaSuccess && p.workers > 1)
-        err = hagl::launch_pdl(embedding_join_kernel<TO>, unsigned((p.workers + kJoinWarps - 1) / kJoinWarps), unsigned(kJoinThreads), p, s);
+        err = launch_with(embedding_join_kernel<TO>,
+                          dim3(unsigned((p.workers + kJoinWarps - 1) / kJoinWarps), unsigned(((p.D + 3) / 4 + kJoinQuads - 1) / kJoinQuads)),
+                          kJoinThreads, 0, p, s);
     return err;
 }
 
@@ -641,15 +740,23 @@ extern "C" hag_status hag_embedding_bwd(const void *ids, hag_id_type id_type, in
     char *partials = w + 2 * part + up256(size_t(kSortMaxBlocks) * kSortBins * 4);
     int side = 0;
     const SortPlan plan = sort_plan(int32_t(n), int32_t(n_rows));
-    const int launches = 2 * plan.passes;
+    const int launches = plan.blocks == 1 ? 1 : 2 * plan.passes;
+    static const bool sort_ready = allow_shared(sort_move_kernel, sizeof(SortShared)) && allow_shared(sort_small_kernel, sizeof(SortShared));
+    if (!sort_ready) return HAG_ERR_CUDA;
     for (int k = 0; k < launches && err == cudaSuccess; ++k) {
         const int pass = k / 2;
         fill.rows_begin = int32_t(n_rows * k / launches);
         fill.rows_end = int32_t(n_rows * (k + 1) / launches);
         fill.blocks = fill_blocks(fill);
-        const SortArgs a{ids, id_type == HAG_ID64, int32_t(n_rows), pass ? list[side] : nullptr, list[side ^ 1], count, int32_t(n), plan.stretch, pass * plan.bits, plan.bits, plan.blocks, fill};
-        err = hagl::launch_pdl(k % 2 ? sort_move_kernel : sort_count_kernel, unsigned(plan.blocks + fill.blocks), unsigned(kSortThreads), a, s);
-        if (k % 2) side ^= 1;
+        const SortArgs a{ids, id_type == HAG_ID64, int32_t(n_rows), pass ? list[side] : nullptr, list[side ^ 1], count, int32_t(n),
+                         plan.stretch, pass * plan.bits, plan.bits, plan.passes, plan.blocks, fill};
+        if (launches == 1)
+            err = launch_with(sort_small_kernel, dim3(unsigned(1 + fill.blocks)), kSortThreads, sizeof(SortShared), a, s);
+        else if (k % 2 == 0)
+            err = launch_with(sort_count_kernel, dim3(unsigned(plan.blocks + fill.blocks)), kSortThreads, 0, a, s);
+        else
+            err = launch_with(sort_move_kernel, dim3(unsigned(plan.blocks + fill.blocks)), kSortThreads, sizeof(SortShared), a, s);
+        if (launches == 1 || k % 2) side ^= 1;
     }
     SumArgs q{list[side], int32_t(n), int32_t(n_rows), grad_out, ld_grad_out, grad_table, ld_grad_table, D, scale, 0, 0, 0,
               reinterpret_cast<float *>(partials), reinterpret_cast<float *>(partials + up256(size_t(partial_floats(n, D)) * 4))};
