@@ -9,6 +9,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 
 #include "hag.h"
@@ -33,13 +34,26 @@ cudaError_t launch_with(void (*kernel)(Args), dim3 grid, unsigned threads, size_
     return cudaLaunchKernelEx(&cfg, kernel, args);
 }
 
-template <typename Args>
-bool allow_shared(void (*kernel)(Args), size_t bytes) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) == cudaSuccess) return true;
-    cudaGetLastError();
-    return false;
+// Lets the kernel use that much dynamic shared memory on the current device (asked once per device).
+template <auto KERNEL>
+bool allow_shared(size_t bytes) {
+    static std::atomic<uint64_t> ready{0};
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return false;
+    const uint64_t bit = uint64_t(1) << (device & 63);
+    if (ready.load(std::memory_order_relaxed) & bit) return true;
+    if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) != cudaSuccess) return false;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+    return true;
 }
 
+#ifndef TILE_SHARE
+#define TILE_SHARE 4
+#endif
+#ifndef TILE_ONE
+#define TILE_ONE 4096
+#endif
+constexpr int kTileOne = TILE_ONE;
 constexpr int kCopyThreads = 256;
 // Vectors per thread: 64 bytes of the wider type in flight, narrow vectors at most 8.
 template <int BYTES> constexpr int kCopyUnroll = BYTES >= 16 ? 4 : 8;
@@ -639,6 +653,214 @@ int64_t partial_floats(int64_t n, int32_t D) {
     return std::min(workers, batches) * width;
 }
 
+// ---------------------------------------------------------------------------------------------------------------
+// Few rows: no sort of the whole list.  Every block sorts a tile of the tokens in shared memory, adds up its runs as
+// above (its groups of lanes are the workers, heads and tails stay in shared memory), and leaves a table of its own:
+// all rows, its columns.  table_join_kernel adds up the blocks' tables in order.  One tile alone writes the result.
+struct TileArgs {
+    SortArgs sort;               // ids, n, digits; stretch: tokens per tile
+    const void *grad;
+    int64_t ld_grad;
+    void *out;
+    int64_t ld_out;
+    int32_t D;
+    float scale;
+    int32_t lanes;               // per worker
+    float *partial;              // [tiles][n_rows][D], or null: one tile, whose sums are the result
+    int32_t parts;
+    hagr::Divisor per_row;       // D (table_join_kernel)
+};
+constexpr int kTileBatch = 4;    // rows in flight per worker: 32 warps of them
+
+template <typename TO>
+__device__ __forceinline__ void store_scalar(const TileArgs &p, int32_t row, int32_t col, float v) {
+    hagr::Vec<TO, 1> o;
+    v *= p.scale;
+    o.set(&v);
+    o.store(static_cast<TO *>(p.out) + int64_t(row) * p.ld_out, col);
+}
+
+template <typename TG, typename TO, int V>
+__global__ void __launch_bounds__(kSortThreads) embedding_tile_kernel(const __grid_constant__ TileArgs p) {
+    hagk::pdl_launch_dependents();
+    extern __shared__ __align__(16) char raw[];
+    SortShared &sm = *reinterpret_cast<SortShared *>(raw);
+    float *open_rows = reinterpret_cast<float *>(raw + sizeof(SortShared));      // [head, tail][threads * V]
+    const int t = threadIdx.x, rows = p.sort.n_rows;
+    const int32_t begin = blockIdx.x * p.sort.stretch, len = min(p.sort.stretch, p.sort.n - begin);
+    const uint32_t mask = (1u << p.sort.bits) - 1u;
+    hagk::pdl_wait();
+    {
+        const int mine = (t >> 5) * (32 * kSortItems) + (t & 31);
+        uint2 pair[kSortItems];
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) pair[k] = mine + 32 * k < len ? sort_pair(p.sort, begin + mine + 32 * k) : make_uint2(0xffffffffu, 0);
+        // rows that no token of the tile names: cleared while the ids are on their way
+        const int c0 = blockIdx.y * p.lanes * V, width = min(p.D - c0, p.lanes * V);
+        for (int r = t / p.lanes; r < rows; r += kSortThreads / p.lanes)
+            for (int c = t % p.lanes; c < width; c += p.lanes) {
+                if (p.partial) p.partial[(int64_t(blockIdx.x) * rows + r) * p.D + c0 + c] = 0.0f;
+                else store_scalar<TO>(p, r, c0 + c, 0.0f);
+            }
+        for (int pass = 0; pass < p.sort.passes; ++pass) {
+            if (pass) {
+#pragma unroll
+                for (int k = 0; k < kSortItems; ++k) pair[k] = sm.pair[mine + 32 * k];
+                __syncthreads();
+            }
+            sort_tile(sm, pair, pass * p.sort.bits, mask, 0);             // ends with a barrier: the rows are clear too
+        }
+    }
+    const int worker = t / p.lanes, gl = t % p.lanes, workers = kSortThreads / p.lanes, vec = blockIdx.y * p.lanes + gl;
+    const bool column = vec < p.D / V;
+    const int stretch = ((len + workers - 1) / workers + kTileBatch - 1) / kTileBatch * kTileBatch;
+    const int i0 = min(worker * stretch, len), i1 = min(i0 + stretch, len);
+    const uint32_t none = 0xffffffffu;
+    auto finish = [&](uint32_t key, const float *acc) {
+        if (!column || key >= uint32_t(rows)) return;
+        if (p.partial) {
+            float *to = p.partial + (int64_t(blockIdx.x) * rows + key) * p.D + int64_t(vec) * V;
+#pragma unroll
+            for (int j = 0; j < V; ++j) to[j] = acc[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) store_scalar<TO>(p, int32_t(key), vec * V + j, acc[j]);
+        }
+    };
+    float *head = open_rows, *tail = open_rows + kSortThreads * V;       // element j of thread t at [j][t]
+    uint32_t cur = none, after = none;
+    bool from_left = false, begins = false;
+    float acc[V];
+    if (i0 < i1) {
+        const uint32_t before = i0 > 0 ? sm.pair[i0 - 1].x : none;
+        after = i1 < len ? sm.pair[i1].x : none;
+        cur = sm.pair[i0].x;
+        from_left = cur == before;
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = 0.0f;
+        for (int i = i0; i < i1; i += kTileBatch) {
+            uint32_t k[kTileBatch];
+            hagr::Vec<TG, V> g[kTileBatch];
+#pragma unroll
+            for (int u = 0; u < kTileBatch; ++u) {
+                const uint2 q = sm.pair[i + u];                          // readable: the tile is whole
+                k[u] = i + u < i1 ? q.x : none;
+                g[u].zero();
+                if (k[u] < uint32_t(rows) && column)
+                    g[u].template load<hagr::kOnce>(static_cast<const TG *>(p.grad) + int64_t(q.y) * p.ld_grad, vec);
+            }
+            if (k[kTileBatch - 1] == cur) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] += (g[0].get(j) + g[1].get(j)) + (g[2].get(j) + g[3].get(j));
+                continue;
+            }
+#pragma unroll
+            for (int u = 0; u < kTileBatch; ++u) {
+                if (i + u < i1 && k[u] != cur) {
+                    if (from_left) {
+#pragma unroll
+                        for (int j = 0; j < V; ++j) head[j * kSortThreads + t] = acc[j];
+                    } else {
+                        finish(cur, acc);
+                    }
+                    from_left = false;
+                    cur = k[u];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) acc[j] = 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] += g[u].get(j);
+            }
+        }
+        if (from_left) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) head[j * kSortThreads + t] = acc[j];
+        } else if (cur == after) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) tail[j * kSortThreads + t] = acc[j];
+            begins = true;
+        } else {
+            finish(cur, acc);
+        }
+    }
+    __syncthreads();
+    if (!begins) return;
+    // this worker's last run goes on: the heads of the workers after it that begin with the same id
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] = tail[j * kSortThreads + t];
+    for (int w = worker + 1; w * stretch < len && sm.pair[w * stretch].x == cur; ++w)
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] += head[j * kSortThreads + w * p.lanes + gl];
+    finish(cur, acc);
+}
+
+// The blocks' tables added up: 32 values per block, its warps take every so-many-th table each.
+template <typename TO>
+__global__ void __launch_bounds__(1024) table_join_kernel(const __grid_constant__ TileArgs p) {
+    hagk::pdl_launch_dependents();
+    __shared__ float sum[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int64_t values = int64_t(p.sort.n_rows) * p.D, i = int64_t(blockIdx.x) * 32 + lane;
+    hagk::pdl_wait();
+    float v = 0.0f;
+    if (i < values) {
+#pragma unroll 8
+        for (int q = warp; q < p.parts; q += warps) v += __ldcg(p.partial + q * values + i);
+    }
+    sum[warp][lane] = v;
+    __syncthreads();
+    if (warp == 0 && i < values) {
+        for (int w = 1; w < warps; ++w) v += sum[w][lane];
+        const uint32_t row = hagr::quotient(uint32_t(i), p.per_row);
+        store_scalar<TO>(p, int32_t(row), int32_t(i - int64_t(row) * p.D), v);
+    }
+}
+
+constexpr int64_t kTileValues = 1 << 20;         // of a table
+constexpr int64_t kTileAlone = 1 << 16;          // of the result that one block clears by itself
+
+// Tiles for a list, or 0 where the tables would be more than a TILE_SHARE-th of the gradient rows.
+int tile_count(int32_t n, int32_t n_rows, int32_t D) {
+    const int64_t values = int64_t(n_rows) * D;
+    if (n <= kTileOne && values <= kTileAlone) return 1;
+    const int64_t tiles = std::max<int64_t>(148, 148 * ((int64_t(n) + 148 * kSortTile - 1) / (148 * kSortTile)));
+    return values <= kTileValues && tiles * n_rows * TILE_SHARE <= n ? int(tiles) : 0;
+}
+
+template <typename TG, typename TO, int V>
+cudaError_t launch_tiles(TileArgs p, int tiles, cudaStream_t s) {
+    if (!allow_shared<embedding_tile_kernel<TG, TO, V>>(sizeof(SortShared) + 2 * kSortThreads * V * 4)) return cudaErrorInvalidConfiguration;
+    const int n_vec = p.D / V;
+    p.lanes = hagl::lanes_per_row(n_vec);
+    // whole waves: where a row takes several blocks there are so many fewer tiles, of at most kSortTile tokens
+    const int columns = (n_vec + 31) / 32;
+    int64_t use = std::max<int64_t>(tiles / columns, (int64_t(p.sort.n) + kSortTile - 1) / kSortTile);
+    p.sort.stretch = int32_t((int64_t(p.sort.n) + use - 1) / use);
+    p.parts = int32_t((int64_t(p.sort.n) + p.sort.stretch - 1) / p.sort.stretch);
+    if (tiles == 1) p.partial = nullptr;
+    p.per_row = hagr::make_divisor(uint32_t(p.D));
+    cudaError_t err = launch_with(embedding_tile_kernel<TG, TO, V>, dim3(unsigned(p.parts), unsigned(columns)), kSortThreads,
+                                  sizeof(SortShared) + 2 * kSortThreads * V * 4, p, s);
+    if (err == cudaSuccess && p.partial) {
+        const int64_t values = int64_t(p.sort.n_rows) * p.D;
+        int warps = 1;
+        while (warps < 32 && warps < p.parts) warps *= 2;
+        err = launch_with(table_join_kernel<TO>, dim3(unsigned((values + 31) / 32)), unsigned(32 * warps), 0, p, s);
+    }
+    return err;
+}
+
+template <typename TG, typename TO>
+cudaError_t launch_tiles_v(const TileArgs &p, int tiles, cudaStream_t s) {
+    const hagr::Operand ops[] = {{p.grad, p.ld_grad, int(sizeof(TG))}};
+    switch (hagr::vector_elems(16 / int(sizeof(TG)), p.D, ops)) {
+        case 8: if constexpr (sizeof(TG) == 2) return launch_tiles<TG, TO, 8>(p, tiles, s);
+        case 4: return launch_tiles<TG, TO, 4>(p, tiles, s);
+        case 2: return launch_tiles<TG, TO, 2>(p, tiles, s);
+        default: return launch_tiles<TG, TO, 1>(p, tiles, s);
+    }
+}
+
 int key_bits(int32_t n_rows) {          // of the largest key, V
     int b = 1;
     while ((int64_t(1) << b) <= n_rows) ++b;
@@ -711,7 +933,8 @@ extern "C" hag_status hag_embedding_fwd(const void *ids, hag_id_type id_type, in
 
 extern "C" size_t hag_embedding_bwd_workspace_bytes(int64_t n, int64_t n_rows, int32_t D) {
     if (n <= 0 || n > 0x7fffffffLL - kSortTile || n_rows < 0 || D <= 0) return 0;
-    return 2 * list_bytes(n) + up256(size_t(kSortMaxBlocks) * kSortBins * 4) + 2 * up256(size_t(partial_floats(n, D)) * 4);
+    return std::max(2 * list_bytes(n) + up256(size_t(kSortMaxBlocks) * kSortBins * 4) + 2 * up256(size_t(partial_floats(n, D)) * 4),
+                    size_t(tile_count(int32_t(n), int32_t(n_rows), D)) * size_t(n_rows) * size_t(D) * 4);
 }
 
 extern "C" hag_status hag_embedding_bwd(const void *ids, hag_id_type id_type, int64_t n, int64_t n_rows, hag_dtype dtype, int32_t D,
@@ -734,15 +957,27 @@ extern "C" hag_status hag_embedding_bwd(const void *ids, hag_id_type id_type, in
         if (err != cudaSuccess) { cudaGetLastError(); return HAG_ERR_CUDA; }
         return HAG_OK;
     }
+    const SortPlan plan = sort_plan(int32_t(n), int32_t(n_rows));
+    if (const int tiles = tile_count(int32_t(n), int32_t(n_rows), D)) {
+        const SortArgs a{ids, id_type == HAG_ID64, int32_t(n_rows), nullptr, nullptr, nullptr, int32_t(n), 0, 0, plan.bits, plan.passes, 0, fill};
+        const TileArgs p{a, grad_out, ld_grad_out, grad_table, ld_grad_table, D, scale, 0, static_cast<float *>(workspace), 0, {}};
+        if (dtype == HAG_F32)
+            err = table_dtype == HAG_F32 ? launch_tiles_v<float, float>(p, tiles, s) : launch_tiles_v<float, __nv_bfloat16>(p, tiles, s);
+        else
+            err = table_dtype == HAG_F32 ? launch_tiles_v<__nv_bfloat16, float>(p, tiles, s) : launch_tiles_v<__nv_bfloat16, __nv_bfloat16>(p, tiles, s);
+        if (err != cudaSuccess) { cudaGetLastError(); return HAG_ERR_CUDA; }
+        return HAG_OK;
+    }
     const size_t part = list_bytes(n);
     uint2 *list[2] = {reinterpret_cast<uint2 *>(w), reinterpret_cast<uint2 *>(w + part)};
     uint32_t *count = reinterpret_cast<uint32_t *>(w + 2 * part);
     char *partials = w + 2 * part + up256(size_t(kSortMaxBlocks) * kSortBins * 4);
     int side = 0;
-    const SortPlan plan = sort_plan(int32_t(n), int32_t(n_rows));
     const int launches = plan.blocks == 1 ? 1 : 2 * plan.passes;
-    static const bool sort_ready = allow_shared(sort_move_kernel, sizeof(SortShared)) && allow_shared(sort_small_kernel, sizeof(SortShared));
-    if (!sort_ready) return HAG_ERR_CUDA;
+    if (!allow_shared<sort_move_kernel>(sizeof(SortShared)) || !allow_shared<sort_small_kernel>(sizeof(SortShared))) {
+        cudaGetLastError();
+        return HAG_ERR_CUDA;
+    }
     for (int k = 0; k < launches && err == cudaSuccess; ++k) {
         const int pass = k / 2;
         fill.rows_begin = int32_t(n_rows * k / launches);
