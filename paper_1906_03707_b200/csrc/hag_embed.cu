@@ -47,13 +47,6 @@ bool allow_shared(size_t bytes) {
     return true;
 }
 
-#ifndef TILE_SHARE
-#define TILE_SHARE 4
-#endif
-#ifndef TILE_ONE
-#define TILE_ONE 4096
-#endif
-constexpr int kTileOne = TILE_ONE;
 constexpr int kCopyThreads = 256;
 // Vectors per thread: 64 bytes of the wider type in flight, narrow vectors at most 8.
 template <int BYTES> constexpr int kCopyUnroll = BYTES >= 16 ? 4 : 8;
@@ -193,6 +186,7 @@ constexpr int kSortItems = 8;                                 // keys per thread
 constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kSortBins = 256;
 constexpr int kSortMaxBlocks = 148;                           // every block reads the counts of all blocks
+constexpr int kSortUnit = kSortThreads;                       // stretches are multiples of one key per thread
 
 struct SortArgs {
     const void *ids;         // first pass: the caller's ids
@@ -202,7 +196,7 @@ struct SortArgs {
     uint2 *out;
     uint32_t *count;         // [blocks][bins]
     int32_t n;
-    int32_t stretch;         // keys per block, a multiple of the tile
+    int32_t stretch;         // keys per block, a multiple of kSortUnit
     int32_t shift, bits;
     int32_t passes;          // of the single-launch form
     int32_t blocks;          // that sort; the blocks after them clear rows of the gradient
@@ -228,7 +222,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
         fill_rows(p.fill, blockIdx.x - p.blocks);
         return;
     }
-    const int32_t begin = blockIdx.x * p.stretch, end = int32_t(min(int64_t(p.n), int64_t(begin) + p.stretch));
+    const int32_t begin = int32_t(blockIdx.x) * p.stretch, end = int32_t(min(int64_t(p.n), int64_t(begin) + p.stretch));
     uint32_t *mine = bin[(t >> 5) % kCopies];
     for (int32_t tile = begin; tile < end; tile += kSortTile) {
         uint32_t key[kSortItems];
@@ -241,6 +235,9 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
     __syncthreads();
     if (t < kSortBins) p.count[blockIdx.x * kSortBins + t] = bin[0][t] + bin[1][t] + bin[2][t] + bin[3][t];
 }
+
+// Keys per thread for a tile of so many: no thread works on more empty places than it must.
+__device__ __forceinline__ int tile_items(int32_t len) { return min((len + kSortThreads - 1) / kSortThreads, kSortItems); }
 
 // What a block needs to order a tile of pairs by one digit.
 struct SortShared {
@@ -270,9 +267,11 @@ __device__ __forceinline__ uint32_t bin_scan(uint32_t count, uint32_t *scan) {
     return lower + x - count;
 }
 
-// Orders a tile by the digit at `shift`: the pairs (in registers, a warp's are consecutive in the list) end in
-// sm.pair.  Returns, for threads below kSortBins, how many keys have digit t; sm.shift_by[t] is set from `base`.
-__device__ __forceinline__ uint32_t sort_tile(SortShared &sm, const uint2 (&pair)[kSortItems], int shift, uint32_t mask, uint32_t base) {
+// Orders a tile by the digit at `shift`: the pairs (in registers, `items` per thread, a warp's are consecutive in the
+// list) end in sm.pair.  Returns, for threads below kSortBins, how many keys have digit t; sm.shift_by[t] is set from
+// `base`.
+__device__ __forceinline__ uint32_t sort_tile(SortShared &sm, const uint2 (&pair)[kSortItems], int items, int shift, uint32_t mask,
+                                              uint32_t base) {
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     for (int i = t; i < kSortWarps * kSortBins / 4; i += kSortThreads) reinterpret_cast<uint4 *>(&sm.seen[0][0])[i] = make_uint4(0, 0, 0, 0);
     uint32_t same[kSortItems], rank[kSortItems];
@@ -285,6 +284,7 @@ __device__ __forceinline__ uint32_t sort_tile(SortShared &sm, const uint2 (&pair
         if ((mask >> bit) == 0) break;
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k) {
+            if (k >= items) break;
             const bool set = (pair[k].x >> (shift + bit)) & 1u;
             const uint32_t votes = __ballot_sync(0xffffffffu, set);
             same[k] &= set ? votes : ~votes;
@@ -293,6 +293,7 @@ __device__ __forceinline__ uint32_t sort_tile(SortShared &sm, const uint2 (&pair
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kSortItems; ++k) {
+        if (k >= items) break;
         uint32_t *count = &sm.seen[warp][(pair[k].x >> shift) & mask];
         rank[k] = *count + __popc(same[k] & ((1u << lane) - 1u));
         __syncwarp();
@@ -316,7 +317,8 @@ __device__ __forceinline__ uint32_t sort_tile(SortShared &sm, const uint2 (&pair
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kSortItems; ++k) sm.pair[sm.seen[warp][(pair[k].x >> shift) & mask] + rank[k]] = pair[k];
+    for (int k = 0; k < kSortItems; ++k)
+        if (k < items) sm.pair[sm.seen[warp][(pair[k].x >> shift) & mask] + rank[k]] = pair[k];
     __syncthreads();
     return all;
 }
@@ -332,14 +334,17 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
         fill_rows(p.fill, blockIdx.x - p.blocks);
         return;
     }
-    const int32_t begin = blockIdx.x * p.stretch, end = int32_t(min(int64_t(p.n), int64_t(begin) + p.stretch));
+    const int32_t begin = int32_t(blockIdx.x) * p.stretch, end = int32_t(min(int64_t(p.n), int64_t(begin) + p.stretch));
     uint2 pair[kSortItems];
     // a warp's keys are consecutive: stable.  Places beyond the end hold the largest key and come after all others of
     // the tile, which is the list's last.
+    int items = 0;
     auto load = [&](int32_t tile) {
-        const int32_t mine = tile + warp * (32 * kSortItems) + lane;
+        items = tile_items(end - tile);
+        const int32_t mine = tile + warp * (32 * items) + lane;
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) pair[k] = mine + 32 * k < end ? sort_pair(p, mine + 32 * k) : make_uint2(0xffffffffu, 0);
+        for (int k = 0; k < kSortItems; ++k)
+            if (k < items) pair[k] = mine + 32 * k < end ? sort_pair(p, mine + 32 * k) : make_uint2(0xffffffffu, 0);
     };
     load(begin);
     uint32_t base = 0;       // for t < kSortBins: keys with a smaller digit + keys of digit t in the blocks before this one
@@ -371,7 +376,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
     for (int32_t tile = begin; tile < end; tile += kSortTile) {
         if (tile != begin) load(tile);
         __syncthreads();
-        base += sort_tile(sm, pair, p.shift, mask, base);
+        base += sort_tile(sm, pair, items, p.shift, mask, base);
         const int32_t len = min(end - tile, kSortTile);
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k) {
@@ -395,19 +400,21 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const SortArgs
         fill_rows(p.fill, blockIdx.x - 1);
         return;
     }
-    const int mine = (t >> 5) * (32 * kSortItems) + (t & 31);
+    const int items = tile_items(p.n), mine = (t >> 5) * (32 * items) + (t & 31);
     uint2 pair[kSortItems];
 #pragma unroll
-    for (int k = 0; k < kSortItems; ++k) pair[k] = mine + 32 * k < p.n ? sort_pair(p, mine + 32 * k) : make_uint2(0xffffffffu, 0);
+    for (int k = 0; k < kSortItems; ++k)
+        if (k < items) pair[k] = mine + 32 * k < p.n ? sort_pair(p, mine + 32 * k) : make_uint2(0xffffffffu, 0);
     for (int pass = 0; pass < p.passes; ++pass) {
-        sort_tile(sm, pair, pass * p.bits, mask, 0);
+        sort_tile(sm, pair, items, pass * p.bits, mask, 0);
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) pair[k] = sm.pair[mine + 32 * k];
+        for (int k = 0; k < kSortItems; ++k)
+            if (k < items) pair[k] = sm.pair[mine + 32 * k];
         __syncthreads();
     }
 #pragma unroll
     for (int k = 0; k < kSortItems; ++k)
-        if (mine + 32 * k < p.n) p.out[mine + 32 * k] = pair[k];
+        if (k < items && mine + 32 * k < p.n) p.out[mine + 32 * k] = pair[k];
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -691,10 +698,11 @@ __global__ void __launch_bounds__(kSortThreads) embedding_tile_kernel(const __gr
     const uint32_t mask = (1u << p.sort.bits) - 1u;
     hagk::pdl_wait();
     {
-        const int mine = (t >> 5) * (32 * kSortItems) + (t & 31);
+        const int items = tile_items(len), mine = (t >> 5) * (32 * items) + (t & 31);
         uint2 pair[kSortItems];
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) pair[k] = mine + 32 * k < len ? sort_pair(p.sort, begin + mine + 32 * k) : make_uint2(0xffffffffu, 0);
+        for (int k = 0; k < kSortItems; ++k)
+            if (k < items) pair[k] = mine + 32 * k < len ? sort_pair(p.sort, begin + mine + 32 * k) : make_uint2(0xffffffffu, 0);
         // rows that no token of the tile names: cleared while the ids are on their way
         const int c0 = blockIdx.y * p.lanes * V, width = min(p.D - c0, p.lanes * V);
         for (int r = t / p.lanes; r < rows; r += kSortThreads / p.lanes)
@@ -705,10 +713,11 @@ __global__ void __launch_bounds__(kSortThreads) embedding_tile_kernel(const __gr
         for (int pass = 0; pass < p.sort.passes; ++pass) {
             if (pass) {
 #pragma unroll
-                for (int k = 0; k < kSortItems; ++k) pair[k] = sm.pair[mine + 32 * k];
+                for (int k = 0; k < kSortItems; ++k)
+                    if (k < items) pair[k] = sm.pair[mine + 32 * k];
                 __syncthreads();
             }
-            sort_tile(sm, pair, pass * p.sort.bits, mask, 0);             // ends with a barrier: the rows are clear too
+            sort_tile(sm, pair, items, pass * p.sort.bits, mask, 0);             // ends with a barrier: the rows are clear too
         }
     }
     const int worker = t / p.lanes, gl = t % p.lanes, workers = kSortThreads / p.lanes, vec = blockIdx.y * p.lanes + gl;
@@ -818,13 +827,22 @@ __global__ void __launch_bounds__(1024) table_join_kernel(const __grid_constant_
 
 constexpr int64_t kTileValues = 1 << 20;         // of a table
 constexpr int64_t kTileAlone = 1 << 16;          // of the result that one block clears by itself
+// Tokens per tile of a short list.  256: 1000 x 16 into 100 rows takes 8.0 us, 4000 x 64 into 119 rows 8.9 us; with 1024
+// they take 8.8 and 11.4 us.
+constexpr int kTileLeast = 256, kTileMost = 2048;
+constexpr int kTileBlocks = 148;
 
-// Tiles for a list, or 0 where the tables would be more than a TILE_SHARE-th of the gradient rows.
+// Tiles for a list, or 0 where the tables would be too large: all of them together up to 4 MB (they stay in the L2), or
+// a quarter of the gradient rows' values.
 int tile_count(int32_t n, int32_t n_rows, int32_t D) {
     const int64_t values = int64_t(n_rows) * D;
-    if (n <= kTileOne && values <= kTileAlone) return 1;
-    const int64_t tiles = std::max<int64_t>(148, 148 * ((int64_t(n) + 148 * kSortTile - 1) / (148 * kSortTile)));
-    return values <= kTileValues && tiles * n_rows * TILE_SHARE <= n ? int(tiles) : 0;
+    if (n <= kTileLeast && values <= kTileAlone) return 1;
+    if (values > kTileValues) return 0;
+    const int64_t most = std::max<int64_t>(1 << 20, int64_t(n) * D / 4);
+    const int64_t waves = (int64_t(n) + kTileBlocks * int64_t(kSortTile) - 1) / (kTileBlocks * int64_t(kSortTile));
+    int64_t tiles = waves > 1 ? waves * kTileBlocks : std::min<int64_t>(kTileBlocks, (int64_t(n) + kTileLeast - 1) / kTileLeast);
+    while (tiles * values > most && tiles > 1 && (int64_t(n) + tiles / 2 - 1) / (tiles / 2) <= kTileMost) tiles /= 2;
+    return tiles * values <= most ? int(tiles) : 0;
 }
 
 template <typename TG, typename TO, int V>
@@ -832,9 +850,9 @@ cudaError_t launch_tiles(TileArgs p, int tiles, cudaStream_t s) {
     if (!allow_shared<embedding_tile_kernel<TG, TO, V>>(sizeof(SortShared) + 2 * kSortThreads * V * 4)) return cudaErrorInvalidConfiguration;
     const int n_vec = p.D / V;
     p.lanes = hagl::lanes_per_row(n_vec);
-    // whole waves: where a row takes several blocks there are so many fewer tiles, of at most kSortTile tokens
+    // where a row takes several blocks there are fewer tiles, of at most kSortTile tokens
     const int columns = (n_vec + 31) / 32;
-    int64_t use = std::max<int64_t>(tiles / columns, (int64_t(p.sort.n) + kSortTile - 1) / kSortTile);
+    const int64_t use = std::max<int64_t>(std::min(tiles, std::max(kTileBlocks / columns, 1)), (int64_t(p.sort.n) + kSortTile - 1) / kSortTile);
     p.sort.stretch = int32_t((int64_t(p.sort.n) + use - 1) / use);
     p.parts = int32_t((int64_t(p.sort.n) + p.sort.stretch - 1) / p.sort.stretch);
     if (tiles == 1) p.partial = nullptr;
@@ -873,10 +891,9 @@ struct SortPlan {
 };
 SortPlan sort_plan(int32_t n, int32_t n_rows) {
     SortPlan s;
-    const int64_t tiles = (int64_t(n) + kSortTile - 1) / kSortTile;
-    const int64_t per_block = (tiles + kSortMaxBlocks - 1) / kSortMaxBlocks;
-    s.blocks = int((tiles + per_block - 1) / std::max<int64_t>(per_block, 1));
-    s.stretch = int32_t(std::min<int64_t>(per_block * kSortTile, 0x7fffffff));
+    const int64_t least = n <= kSortTile ? kSortTile : (int64_t(n) + kSortMaxBlocks - 1) / kSortMaxBlocks;
+    s.stretch = int32_t((least + kSortUnit - 1) / kSortUnit * kSortUnit);
+    s.blocks = int((int64_t(n) + s.stretch - 1) / s.stretch);
     const int total = key_bits(n_rows);
     s.passes = (total + 7) / 8;
     s.bits = (total + s.passes - 1) / s.passes;
