@@ -31,6 +31,8 @@ struct NormArgs {
     float *partial;             // backward: [parts][2][D]
     void *gw, *gb;
     int32_t parts;
+    int32_t stages;             // of the ring
+    int32_t w_vectors;          // whether w and b can be read a vector at a time
 };
 
 constexpr int kRowThreads = 256;
@@ -155,28 +157,34 @@ __global__ void __launch_bounds__(32 * kStripRows) norm_params_any_kernel(const 
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Rows held in registers.  A group of lanes owns a row, K vectors of V elements per lane, so a row is read once; the
-// weights stay in registers over all rows of the group.
-//   warp kernels : L = 8, 16 or 32 lanes of a warp per row, R rows per group at a time (loads in flight)
-//   block kernels: a whole block per row, sums over the block through shared memory
-constexpr int kPerLane = 16;              // elements of a row per lane, at most
-constexpr int kWarpThreads = 256;
-constexpr int kWarpRows = kWarpThreads / 32;
+// Rows read once.  A group of threads owns a row, K vectors of V elements per thread, and reads ahead of the rows it
+// works on.
+//   L = 8, 16, 32: that many lanes of a warp per row, R rows per group at a time
+//   L = 0 or -1  : a whole block per row (of up to kMostThreads or kFewThreads threads), sums over the block through
+//                  shared memory
+// With 16-byte vectors the rows ahead are on their way into a ring of slots in shared memory (asynchronous copies, each
+// thread its own), so what is in flight does not depend on registers.  Narrower vectors (unaligned rows) are read one
+// turn ahead into registers: with 4-byte asynchronous copies 100 000 x 1433 fp32 forward takes 350 us, so 209.
+// The weights stay with the thread over all its rows: in registers, or from 16 columns per thread on in shared memory
+// (ring) or registers.
+constexpr int kMostThreads = 1024;        // of a block per row; up to kFewThreads the compiler may use 128 registers
+constexpr int kFewThreads = 512;
+// Stages of the ring.  What is in flight per SM matters more than how many warps are there: about 64 KB (one block of
+// eight warps, 64 bytes per lane and turn) is best; with three blocks 10^6 x 256 bf16 forward takes 196 us, with one 160.
+constexpr int kFwdStages = 3, kBwdStages = 4, kBlockStages = 2;
 
-template <int V, int K>
-__device__ __forceinline__ void load_params(const void *p, int bf16, int32_t D, int first, int step, float fill, float *v) {
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int32_t c = (first + k * step) * V + j;
-            v[k * V + j] = p && c < D ? load_param(p, bf16, c) : fill;
-        }
-}
+template <typename T, int V> constexpr bool kRing = V * int(sizeof(T)) == 16;
+constexpr int kWarpThreads = 256;
+template <int L> constexpr int kThreads = L == 0 ? kMostThreads : L < 0 ? kFewThreads : kWarpThreads;
+template <typename T, int L, int V, int K, bool BWD> constexpr int kLeastBlocks = L < 0 && !BWD && kRing<T, V> ? 2 : 1;    // per SM
+// Rows per turn: 64 bytes per lane and turn (both operands of the backward pass together), but at least one row.
+constexpr int rows_per_turn(int bytes, int most) { return bytes >= 64 ? 1 : 64 / bytes < most ? 64 / bytes : most; }
+template <typename T, int L, int V, int K> constexpr int kFwdRows = L <= 0 ? 1 : kRing<T, V> ? rows_per_turn(K * V * int(sizeof(T)), 4) : V * K >= 16 ? 1 : 16 / (V * K) < 4 ? 16 / (V * K) : 4;
+template <typename T, int L, int V, int K> constexpr int kBwdRows = L > 0 && V * K <= 8 ? V * K <= 4 && kRing<T, V> ? 2 : 2 : 1;
 
 // Sums of R values per lane over the L lanes of a group: lanes trade halves of the list while it has more than one
-// value, so the R sums take about L + R shuffles' worth less than R butterflies, and each lane ends with ONE of the
-// sums: number (gl * R / L).  What follows a sum (a division, a root) is then done once, not once per value.
+// value (4 sums over 32 lanes take 6 shuffles, not 20), and each lane ends with ONE of the sums: number (gl * R / L).
+// What follows a sum (a division, a root) is then done once, not once per value.
 template <int L, int R>
 __device__ __forceinline__ float spread_sums(const float (&in)[R], int gl) {
     float v[R];
@@ -255,273 +263,449 @@ struct Pairs {
     }
 };
 
-// A lane's share of a row: K vectors of V elements, `step` vectors apart.
-template <typename T, int V, int K>
-struct RowPart {
-    hagr::Vec<T, V> raw[K];
-    __device__ __forceinline__ void load(const void *base, int64_t ld, int64_t r, bool live, int first, int step, int32_t n_vec) {
+template <typename T, int V>
+__device__ __forceinline__ Pairs<V> widen(const hagr::Vec<T, V> &a) {
+    Pairs<V> f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) f.v[j] = a.get(j);
+    return f;
+}
+
+// The rows that a thread has ahead: slots in shared memory (stages x OPS matrices x R rows x K vectors; those of the
+// threads lie side by side), or one turn in registers.  THREADS is the block's size where it is fixed, else 0.
+template <typename T, int V, int K, int R, int OPS, int THREADS>
+struct Ahead {
+    static constexpr bool RING = kRing<T, V>;
+    static constexpr int kSlot = V * int(sizeof(T)), kStage = RING ? OPS * R * K * kSlot : 0;         // bytes per thread
+    hagr::Vec<T, V> next[RING ? 1 : OPS * R * K];
+    char *mine;
+    int write = 0, read = 0, end;                              // offsets of the stages in turn
+
+    static __device__ __forceinline__ int threads() { return THREADS ? THREADS : int(blockDim.x); }
+    __device__ __forceinline__ Ahead(char *base, int stages) : mine(base + threadIdx.x * kSlot), end(stages * kStage * threads()) {}
+    __device__ __forceinline__ char *slot(int stage, int op, int i, int k) const { return mine + stage + ((op * R + i) * K + k) * (threads() * kSlot); }
+    // row i of the turn being issued starts at `row`; a row that does not exist is read as zeros
+    __device__ __forceinline__ void issue(int op, int i, const char *row, bool live, int first, int step, int32_t n_vec) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            raw[k].zero();
-            if (live && first + k * step < n_vec) raw[k].template load<hagr::kOnce>(static_cast<const T *>(base) + r * ld, first + k * step);
+            const bool column = first + k * step < n_vec;
+            if constexpr (RING) {
+                char *to = slot(write, op, i, k);
+                if (live && column) hagr::copy_async<kSlot>(to, row + int64_t(first + k * step) * kSlot);
+                else *reinterpret_cast<hagr::Words<kSlot> *>(to) = hagr::Words<kSlot>{};
+            } else {
+                hagr::Vec<T, V> &to = next[(op * R + i) * K + k];
+                to.zero();
+                if (live && column) to.template load<hagr::kOnce>(row, first + k * step);
+            }
         }
     }
-    __device__ __forceinline__ Pairs<K * V> wide() const {
-        Pairs<K * V> f;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int j = 0; j < V; ++j) f.v[k * V + j] = raw[k].get(j);
-        return f;
+    __device__ __forceinline__ void issued() {                 // the turn is complete
+        if constexpr (RING) {
+            hagr::commit_copies();
+            write = write + kStage * threads() == end ? 0 : write + kStage * threads();
+        }
     }
-    static __device__ __forceinline__ void store(void *base, int64_t ld, int64_t r, bool live, int first, int step, int32_t n_vec,
-                                                 const Pairs<K * V> &f) {
+    __device__ __forceinline__ hagr::Vec<T, V> get(int op, int i, int k) const {
+        if constexpr (RING) {
+            hagr::Vec<T, V> v;
+            v.raw = *reinterpret_cast<const hagr::Words<kSlot> *>(slot(read, op, i, k));
+            return v;
+        } else {
+            return next[(op * R + i) * K + k];
+        }
+    }
+    __device__ __forceinline__ void done() {                   // with the oldest turn's slots
+        if constexpr (RING) read = read + kStage * threads() == end ? 0 : read + kStage * threads();
+    }
+    // until the oldest of the stages has arrived (a launch has fewer stages where a row fills the shared memory)
+    static __device__ __forceinline__ void wait(int stages) {
+        if constexpr (RING) {
+            if (stages == 4) hagr::wait_copies<3>();
+            else if (stages == 3) hagr::wait_copies<2>();
+            else if (stages == 2) hagr::wait_copies<1>();
+            else hagr::wait_copies<0>();
+        }
+    }
+};
+
+// The rows of a group of threads: R at a time, `stride` rows from one turn to the next.
+template <int L, int R>
+struct Turns {
+    static constexpr int G = L <= 0 ? 1 : 32 / (L <= 0 ? 32 : L);        // groups per warp
+    int first, step, side;               // this thread's place in its group, the group's threads, the group's place in its warp
+    int64_t row, stride;
+    int32_t all, live[R];                // turns of the warp (or block); turns in which row i exists
+
+    __device__ __forceinline__ explicit Turns(int64_t n) {
+        const int lane = threadIdx.x & 31;
+        first = L <= 0 ? int(threadIdx.x) : lane % (L <= 0 ? 32 : L);
+        step = L <= 0 ? int(blockDim.x) : L;
+        side = L <= 0 ? 0 : lane / (L <= 0 ? 32 : L);
+        const int64_t group = L <= 0 ? int64_t(blockIdx.x) : (int64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5)) * G + side;
+        row = group * R;
+        stride = L <= 0 ? int64_t(gridDim.x) * R : int64_t(gridDim.x) * (blockDim.x >> 5) * G * R;
+        all = count(n, (group - side) * R);
+#pragma unroll
+        for (int i = 0; i < R; ++i) live[i] = count(n, row + i);
+    }
+    __device__ __forceinline__ int32_t count(int64_t n, int64_t from) const { return from < n ? int32_t((n - from + stride - 1) / stride) : 0; }
+};
+
+// Parameters of a thread's columns, N vectors of them (weights, or weights and biases), in registers or in shared
+// memory in planes of up to four columns (so that neighbours read neighbouring words).
+template <int V, int K, int N, bool RING>
+struct Params {
+    static constexpr bool kShared = RING && V * K >= 16;
+    static constexpr int W = V < 4 ? V : 4;
+    struct alignas(4 * W) Piece { float v[W]; };
+    float own[kShared ? 1 : N * K * V];
+    Piece *shared;
+    int first, step;
+
+    static __host__ __device__ constexpr size_t bytes(int step) { return kShared ? size_t(N) * K * V * step * 4 : 0; }
+    __device__ __forceinline__ Params(char *base, int first_, int step_) : shared(reinterpret_cast<Piece *>(base)), first(first_), step(step_) {}
+    __device__ __forceinline__ Piece *piece(int n, int k, int h) const { return shared + ((n * (V / W) + h) * K + k) * step + first; }
+    // `writes`: whether this thread fills the shared copy of its columns
+    __device__ __forceinline__ void load(int n, const void *p, int bf16, bool vectors, int32_t D, float fill, bool writes) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (!live || first + k * step >= n_vec) continue;
-            hagr::Vec<T, V> o;
-            o.set(&f.v[k * V]);
-            o.store(static_cast<T *>(base) + r * ld, first + k * step);
+            float v[V];
+            const int32_t vec = first + k * step;
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = fill;
+            if (p && vec < D / V) {
+                if (vectors && bf16) {
+                    hagr::Vec<__nv_bfloat16, V> q;
+                    q.template load<hagr::kKeep>(p, vec);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) v[j] = q.get(j);
+                } else if (vectors) {
+                    hagr::Vec<float, V> q;
+                    q.template load<hagr::kKeep>(p, vec);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) v[j] = q.get(j);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) v[j] = load_param(p, bf16, int64_t(vec) * V + j);
+                }
+            }
+            if constexpr (kShared) {
+                if (writes)
+#pragma unroll
+                    for (int h = 0; h < V / W; ++h) {
+                        Piece q;
+#pragma unroll
+                        for (int j = 0; j < W; ++j) q.v[j] = v[h * W + j];
+                        *piece(n, k, h) = q;
+                    }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) own[(n * K + k) * V + j] = v[j];
+            }
         }
     }
-    // differences from the mean; lanes beyond the row hold zeros
-    __device__ __forceinline__ Pairs<K * V> centred(float mean, int first, int step, int32_t n_vec) const {
-        Pairs<K * V> f = wide();
-        f.shift(-mean);
+    __device__ __forceinline__ Pairs<V> get(int n, int k) const {
+        Pairs<V> f;
+        if constexpr (kShared) {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (first + k * step >= n_vec)
+            for (int h = 0; h < V / W; ++h) {
+                const Piece q = *piece(n, k, h);
 #pragma unroll
-                for (int j = 0; j < V; ++j) f.v[k * V + j] = 0.0f;
+                for (int j = 0; j < W; ++j) f.v[h * W + j] = q.v[j];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) f.v[j] = own[(n * K + k) * V + j];
+        }
         return f;
     }
 };
 
-template <typename T, int V, int L, int K, int R>
-__global__ void __launch_bounds__(kWarpThreads) norm_fwd_warp_kernel(const NormArgs p) {
-    hagk::pdl_launch_dependents();
-    constexpr int G = 32 / L;                                  // rows side by side in a warp
-    const int lane = threadIdx.x & 31, gl = lane % L;
-    const int32_t n_vec = p.D / V;
-    const float cols = float(p.D);
-    const int64_t group = (int64_t(blockIdx.x) * kWarpRows + (threadIdx.x >> 5)) * G + lane / L;
-    const int64_t groups = int64_t(gridDim.x) * kWarpRows * G;
-    Pairs<K * V> w, b;
-    hagk::pdl_wait();
-    load_params<V, K>(p.w, p.w_bf16, p.D, gl, L, 1.0f, w.v);
-    load_params<V, K>(p.b, p.w_bf16, p.D, gl, L, 0.0f, b.v);
-    RowPart<T, V, K> x[R], next[R];
-    auto load = [&](RowPart<T, V, K> (&to)[R], int64_t r0) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) to[i].load(p.x, p.ld_x, r0 + i, r0 + i < p.n, gl, L, n_vec);
-    };
-    // a warp's groups leave together: the row of its first group decides
-    int64_t r0 = group * R;
-    load(x, r0);
-    for (; r0 - (lane / L) * R < p.n; r0 += groups * R) {
-        load(next, r0 + groups * R);                           // in flight while these rows are worked on
-        float s[R], mean[R];
-#pragma unroll
-        for (int i = 0; i < R; ++i) s[i] = x[i].wide().sum();
-        const float my_mean = spread_sums<L, R>(s, gl) / cols;
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            mean[i] = spread_get<L, R>(my_mean, i, lane);
-            const Pairs<K * V> d = x[i].centred(mean[i], gl, L, n_vec);
-            s[i] = d.dot(d);
-        }
-        const float my_rstd = rsqrtf(spread_sums<L, R>(s, gl) / cols + p.eps);
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const float rstd = spread_get<L, R>(my_rstd, i, lane);
-            Pairs<K * V> v = x[i].wide(), y = b;
-            v.shift_scale(-mean[i], rstd);
-            y.fma(v, w);
-            RowPart<T, V, K>::store(p.y, p.ld_y, r0 + i, r0 + i < p.n, gl, L, n_vec, y);
-        }
-        const int64_t r = r0 + gl * R / L;                     // the row whose statistics this lane holds
-        if (gl % (L / R) == 0 && r < p.n) {
-            if (p.mean) p.mean[r] = my_mean;
-            if (p.rstd) p.rstd[r] = my_rstd;
-        }
-#pragma unroll
-        for (int i = 0; i < R; ++i) x[i] = next[i];
+// Sums over the group, spread over its lanes (L > 0) or in every thread (L = 0: up to two values; `slot` alternates
+// between calls, so one barrier is enough).
+template <int L, int R>
+__device__ __forceinline__ float group_sums(const float (&s)[R], int gl, float2 *slot) {
+    if constexpr (L > 0) {
+        return spread_sums<L, R>(s, gl);
+    } else {
+        static_assert(R == 1, "");
+        const float a = hagr::warp_sum(s[0]);
+        if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5].x = a;
+        __syncthreads();
+        return hagr::warp_sum((threadIdx.x & 31) < (blockDim.x >> 5) ? slot[threadIdx.x & 31].x : 0.0f);
     }
 }
-
-// Sum of two values over the block; `slot` alternates between calls, so one barrier is enough.
 __device__ __forceinline__ float2 block_sum2(float a, float b, float2 *slot) {
     a = hagr::warp_sum(a);
     b = hagr::warp_sum(b);
     if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = make_float2(a, b);
     __syncthreads();
-    float2 s = make_float2(0.0f, 0.0f);
-    for (int w = 0; w < int(blockDim.x >> 5); ++w) {
-        s.x += slot[w].x;
-        s.y += slot[w].y;
-    }
-    return s;
+    const float2 q = (threadIdx.x & 31) < (blockDim.x >> 5) ? slot[threadIdx.x & 31] : make_float2(0.0f, 0.0f);
+    return make_float2(hagr::warp_sum(q.x), hagr::warp_sum(q.y));
 }
 
-template <typename T, int V, int MAX_THREADS>
-__global__ void __launch_bounds__(MAX_THREADS) norm_fwd_block_kernel(const NormArgs p) {
+template <typename T, int V, int L, int K>
+__global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, false>)) norm_fwd_kernel(const NormArgs p) {
     hagk::pdl_launch_dependents();
-    constexpr int K = kPerLane / V;
-    __shared__ float2 slot[2][32];
-    const int32_t n_vec = p.D / V, step = blockDim.x;
-    const float cols = float(p.D);
-    const int first = threadIdx.x;
-    Pairs<K * V> w, b;
-    hagk::pdl_wait();
-    load_params<V, K>(p.w, p.w_bf16, p.D, first, step, 1.0f, w.v);
-    load_params<V, K>(p.b, p.w_bf16, p.D, first, step, 0.0f, b.v);
-    RowPart<T, V, K> x, next;
-    x.load(p.x, p.ld_x, blockIdx.x, blockIdx.x < p.n, first, step, n_vec);
-    for (int64_t r = blockIdx.x; r < p.n; r += gridDim.x) {
-        next.load(p.x, p.ld_x, r + gridDim.x, r + gridDim.x < p.n, first, step, n_vec);
-        const float mean = block_sum2(x.wide().sum(), 0.0f, slot[0]).x / cols;
-        const Pairs<K * V> d = x.centred(mean, first, step, n_vec);
-        const float rstd = rsqrtf(block_sum2(d.dot(d), 0.0f, slot[1]).x / cols + p.eps);
-        Pairs<K * V> v = x.wide(), y = b;
-        v.shift_scale(-mean, rstd);
-        y.fma(v, w);
-        RowPart<T, V, K>::store(p.y, p.ld_y, r, true, first, step, n_vec, y);
-        if (first == 0) {
-            if (p.mean) p.mean[r] = mean;
-            if (p.rstd) p.rstd[r] = rstd;
-        }
-        x = next;
-    }
-}
-
-// One row of the backward pass: its sums, what it adds to the parameters' gradients, and its gradient.
-template <typename T, int V, int K>
-struct BwdRow {
-    RowPart<T, V, K> x, g;
-    float mean, rstd;
-
-    __device__ __forceinline__ void load(const NormArgs &p, int64_t r, int first, int step, int32_t n_vec) {
-        const bool live = r < p.n;
-        mean = live ? __ldcg(p.mean_in + r) : 0.0f;
-        rstd = live ? __ldcg(p.rstd_in + r) : 0.0f;
-        x.load(p.x, p.ld_x, r, live, first, step, n_vec);
-        g.load(p.g, p.ld_g, r, live, first, step, n_vec);
-    }
-    // sum q and sum q * xh over this lane; where the lane is beyond the row g is zero and its terms vanish
-    __device__ __forceinline__ void sums(const Pairs<K * V> &w, Pairs<K * V> &aw, Pairs<K * V> &ab, float &s1, float &s2) const {
-        Pairs<K * V> xh = x.wide(), q = g.wide();
-        xh.shift_scale(-mean, rstd);
-        ab.add(q);
-        aw.fma(q, xh);
-        q.mul(w);
-        s1 = q.sum();
-        s2 = q.dot(xh);
-    }
-    __device__ __forceinline__ void store(const NormArgs &p, int64_t r, int first, int step, int32_t n_vec, const Pairs<K * V> &w,
-                                          float s1, float s2) const {
-        Pairs<K * V> xh = x.wide(), q = g.wide();
-        xh.shift_scale(-mean, rstd);
-        xh.affine(-s2, -s1);
-        xh.fma(q, w);
-        xh.mul_all(rstd);
-        RowPart<T, V, K>::store(p.y, p.ld_y, r, r < p.n, first, step, n_vec, xh);
-    }
-};
-
-template <typename T, int V, int L, int K, int R>
-__global__ void __launch_bounds__(kWarpThreads) norm_bwd_warp_kernel(const NormArgs p) {
-    hagk::pdl_launch_dependents();
-    constexpr int G = 32 / L;
-    extern __shared__ float joined[];                          // [warps][2][L * K * V], only if gw or gb is wanted
-    const int lane = threadIdx.x & 31, gl = lane % L, warp = threadIdx.x >> 5;
+    extern __shared__ __align__(16) char raw[];
+    __shared__ float2 slots[2][32];
+    constexpr int R = kFwdRows<T, L, V, K>;
+    const Turns<L, R> turns(p.n);
+    const int lane = threadIdx.x & 31, first = turns.first, step = turns.step;
     const int32_t n_vec = p.D / V;
-    const float cols = float(p.D);
-    const int64_t group = (int64_t(blockIdx.x) * kWarpRows + warp) * G + lane / L;
-    const int64_t groups = int64_t(gridDim.x) * kWarpRows * G;
-    Pairs<K * V> w, aw, ab;
-    aw.fill(0.0f);
-    ab.fill(0.0f);
+    const float cols = float(p.D), inverse = 1.0f / cols;
+    Params<V, K, 2, kRing<T, V>> wb(raw, first, step);
+    Ahead<T, V, K, R, 1, (L > 0 ? kThreads<L> : 0)> ahead(raw + Params<V, K, 2, kRing<T, V>>::bytes(step), p.stages);
+    const int64_t ld_x = p.ld_x * int64_t(sizeof(T)), ld_y = p.ld_y * int64_t(sizeof(T));
+    const char *x_next = static_cast<const char *>(p.x) + turns.row * ld_x;
+    char *y = static_cast<char *>(p.y) + turns.row * ld_y;
+    const int64_t step_x = turns.stride * ld_x, step_y = turns.stride * ld_y;
+    auto issue = [&](int32_t turn) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) ahead.issue(0, i, x_next + i * ld_x, turn < turns.live[i], first, step, n_vec);
+        ahead.issued();
+        x_next += step_x;
+    };
     hagk::pdl_wait();
-    load_params<V, K>(p.w, p.w_bf16, p.D, gl, L, 1.0f, w.v);
-    BwdRow<T, V, K> row[R], next[R];
-    int64_t r0 = group * R;
+    for (int32_t s = 0; s < p.stages; ++s) issue(s);
+    wb.load(0, p.w, p.w_bf16, p.w_vectors, p.D, 1.0f, L <= 0 || threadIdx.x < L);
+    wb.load(1, p.b, p.w_bf16, p.w_vectors, p.D, 0.0f, L <= 0 || threadIdx.x < L);
+    if (L > 0 && wb.kShared) __syncthreads();
+    int64_t r = turns.row + (L <= 0 ? 0 : first * R / (L <= 0 ? 1 : L));        // the row whose statistics this thread holds
+    for (int32_t turn = 0; turn < turns.all; ++turn) {
+        ahead.wait(p.stages);
+        Pairs<V> x[R][K];
+        float s[R];
 #pragma unroll
-    for (int i = 0; i < R; ++i) row[i].load(p, r0 + i, gl, L, n_vec);
-    for (; r0 - (lane / L) * R < p.n; r0 += groups * R) {
-        float s[2 * R];
+        for (int i = 0; i < R; ++i) {
+            s[i] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < R; ++i) next[i].load(p, r0 + groups * R + i, gl, L, n_vec);
-#pragma unroll
-        for (int i = 0; i < R; ++i) row[i].sums(w, aw, ab, s[2 * i], s[2 * i + 1]);
-        const float mine = spread_sums<L, 2 * R>(s, gl) / cols;
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-            row[i].store(p, r0 + i, gl, L, n_vec, w, spread_get<L, 2 * R>(mine, 2 * i, lane), spread_get<L, 2 * R>(mine, 2 * i + 1, lane));
-#pragma unroll
-        for (int i = 0; i < R; ++i) row[i] = next[i];
-    }
-    if (!p.partial) return;
-    // groups of the warp, then warps of the block, in a fixed order
-#pragma unroll
-    for (int o = L; o < 32; o <<= 1)
-#pragma unroll
-        for (int i = 0; i < K * V; ++i) {
-            aw.v[i] += __shfl_xor_sync(0xffffffffu, aw.v[i], o);
-            ab.v[i] += __shfl_xor_sync(0xffffffffu, ab.v[i], o);
+            for (int k = 0; k < K; ++k) {
+                x[i][k] = widen(ahead.get(0, i, k));
+                s[i] += x[i][k].sum();                         // places beyond the row hold zeros
+            }
         }
-    constexpr int C = L * K * V;
-    if (lane < L)
+        ahead.done();
+        issue(turn + p.stages);                                // into the slots just read
+        const float my_mean = group_sums<L, R>(s, first, slots[0]) / cols;     // a division: constant rows give exact zeros
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const float mean = L <= 0 ? my_mean : spread_get<L <= 0 ? 32 : L, R>(my_mean, i, lane);
+            s[i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                x[i][k].shift(-mean);
+                const float q = x[i][k].dot(x[i][k]);
+                s[i] += first + k * step < n_vec ? q : 0.0f;
+            }
+        }
+        const float my_rstd = rsqrtf(group_sums<L, R>(s, first, slots[1]) * inverse + p.eps);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const float rstd = L <= 0 ? my_rstd : spread_get<L <= 0 ? 32 : L, R>(my_rstd, i, lane);
+            const bool live = turn < turns.live[i];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                Pairs<V> o = wb.get(1, k);
+                x[i][k].mul_all(rstd);
+                o.fma(x[i][k], wb.get(0, k));
+                hagr::Vec<T, V> to;
+                to.set(o.v);
+                if (live && first + k * step < n_vec) to.store(y + i * ld_y, first + k * step);
+            }
+        }
+        if (L <= 0 ? first == 0 : first % ((L <= 0 ? R : L) / R) == 0 && r < p.n) {
+            if (p.mean) p.mean[r] = my_mean;
+            if (p.rstd) p.rstd[r] = my_rstd;
+        }
+        y += step_y;
+        r += turns.stride;
+    }
+    hagr::wait_copies<0>();
+}
+
+template <typename T, int V, int L, int K>
+__global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>)) norm_bwd_kernel(const NormArgs p) {
+    hagk::pdl_launch_dependents();
+    extern __shared__ __align__(16) char raw[];
+    __shared__ float2 slots[2][32];
+    constexpr int R = kBwdRows<T, L, V, K>, S = L <= 0 ? 32 : L;
+    constexpr bool HOLD = L != 0 && R * K * V <= 16;                     // keep xh and g * w between their two uses
+    constexpr bool RAW = !HOLD && !kRing<T, V>;                // keep the raw row (the ring still has it)
+    const Turns<L, R> turns(p.n);
+    const int lane = threadIdx.x & 31, first = turns.first, step = turns.step;
+    const int32_t n_vec = p.D / V;
+    const float inverse = 1.0f / float(p.D);
+    Params<V, K, 1, kRing<T, V>> weights(raw, first, step);
+    Ahead<T, V, K, R, 2, (L > 0 ? kThreads<L> : 0)> ahead(raw + Params<V, K, 1, kRing<T, V>>::bytes(step), p.stages);
+    const int64_t ld_x = p.ld_x * int64_t(sizeof(T)), ld_g = p.ld_g * int64_t(sizeof(T)), ld_y = p.ld_y * int64_t(sizeof(T));
+    const char *x_next = static_cast<const char *>(p.x) + turns.row * ld_x, *g_next = static_cast<const char *>(p.g) + turns.row * ld_g;
+    char *y = static_cast<char *>(p.y) + turns.row * ld_y;
+    const int64_t step_x = turns.stride * ld_x, step_g = turns.stride * ld_g, step_y = turns.stride * ld_y;
+    auto issue = [&](int32_t turn) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            ahead.issue(0, i, x_next + i * ld_x, turn < turns.live[i], first, step, n_vec);
+            ahead.issue(1, i, g_next + i * ld_g, turn < turns.live[i], first, step, n_vec);
+        }
+        ahead.issued();
+        x_next += step_x;
+        g_next += step_g;
+    };
+    // The rows' statistics: each lane of a group (or warp) reads those of another turn, S turns at once and S turns
+    // ahead, and hands them round when the turn comes.
+    float mean[R], rstd[R], mean_next[R], rstd_next[R];
+    auto statistics = [&](int32_t turn) {
+        const int32_t mine = turn + lane % S;
+        const int64_t at = turns.row + int64_t(mine) * turns.stride;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            mean_next[i] = mine < turns.live[i] ? __ldcg(p.mean_in + at + i) : 0.0f;
+            rstd_next[i] = mine < turns.live[i] ? __ldcg(p.rstd_in + at + i) : 0.0f;
+        }
+    };
+    Pairs<V> aw[K], ab[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        aw[k].fill(0.0f);
+        ab[k].fill(0.0f);
+    }
+    hagk::pdl_wait();
+    for (int32_t s = 0; s < p.stages; ++s) issue(s);
+    statistics(0);
+    weights.load(0, p.w, p.w_bf16, p.w_vectors, p.D, 1.0f, L <= 0 || threadIdx.x < L);
+    if (L > 0 && weights.kShared) __syncthreads();
+    for (int32_t turn = 0; turn < turns.all; ++turn) {
+        if (turn % S == 0) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                mean[i] = mean_next[i];
+                rstd[i] = rstd_next[i];
+            }
+            statistics(turn + S);
+        }
+        ahead.wait(p.stages);
+        hagr::Vec<T, V> rx[RAW ? R * K : 1], rg[RAW ? R * K : 1];
+        Pairs<V> xh[R][K], gw[R][K];
+        float m[R], q[R], s[2 * R];
+        // where the thread is beyond the row g is zero and its terms vanish
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            m[i] = __shfl_sync(0xffffffffu, mean[i], (lane & ~(S - 1)) + turn % S);
+            q[i] = __shfl_sync(0xffffffffu, rstd[i], (lane & ~(S - 1)) + turn % S);
+            s[2 * i] = s[2 * i + 1] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const hagr::Vec<T, V> vx = ahead.get(0, i, k), vg = ahead.get(1, i, k);
+                if (RAW) {
+                    rx[RAW ? i * K + k : 0] = vx;
+                    rg[RAW ? i * K + k : 0] = vg;
+                }
+                Pairs<V> a = widen(vx), t = widen(vg);
+                a.shift_scale(-m[i], q[i]);
+                ab[k].add(t);
+                aw[k].fma(t, a);
+                t.mul(weights.get(0, k));
+                s[2 * i] += t.sum();
+                s[2 * i + 1] += t.dot(a);
+                if (HOLD) {
+                    xh[i][k] = a;
+                    gw[i][k] = t;
+                }
+            }
+        }
+        if (HOLD || RAW) {
+            ahead.done();
+            issue(turn + p.stages);
+        }
+        float s1[R], s2[R];
+        if constexpr (L <= 0) {
+            const float2 t = block_sum2(s[0], s[1], slots[turn & 1]);
+            s1[0] = t.x * inverse;
+            s2[0] = t.y * inverse;
+        } else {
+            const float mine = spread_sums<L, 2 * R>(s, first) * inverse;
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                s1[i] = spread_get<L, 2 * R>(mine, 2 * i, lane);
+                s2[i] = spread_get<L, 2 * R>(mine, 2 * i + 1, lane);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const bool live = turn < turns.live[i];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                Pairs<V> a, t;
+                if constexpr (HOLD) {
+                    a = xh[i][k];
+                    t = gw[i][k];
+                } else {
+                    a = widen(RAW ? rx[RAW ? i * K + k : 0] : ahead.get(0, i, k));
+                    t = widen(RAW ? rg[RAW ? i * K + k : 0] : ahead.get(1, i, k));
+                    a.shift_scale(-m[i], q[i]);
+                    t.mul(weights.get(0, k));
+                }
+                a.affine(-s2[i], -s1[i]);
+                a.add(t);
+                a.mul_all(q[i]);
+                hagr::Vec<T, V> o;
+                o.set(a.v);
+                if (live && first + k * step < n_vec) o.store(y + i * ld_y, first + k * step);
+            }
+        }
+        if (!HOLD && !RAW) {
+            ahead.done();
+            issue(turn + p.stages);
+        }
+        y += step_y;
+    }
+    hagr::wait_copies<0>();
+    if (!p.partial) return;
+    if constexpr (L <= 0) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                joined[(warp * 2 + 0) * C + (gl + k * L) * V + j] = aw.v[k * V + j];
-                joined[(warp * 2 + 1) * C + (gl + k * L) * V + j] = ab.v[k * V + j];
+                const int32_t c = (first + k * step) * V + j;
+                if (c >= p.D) continue;
+                p.partial[int64_t(blockIdx.x) * 2 * p.D + c] = aw[k].v[j];
+                p.partial[(int64_t(blockIdx.x) * 2 + 1) * p.D + c] = ab[k].v[j];
             }
-    __syncthreads();
-    for (int c = threadIdx.x; c < 2 * C; c += kWarpThreads) {
-        const int which = c / C, col = c - which * C;
-        if (col >= p.D) continue;
-        float s = 0.0f;
+    } else {
+        // groups of the warp, then warps of the block, in a fixed order
 #pragma unroll
-        for (int q = 0; q < kWarpRows; ++q) s += joined[q * 2 * C + c];
-        p.partial[(int64_t(blockIdx.x) * 2 + which) * p.D + col] = s;
-    }
-}
-
-template <typename T, int V, int MAX_THREADS>
-__global__ void __launch_bounds__(MAX_THREADS) norm_bwd_block_kernel(const NormArgs p) {
-    hagk::pdl_launch_dependents();
-    constexpr int K = kPerLane / V;
-    __shared__ float2 slot[2][32];
-    const int32_t n_vec = p.D / V, step = blockDim.x;
-    const float cols = float(p.D);
-    Pairs<K * V> w, aw, ab;
-    aw.fill(0.0f);
-    ab.fill(0.0f);
-    hagk::pdl_wait();
-    load_params<V, K>(p.w, p.w_bf16, p.D, threadIdx.x, step, 1.0f, w.v);
-    int turn = 0;
-    BwdRow<T, V, K> row, next;
-    row.load(p, blockIdx.x, threadIdx.x, step, n_vec);
-    for (int64_t r = blockIdx.x; r < p.n; r += gridDim.x, turn ^= 1) {
-        next.load(p, r + gridDim.x, threadIdx.x, step, n_vec);
-        float s1, s2;
-        row.sums(w, aw, ab, s1, s2);
-        const float2 s = block_sum2(s1, s2, slot[turn]);
-        row.store(p, r, threadIdx.x, step, n_vec, w, s.x / cols, s.y / cols);
-        row = next;
-    }
-    if (!p.partial) return;
+        for (int o = S; o < 32; o <<= 1)
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+            for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int32_t c = (int32_t(threadIdx.x) + k * step) * V + j;
-            if (c >= p.D) continue;
-            p.partial[int64_t(blockIdx.x) * 2 * p.D + c] = aw.v[k * V + j];
-            p.partial[(int64_t(blockIdx.x) * 2 + 1) * p.D + c] = ab.v[k * V + j];
+                for (int j = 0; j < V; ++j) {
+                    aw[k].v[j] += __shfl_xor_sync(0xffffffffu, aw[k].v[j], o);
+                    ab[k].v[j] += __shfl_xor_sync(0xffffffffu, ab[k].v[j], o);
+                }
+        constexpr int C = S * K * V;
+        float *joined = reinterpret_cast<float *>(raw);        // [warps][2][C], over the ring
+        const int warp = threadIdx.x >> 5;
+        __syncthreads();
+        if (lane < S)
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    joined[(warp * 2 + 0) * C + (first + k * S) * V + j] = aw[k].v[j];
+                    joined[(warp * 2 + 1) * C + (first + k * S) * V + j] = ab[k].v[j];
+                }
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * C; c += blockDim.x) {
+            const int which = c / C, col = c - which * C;
+            if (col >= p.D) continue;
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kThreads<L> / 32; ++w) v += joined[w * 2 * C + c];
+            p.partial[(int64_t(blockIdx.x) * 2 + which) * p.D + col] = v;
         }
+    }
 }
 
 // gw and gb from the parts: a block takes 32 columns of [gw | gb], its 32 warps every 32nd part each.
@@ -549,7 +733,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) norm_params_join_kernel(const
 
 constexpr int kParts = 64;                // of the kernels for rows of any width
 constexpr int kSms = 148;
-constexpr int kMaxParts = kSms * 8;       // of the register kernels: their blocks
+constexpr int kMaxParts = kSms * 8;       // of the other kernels: their blocks
+constexpr int kSmShared = 227 * 1024;     // shared memory of an SM that blocks can use, and of one block
+constexpr int kMostShared = kSmShared - 1024;
 
 cudaError_t launch(void (*kernel)(NormArgs), dim3 grid, unsigned threads, size_t shared, const NormArgs &p, cudaStream_t s) {
     cudaLaunchConfig_t cfg{};
@@ -575,65 +761,86 @@ int resident_blocks(void (*kernel)(NormArgs), unsigned threads, size_t shared) {
     return std::min(per_sm * kSms, kMaxParts);
 }
 
-template <typename T, int V, int L, int K>
-cudaError_t launch_warp(NormArgs &p, bool bwd, cudaStream_t s) {
-    constexpr int RF = kPerLane / (K * V) < 4 ? kPerLane / (K * V) : 4, RB = K * V <= 8 ? 2 : 1;
-    void (*const kernel)(NormArgs) = bwd ? norm_bwd_warp_kernel<T, V, L, K, RB> : norm_fwd_warp_kernel<T, V, L, K, RF>;
-    const size_t shared = bwd && p.partial ? size_t(kWarpRows) * 2 * L * K * V * 4 : 0;
-    static const int resident[2] = {resident_blocks(norm_fwd_warp_kernel<T, V, L, K, RF>, kWarpThreads, 0),
-                                    resident_blocks(norm_bwd_warp_kernel<T, V, L, K, RB>, kWarpThreads, size_t(kWarpRows) * 2 * L * K * V * 4)};
-    const int64_t rows_per_block = int64_t(kWarpRows) * (32 / L) * (bwd ? RB : RF);
-    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>((p.n + rows_per_block - 1) / rows_per_block, resident[bwd]));
-    p.parts = int32_t(blocks);
-    return launch(kernel, dim3(unsigned(blocks)), kWarpThreads, shared, p, s);
+// Lets a kernel use all the shared memory of the current device's SMs (once per kernel and device).
+template <auto KERNEL>
+cudaError_t allow_shared() {
+    static std::atomic<uint64_t> ready{0};
+    int device = 0;
+    cudaError_t err = cudaGetDevice(&device);
+    const uint64_t bit = uint64_t(1) << (device & 63);
+    if (err != cudaSuccess || (ready.load(std::memory_order_relaxed) & bit)) return err;
+    err = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+    if (err == cudaSuccess) ready.fetch_or(bit, std::memory_order_relaxed);
+    return err;
 }
 
-// MAX_THREADS 512 leaves a thread the 128 registers that the three per-column sets of the backward pass need; only
-// rows that need more threads pay with spills.
-template <typename T, int V, int MAX_THREADS>
-cudaError_t launch_block(NormArgs &p, bool bwd, cudaStream_t s) {
-    constexpr int K = kPerLane / V;
-    void (*const kernel)(NormArgs) = bwd ? norm_bwd_block_kernel<T, V, MAX_THREADS> : norm_fwd_block_kernel<T, V, MAX_THREADS>;
-    const unsigned threads = unsigned(((p.D / V + K - 1) / K + 31) / 32 * 32);
-    static std::atomic<int> resident[2][MAX_THREADS / 32 + 1];
-    int most = resident[bwd][threads / 32].load(std::memory_order_relaxed);
-    if (most == 0) resident[bwd][threads / 32].store(most = resident_blocks(kernel, threads, 0), std::memory_order_relaxed);
-    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(p.n, most));
-    p.parts = int32_t(blocks);
-    return launch(kernel, dim3(unsigned(blocks)), threads, 0, p, s);
+template <typename T, int V, int L, int K, bool BWD>
+cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
+    constexpr int R = BWD ? kBwdRows<T, L, V, K> : kFwdRows<T, L, V, K>, OPS = BWD ? 2 : 1;
+    constexpr auto kernel = BWD ? norm_bwd_kernel<T, V, L, K> : norm_fwd_kernel<T, V, L, K>;
+    cudaError_t err = allow_shared<kernel>();
+    if (err != cudaSuccess) return err;
+    const int threads = L <= 0 ? ((p.D / V + K - 1) / K + 31) / 32 * 32 : kThreads<L>;
+    const size_t params = Params<V, K, BWD ? 1 : 2, kRing<T, V>>::bytes(L <= 0 ? threads : L);
+    const size_t stage = size_t(Ahead<T, V, K, R, OPS, 0>::kStage) * threads;
+    // as many stages as leave room for the blocks that the registers allow
+    const int blocks = L <= 0 ? std::max(1, std::min(8, 768 / threads)) : BWD ? 2 : 1;
+    p.stages = L <= 0 ? kBlockStages : BWD ? kBwdStages : kFwdStages;
+    if (!kRing<T, V>) p.stages = 1;
+    while (p.stages > 1 && (params + p.stages * stage + 1024) * blocks > size_t(kSmShared)) --p.stages;
+    size_t shared = params + p.stages * stage;
+    if (BWD && L > 0) shared = std::max(shared, size_t(threads / 32) * 2 * (L > 0 ? L : 0) * K * V * 4);
+    if (shared > size_t(kMostShared)) return cudaErrorInvalidConfiguration;
+    static std::atomic<int> resident[kMostThreads / 32 + 1];
+    int most = resident[threads / 32].load(std::memory_order_relaxed);
+    if (most == 0) resident[threads / 32].store(most = resident_blocks(kernel, threads, shared), std::memory_order_relaxed);
+    if (kRing<T, V> && L > 0) most = std::min(most, kSms * (BWD ? 2 : 1));
+    const int64_t rows_per_block = L <= 0 ? 1 : int64_t(threads / 32) * (32 / (L <= 0 ? 32 : L)) * R;
+    const int64_t grid = std::max<int64_t>(1, std::min<int64_t>((p.n + rows_per_block - 1) / rows_per_block, most));
+    p.parts = int32_t(grid);
+    return launch(kernel, dim3(unsigned(grid)), unsigned(threads), shared, p, s);
 }
 
-// Rows of up to 32 * kPerLane elements go to a warp or a part of one, rows of up to 1024 * kPerLane to a block.
-template <typename T, int V>
-cudaError_t launch_rows(NormArgs &p, bool bwd, cudaStream_t s) {
+// Rows of up to 1024 elements (narrow vectors: 512) go to a warp or a part of one, rows of up to 1024 * kPerThread to
+// a block.
+constexpr int kPerThread = 16;
+template <typename T, int V, bool BWD>
+cudaError_t launch_width(NormArgs &p, cudaStream_t s) {
     const int32_t n_vec = p.D / V;
     if constexpr (V * int(sizeof(T)) == 16) {
-        if (n_vec <= 8) return launch_warp<T, V, 8, 1>(p, bwd, s);
-        if (n_vec <= 16) return launch_warp<T, V, 16, 1>(p, bwd, s);
+        if (n_vec <= 8) return launch_rows<T, V, 8, 1, BWD>(p, s);
+        if (n_vec <= 16) return launch_rows<T, V, 16, 1, BWD>(p, s);
     }
-    if (n_vec <= 32) return launch_warp<T, V, 32, 1>(p, bwd, s);
-    if (n_vec <= 64) return launch_warp<T, V, 32, 2>(p, bwd, s);
-    if constexpr (V <= 4)
-        if (n_vec <= 128) return launch_warp<T, V, 32, 4>(p, bwd, s);
-    if constexpr (V <= 2)
-        if (n_vec <= 256) return launch_warp<T, V, 32, 8>(p, bwd, s);
-    if constexpr (V == 1)
-        if (n_vec <= 512) return launch_warp<T, V, 32, 16>(p, bwd, s);
-    if (p.D <= 512 * kPerLane) return launch_block<T, V, 512>(p, bwd, s);
-    return launch_block<T, V, 1024>(p, bwd, s);
+    if (n_vec <= 32) return launch_rows<T, V, 32, 1, BWD>(p, s);
+    if (n_vec <= 64) return launch_rows<T, V, 32, 2, BWD>(p, s);
+    // vectors per lane of a warp; narrow vectors of the backward pass: 8 columns per thread (300 000 x 333 bf16 takes
+    // 249 us, with 16 columns 600: too many registers), of the forward pass 16 (138 us, with 8 215)
+    constexpr int kMost = (kRing<T, V> ? 32 : BWD ? 8 : 16) / V;
+    if constexpr (kMost >= 4)
+        if (n_vec <= 128) return launch_rows<T, V, 32, 4, BWD>(p, s);
+    if constexpr (kMost >= 8)
+        if (n_vec <= 256) return launch_rows<T, V, 32, 8, BWD>(p, s);
+    if constexpr (kMost >= 16)
+        if (n_vec <= 512) return launch_rows<T, V, 32, 16, BWD>(p, s);
+    constexpr int kFew = (kRing<T, V> || !BWD ? kPerThread : 8) / V;
+    if (n_vec <= kFewThreads * kFew) return launch_rows<T, V, -1, kFew, BWD>(p, s);
+    return launch_rows<T, V, 0, kPerThread / V, BWD>(p, s);
 }
 
-constexpr int32_t kMostInRegisters = 1024 * kPerLane;
+constexpr int32_t kMostInBlock = kMostThreads * kPerThread;
 
-template <typename T>
-cudaError_t launch_typed(NormArgs &p, bool bwd, cudaStream_t s) {
-    const int e = int(sizeof(T));
+template <typename T, bool BWD>
+cudaError_t launch_typed(NormArgs &p, cudaStream_t s) {
+    const int e = int(sizeof(T)), we = p.w_bf16 ? 2 : 4;
     const hagr::Operand ops[] = {{p.x, p.ld_x, e}, {p.y, p.ld_y, e}, {p.g, p.ld_g, e}};
-    const int v = hagr::vector_elems(16 / e, p.D, ops);
-    if (v == 16 / e) return launch_rows<T, 16 / e>(p, bwd, s);
+    int v = hagr::vector_elems(16 / e, p.D, ops);
+    if (v < 16 / e) v = sizeof(T) == 2 && v > 1 ? 2 : 1;
+    const hagr::Operand params[] = {{p.w, 0, we}, {p.b, 0, we}};
+    p.w_vectors = hagr::vector_elems(v, p.D, params) == v;
+    if (v == 16 / e) return launch_width<T, 16 / e, BWD>(p, s);
     if constexpr (sizeof(T) == 2)
-        if (v > 1) return launch_rows<T, 2>(p, bwd, s);
-    return launch_rows<T, 1>(p, bwd, s);
+        if (v == 2) return launch_width<T, 2, BWD>(p, s);
+    return launch_width<T, 1, BWD>(p, s);
 }
 
 bool dtype_ok(hag_dtype d) { return d == HAG_F32 || d == HAG_BF16; }
@@ -680,8 +887,8 @@ extern "C" hag_status hag_layer_norm_fwd(int64_t n, int32_t D, hag_dtype dtype, 
     p.x = x; p.ld_x = ld_x; p.w = weight; p.b = bias; p.y = y; p.ld_y = ld_y; p.mean = mean; p.rstd = rstd; p.eps = eps;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t err;
-    if (D <= kMostInRegisters)
-        err = dtype == HAG_F32 ? launch_typed<float>(p, false, s) : launch_typed<__nv_bfloat16>(p, false, s);
+    if (D <= kMostInBlock)
+        err = dtype == HAG_F32 ? launch_typed<float, false>(p, s) : launch_typed<__nv_bfloat16, false>(p, s);
     else
         err = launch(dtype == HAG_F32 ? norm_fwd_any_kernel<float> : norm_fwd_any_kernel<__nv_bfloat16>,
                      dim3(unsigned(std::min<int64_t>(n, kSms * 8))), kRowThreads, 0, p, s);
@@ -691,7 +898,7 @@ extern "C" hag_status hag_layer_norm_fwd(int64_t n, int32_t D, hag_dtype dtype, 
 
 extern "C" size_t hag_layer_norm_bwd_workspace_bytes(int64_t n, int32_t D) {
     if (n < 0 || D <= 0) return 0;
-    return size_t(D <= kMostInRegisters ? kMaxParts : kParts) * 2 * size_t(D) * 4;
+    return size_t(D <= kMostInBlock ? kMaxParts : kParts) * 2 * size_t(D) * 4;
 }
 
 extern "C" hag_status hag_layer_norm_bwd(int64_t n, int32_t D, hag_dtype dtype, const void *grad_y, int64_t ld_grad_y, const void *x,
@@ -716,8 +923,8 @@ extern "C" hag_status hag_layer_norm_bwd(int64_t n, int32_t D, hag_dtype dtype, 
     const bool f32 = dtype == HAG_F32;
     const dim3 join_grid(unsigned((2 * int64_t(D) + 31) / 32));
     if (!params) p.partial = nullptr;
-    if (D <= kMostInRegisters) {
-        if (n > 0 || params) err = f32 ? launch_typed<float>(p, true, s) : launch_typed<__nv_bfloat16>(p, true, s);
+    if (D <= kMostInBlock) {
+        if (n > 0 || params) err = f32 ? launch_typed<float, true>(p, s) : launch_typed<__nv_bfloat16, true>(p, s);
         if (params && err == cudaSuccess) err = launch(norm_params_join_kernel, join_grid, 32 * kJoinWarps, 0, p, s);
     } else {
         if (params) {      // first: grad_x may take the place of grad_y or x

@@ -106,16 +106,12 @@ struct Vec {
     }
 };
 
-// Asynchronous copies of B bytes from global to shared memory, straight past the registers; `live` false writes zeros
-// and reads nothing.  A thread sees its own copies after wait_copies.
+// Asynchronous copy of 16 bytes from global to shared memory, straight past the registers.  A thread sees its own copies
+// after wait_copies.
 template <int B>
-__device__ __forceinline__ void copy_async(void *shared, const void *global, bool live) {
-    const uint32_t to = uint32_t(__cvta_generic_to_shared(shared));
-    const int bytes = live ? B : 0;
-    if constexpr (B == 16)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(global), "r"(bytes) : "memory");
-    else
-        asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(to), "l"(global), "r"(bytes), "n"(B) : "memory");
+__device__ __forceinline__ void copy_async(void *shared, const void *global) {
+    static_assert(B == 16, "");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(uint32_t(__cvta_generic_to_shared(shared))), "l"(global) : "memory");
 }
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING>
