@@ -469,8 +469,8 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, false>)
     };
     hagk::pdl_wait();
     for (int32_t s = 0; s < p.stages; ++s) issue(s);
-    wb.load(0, p.w, p.w_bf16, p.w_vectors, p.D, 1.0f, L <= 0 || threadIdx.x < L);
-    wb.load(1, p.b, p.w_bf16, p.w_vectors, p.D, 0.0f, L <= 0 || threadIdx.x < L);
+    wb.load(0, p.w, p.w_bf16, p.w_vectors, p.D, 1.0f, L <= 0 || int(threadIdx.x) < L);
+    wb.load(1, p.b, p.w_bf16, p.w_vectors, p.D, 0.0f, L <= 0 || int(threadIdx.x) < L);
     if (L > 0 && wb.kShared) __syncthreads();
     int64_t r = turns.row + (L <= 0 ? 0 : first * R / (L <= 0 ? 1 : L));        // the row whose statistics this thread holds
     for (int32_t turn = 0; turn < turns.all; ++turn) {
@@ -574,7 +574,7 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
     hagk::pdl_wait();
     for (int32_t s = 0; s < p.stages; ++s) issue(s);
     statistics(0);
-    weights.load(0, p.w, p.w_bf16, p.w_vectors, p.D, 1.0f, L <= 0 || threadIdx.x < L);
+    weights.load(0, p.w, p.w_bf16, p.w_vectors, p.D, 1.0f, L <= 0 || int(threadIdx.x) < L);
     if (L > 0 && weights.kShared) __syncthreads();
     for (int32_t turn = 0; turn < turns.all; ++turn) {
         if (turn % S == 0) {

@@ -50,18 +50,25 @@ __device__ __forceinline__ Words<B> load_words(const void *p) {
     return r;
 }
 
-template <int B>
+// kOnce: written once and not read again soon (evict-first); else an ordinary store.
+template <CacheOp OP, typename W>
+__device__ __forceinline__ void store_word(W *p, W v) {
+    if constexpr (OP == kOnce) __stcs(p, v);
+    else *p = v;
+}
+
+template <CacheOp OP, int B>
 __device__ __forceinline__ void store_words(void *p, const Words<B> &r) {
     if constexpr (B == 2) {
-        *static_cast<uint16_t *>(p) = r.w[0];
+        store_word<OP>(static_cast<uint16_t *>(p), r.w[0]);
     } else if constexpr (B == 4) {
-        *static_cast<uint32_t *>(p) = r.w[0];
+        store_word<OP>(static_cast<uint32_t *>(p), r.w[0]);
     } else if constexpr (B == 8) {
-        *static_cast<uint2 *>(p) = make_uint2(r.w[0], r.w[1]);
+        store_word<OP>(static_cast<uint2 *>(p), make_uint2(r.w[0], r.w[1]));
     } else {
 #pragma unroll
         for (int h = 0; h < B / 16; ++h)
-            static_cast<uint4 *>(p)[h] = make_uint4(r.w[4 * h], r.w[4 * h + 1], r.w[4 * h + 2], r.w[4 * h + 3]);
+            store_word<OP>(static_cast<uint4 *>(p) + h, make_uint4(r.w[4 * h], r.w[4 * h + 1], r.w[4 * h + 2], r.w[4 * h + 3]));
     }
 }
 
@@ -74,8 +81,9 @@ struct Vec {
     __device__ __forceinline__ void load(const void *row, size_t i) {        // elements i * V .. of the row
         raw = load_words<OP, kBytes>(static_cast<const char *>(row) + i * kBytes);
     }
+    template <CacheOp OP = kKeep>
     __device__ __forceinline__ void store(void *row, size_t i) const {
-        store_words<kBytes>(static_cast<char *>(row) + i * kBytes, raw);
+        store_words<OP, kBytes>(static_cast<char *>(row) + i * kBytes, raw);
     }
     __device__ __forceinline__ void zero() {
 #pragma unroll
