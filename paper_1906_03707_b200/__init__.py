@@ -569,6 +569,7 @@ def graph_pool_bwd(seg_ptr, grad_out, n_rows: int, reduce="mean", out=None):
 
 
 # -- around the aggregation: embedding, layer norm, clipping by the global norm -------------------------------------- #
+# Small graphs make these calls a matter of host time: each check below is one cheap attribute of the tensor.
 def _code(dtype) -> int:
     import torch
     if dtype is torch.float32:
@@ -578,14 +579,14 @@ def _code(dtype) -> int:
     raise TypeError(f"values must be float32 or bfloat16, got {dtype}")
 
 
-def _rows(t, what, like=None, device=None, dtype=None):
+def _rows(t, what, like=None, index=None, dtype=None):
     """A 2-D device tensor whose rows are contiguous (any row stride); returns the row stride in elements."""
     if t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{what} must be a 2-D device tensor")
     if like is not None and t.shape != like:
         raise ValueError(f"{what} must have shape {tuple(like)}, got {tuple(t.shape)}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{what} must live on {device}")
+    if index is not None and t.get_device() != index:
+        raise ValueError(f"{what} must live on cuda:{index}")
     if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
     rs, cs = t.stride()
@@ -594,10 +595,10 @@ def _rows(t, what, like=None, device=None, dtype=None):
     return rs
 
 
-def _vector(t, what, count, device, dtype=None):
-    """A contiguous 1-D device tensor of `count` values."""
-    if t.dim() != 1 or t.shape[0] != count or not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{what} must be a contiguous tensor of {count} values on {device}")
+def _vector(t, what, count, index, dtype=None):
+    """A contiguous 1-D device tensor of `count` values; returns its address."""
+    if t.dim() != 1 or t.shape[0] != count or not t.is_contiguous() or t.get_device() != index:
+        raise ValueError(f"{what} must be a contiguous tensor of {count} values on cuda:{index}")
     if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
     return t.data_ptr()
@@ -612,29 +613,37 @@ def _scratch_for(workspace, need, device):
     return workspace
 
 
-def _call(name, device, *args):
-    """One C call on the device's current stream."""
+def _call(name, index, *args):
+    """One C call on the current stream of device `index`."""
     import torch
     fn = getattr(_lib or load_library(), name)
-    index = device.index
     if torch.cuda.current_device() == index:
-        st = fn(*args, torch.cuda.current_stream(index).cuda_stream)
+        st = fn(*args, _stream(index))
     else:
         with torch.cuda.device(index):
-            st = fn(*args, torch.cuda.current_stream(index).cuda_stream)
+            st = fn(*args, _stream(index))
     if st != 0:
         _check(st, name)
 
 
-def _ids(ids, device, n=None):
+def _stream(index):
+    """The current stream's handle: what torch.cuda.current_stream(index).cuda_stream gives, without the Stream object
+    (1.3 us of a call's 10)."""
     import torch
-    if ids.dim() != 1 or not ids.is_contiguous() or ids.device != device or (n is not None and ids.shape[0] != n):
-        raise ValueError(f"ids must be a contiguous 1-D tensor{'' if n is None else f' of {n} values'} on {device}")
-    if ids.dtype is torch.int64:
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+
+
+def _ids(ids, index, n=None):
+    import torch
+    if ids.dim() != 1 or not ids.is_contiguous() or ids.get_device() != index or (n is not None and ids.shape[0] != n):
+        raise ValueError(f"ids must be a contiguous 1-D tensor{'' if n is None else f' of {n} values'} on cuda:{index}")
+    dtype = ids.dtype
+    if dtype is torch.int64:
         return HAG_ID64
-    if ids.dtype is torch.int32:
+    if dtype is torch.int32:
         return HAG_ID32
-    raise TypeError(f"ids must be int32 or int64, got {ids.dtype}")
+    raise TypeError(f"ids must be int32 or int64, got {dtype}")
 
 
 def embedding_fwd(ids, table, scale=1.0, out=None, dtype=None):
@@ -642,14 +651,15 @@ def embedding_fwd(ids, table, scale=1.0, out=None, dtype=None):
     of ``dtype`` (default: the table's)."""
     import torch
     ld = _rows(table, "table")
-    device, n, (v, d) = table.device, ids.shape[0] if ids.dim() == 1 else -1, table.shape
-    id_type = _ids(ids, device)
+    index, (v, d) = table.get_device(), table.shape
+    id_type = _ids(ids, index)
+    n = ids.shape[0]
     if out is None:
-        out = torch.empty((n, d), dtype=dtype or table.dtype, device=device)
+        out = torch.empty((n, d), dtype=dtype or table.dtype, device=table.device)
         ld_out = d
     else:
-        ld_out = _rows(out, "out", (n, d), device, dtype)
-    _call("hag_embedding_fwd", device, ids.data_ptr(), id_type, n, v, table.data_ptr(), _code(table.dtype), ld, _code(out.dtype), d,
+        ld_out = _rows(out, "out", (n, d), index, dtype)
+    _call("hag_embedding_fwd", index, ids.data_ptr(), id_type, n, v, table.data_ptr(), _code(table.dtype), ld, _code(out.dtype), d,
           scale, out.data_ptr(), ld_out)
     return out
 
@@ -659,15 +669,15 @@ def embedding_bwd(ids, grad_out, n_rows: int, scale=1.0, out=None, dtype=None, w
     (default: grad_out's)."""
     import torch
     ld = _rows(grad_out, "grad_out")
-    device, (n, d) = grad_out.device, grad_out.shape
-    id_type = _ids(ids, device, n)
+    index, device, (n, d) = grad_out.get_device(), grad_out.device, grad_out.shape
+    id_type = _ids(ids, index, n)
     if out is None:
         out = torch.empty((n_rows, d), dtype=dtype or grad_out.dtype, device=device)
         ld_out = d
     else:
-        ld_out = _rows(out, "out", (n_rows, d), device, dtype)
+        ld_out = _rows(out, "out", (n_rows, d), index, dtype)
     ws = _scratch_for(workspace, load_library().hag_embedding_bwd_workspace_bytes(n, n_rows, d), device)
-    _call("hag_embedding_bwd", device, ids.data_ptr(), id_type, n, n_rows, _code(grad_out.dtype), d, grad_out.data_ptr(), ld, scale,
+    _call("hag_embedding_bwd", index, ids.data_ptr(), id_type, n, n_rows, _code(grad_out.dtype), d, grad_out.data_ptr(), ld, scale,
           out.data_ptr(), _code(out.dtype), ld_out, None if ws is None else ws.data_ptr())
     return out
 
@@ -677,20 +687,22 @@ def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None, stats=True):
     false (no gradient wanted).  ``out`` may be x."""
     import torch
     ld = _rows(x, "x")
-    device, (n, d) = x.device, x.shape
+    index, dtype, (n, d) = x.get_device(), x.dtype, x.shape
     wdt = weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
-    w = None if weight is None else _vector(weight, "weight", d, device)
-    b = None if bias is None else _vector(bias, "bias", d, device, wdt)
+    w = None if weight is None else _vector(weight, "weight", d, index)
+    b = None if bias is None else _vector(bias, "bias", d, index, wdt)
     if out is None:
-        out = torch.empty((n, d), dtype=x.dtype, device=device)
+        out = torch.empty((n, d), dtype=dtype, device=x.device)
         ld_out = d
     else:
-        ld_out = _rows(out, "out", x.shape, device, x.dtype)
-    mean = rstd = None
+        ld_out = _rows(out, "out", x.shape, index, dtype)
+    mean = rstd = m = r = None
     if stats:
-        mean, rstd = torch.empty((2, n), dtype=torch.float32, device=device).unbind()
-    _call("hag_layer_norm_fwd", device, n, d, _code(x.dtype), x.data_ptr(), ld, w, b, _code(wdt), eps, out.data_ptr(), ld_out,
-          None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr())
+        both = torch.empty((2, n), dtype=torch.float32, device=x.device)
+        mean, rstd = both.unbind()
+        m = both.data_ptr()
+        r = m + 4 * n
+    _call("hag_layer_norm_fwd", index, n, d, _code(dtype), x.data_ptr(), ld, w, b, _code(wdt), eps, out.data_ptr(), ld_out, m, r)
     return out, mean, rstd
 
 
@@ -700,76 +712,71 @@ def layer_norm_bwd(grad_out, x, mean, rstd, weight=None, out=None, param_grads=T
     is false.  ``out`` may be grad_out or x."""
     import torch
     ld = _rows(x, "x")
-    device, (n, d) = x.device, x.shape
-    ld_g = _rows(grad_out, "grad_out", x.shape, device, x.dtype)
-    w = None if weight is None else _vector(weight, "weight", d, device, param_dtype)
+    index, device, dtype, shape = x.get_device(), x.device, x.dtype, x.shape
+    n, d = shape
+    ld_g = _rows(grad_out, "grad_out", shape, index, dtype)
+    w = None if weight is None else _vector(weight, "weight", d, index, param_dtype)
     wdt = weight.dtype if weight is not None else param_dtype or torch.float32
-    m, r = _vector(mean, "mean", n, device, torch.float32), _vector(rstd, "rstd", n, device, torch.float32)
+    m, r = _vector(mean, "mean", n, index, torch.float32), _vector(rstd, "rstd", n, index, torch.float32)
     if out is None:
-        out = torch.empty((n, d), dtype=x.dtype, device=device)
+        out = torch.empty((n, d), dtype=dtype, device=device)
         ld_out = d
     else:
-        ld_out = _rows(out, "out", x.shape, device, x.dtype)
-    gw = gb = ws = None
+        ld_out = _rows(out, "out", shape, index, dtype)
+    gw = gb = ws = gwp = gbp = None
+    code = _code(wdt)
     if param_grads:
-        gw, gb = torch.empty((2, d), dtype=wdt, device=device).unbind()
+        both = torch.empty((2, d), dtype=wdt, device=device)
+        gw, gb = both.unbind()
+        gwp = both.data_ptr()
+        gbp = gwp + d * (4 if code == HAG_F32 else 2)
         ws = _scratch_for(workspace, load_library().hag_layer_norm_bwd_workspace_bytes(n, d), device)
-    _call("hag_layer_norm_bwd", device, n, d, _code(x.dtype), grad_out.data_ptr(), ld_g, x.data_ptr(), ld, m, r, w, _code(wdt),
-          out.data_ptr(), ld_out, None if gw is None else gw.data_ptr(), None if gb is None else gb.data_ptr(),
-          None if ws is None else ws.data_ptr())
+    _call("hag_layer_norm_bwd", index, n, d, _code(dtype), grad_out.data_ptr(), ld_g, x.data_ptr(), ld, m, r, w, code, out.data_ptr(),
+          ld_out, gwp, gbp, None if ws is None else ws.data_ptr())
     return out, gw, gb
 
 
-def _tensor_list(tensors, device):
-    """Pointers, lengths and type codes of a list of contiguous device tensors."""
-    import torch
-    codes = {torch.float32: HAG_F32, torch.bfloat16: HAG_BF16}
-    try:
-        kinds = [codes[t.dtype] for t in tensors]
-    except KeyError as e:
-        raise TypeError(f"gradients must be float32 or bfloat16, got {e.args[0]}") from None
-    if not all(t.is_contiguous() and t.device == device for t in tensors):
-        raise ValueError(f"gradients must be contiguous tensors on {device}")
+def _tensor_list(tensors, index):
+    """Addresses, lengths and type codes of a list of contiguous device tensors."""
+    kinds = [t.dtype for t in tensors]
+    for k in set(kinds):
+        _code(k)
+    if not all([t.is_contiguous() for t in tensors]) or {t.get_device() for t in tensors} != {index}:
+        raise ValueError(f"gradients must be contiguous tensors on cuda:{index}")
     return [t.data_ptr() for t in tensors], [t.numel() for t in tensors], kinds
 
 
 def clip_grad_norm(grads, max_norm, out=None, workspace=None):
     """``hag_clip_grad_norm``: (the gradients scaled so that their global norm is at most max_norm, that norm as it was).
-    ``out`` is a list of tensors like ``grads``, or ``grads`` itself (in place); default: new tensors."""
+    ``out`` is a list of tensors with the lengths and types of ``grads``, or ``grads`` itself (in place); default: new
+    tensors."""
     import torch
-    grads = list(grads)
-    if not grads:
-        raise ValueError("the list of gradients is empty")
-    device, count = grads[0].device, len(grads)
-    if not grads[0].is_cuda:
-        raise ValueError("gradients must be device tensors")
-    ptrs, lens, kinds = _tensor_list(grads, device)
-    if len(set(ptrs)) != count and len({p for p, m in zip(ptrs, lens) if m}) != sum(m > 0 for m in lens):
-        raise ValueError("a gradient is named twice")
-    if out is None:
-        out = [torch.empty_like(g) for g in grads]
-    elif len(out) != count or not all(o is g or (o.shape == g.shape and o.dtype is g.dtype) for o, g in zip(out, grads)):
-        raise ValueError("out must be tensors like the gradients")
-    return out, _clip(device, count, ptrs, _tensor_list(out, device)[0], lens, kinds, max_norm, workspace)
+    return _clip(grads, max_norm, [torch.empty_like(g) for g in grads] if out is None else out, workspace)
 
 
 def grad_norm(grads, workspace=None):
     """The global norm alone (``hag_clip_grad_norm`` without outputs): a float32 tensor of one value."""
-    grads = list(grads)
-    if not grads:
-        raise ValueError("the list of gradients is empty")
-    device = grads[0].device
-    if not grads[0].is_cuda:
-        raise ValueError("gradients must be device tensors")
-    ptrs, lens, kinds = _tensor_list(grads, device)
-    return _clip(device, len(grads), ptrs, None, lens, kinds, float("inf"), workspace)
+    return _clip(grads, float("inf"), None, workspace)[1]
 
 
-def _clip(device, count, ptrs, out_ptrs, lens, kinds, max_norm, workspace):
+def _clip(grads, max_norm, out, workspace):
     import torch
-    pointers = ctypes.c_void_p * count
+    from array import array
+    if not grads or not grads[0].is_cuda:
+        raise ValueError("gradients must be a list of device tensors, not empty")
+    device, index, count = grads[0].device, grads[0].get_device(), len(grads)
+    ptrs, lens, kinds = _tensor_list(grads, index)
+    if out is not None:
+        to, to_lens, to_kinds = (ptrs, lens, kinds) if out is grads else _tensor_list(out, index)
+        if to_lens != lens or to_kinds != kinds:
+            raise ValueError("out must be tensors with the lengths and types of the gradients")
+        for addresses in (ptrs, to):
+            if len(set(addresses)) != count and len({p for p, m in zip(addresses, lens) if m}) != sum(m > 0 for m in lens):
+                raise ValueError("a tensor is named twice")
+        to = array("Q", to)
+    addresses, lengths, codes = array("Q", ptrs), array("q", lens), array("i", [HAG_BF16 if k is torch.bfloat16 else HAG_F32 for k in kinds])
     ws = _scratch_for(workspace, load_library().hag_clip_grad_norm_workspace_bytes(count), device)
     norm = torch.empty((), dtype=torch.float32, device=device)
-    _call("hag_clip_grad_norm", device, count, pointers(*ptrs), None if out_ptrs is None else pointers(*out_ptrs),
-          (ctypes.c_int64 * count)(*lens), (ctypes.c_int * count)(*kinds), max_norm, norm.data_ptr(), ws.data_ptr())
-    return norm
+    _call("hag_clip_grad_norm", index, count, addresses.buffer_info()[0], None if out is None else to.buffer_info()[0],
+          lengths.buffer_info()[0], codes.buffer_info()[0], max_norm, norm.data_ptr(), ws.data_ptr())
+    return out, norm

@@ -2,8 +2,11 @@
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -27,13 +30,14 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
-    cmd = [nvcc, "-O3", "-std=c++17", "-shared", "-Xcompiler", "-fPIC",
-           "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", LIB]
-    if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES] + ["-ldl"]     # -ldl: the header-only NVTX ranges load their tool lazily
-    subprocess.check_call(cmd)
+    common = [nvcc, "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-gencode", "arch=compute_100a,code=sm_100a"]
+    flags = ["-lineinfo", "-I", os.path.join(ROOT, "include"), "-I", CSRC] + (["-Xptxas", "-v"] if verbose else [])
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(len(SOURCES)) as pool:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        list(pool.map(lambda p: subprocess.check_call(common + flags + ["-c", "-o", p[1], os.path.join(CSRC, p[0])]), zip(SOURCES, objects)))
+        linked = os.path.join(tmp, "library.so")
+        subprocess.check_call(common + ["-shared", "-o", linked] + objects + ["-ldl"])     # -ldl: the header-only NVTX ranges load their tool lazily
+        shutil.move(linked, LIB)
     return LIB
 
 

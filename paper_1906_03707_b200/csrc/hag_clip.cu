@@ -18,8 +18,12 @@ namespace {
 
 constexpr int kClipThreads = 256;
 constexpr int kClipList = 128;                 // tensors per launch: the list must fit in 4 KB of parameters
-constexpr int kPieceBytes = 16384;             // a piece of a tensor: four 16-byte loads per thread
-constexpr int kClipBlocks = 148 * 8;
+constexpr int kClipBlocks = 148 * 4;
+// A piece of a tensor: U 16-byte loads per thread, all in flight together.  Long lists take 32 KB pieces (40 tensors of
+// 664 MB: 322 us, with 16 KB pieces 347); short ones 8 KB, which more SMs share.
+constexpr int kLoadsLong = 8, kLoadsShort = 2;
+constexpr int64_t kShortList = 8 << 20;        // bytes
+__host__ __device__ constexpr int piece_bytes(int loads) { return kClipThreads * 16 * loads; }
 
 struct ClipArgs {
     int32_t tensors;
@@ -49,77 +53,106 @@ __device__ __forceinline__ double block_sum(double v, double *slot) {
     return s;
 }
 
-// Calls f(tensor, first element, end element) for the pieces of this block, which ascend.
-template <typename F>
+// Calls f(tensor, first element, end element) for the pieces of this block, from the first to the last or the other way.
+template <int U, bool DOWN, typename F>
 __device__ __forceinline__ void for_pieces(const ClipArgs &p, F f) {
-    int t = 0;
-    for (uint32_t k = blockIdx.x; k < p.pieces; k += gridDim.x) {
-        while (t + 1 < p.tensors && p.first_piece[t + 1] <= k) ++t;
-        const int64_t per = kPieceBytes / (p.bf16[t] ? 2 : 4), b = int64_t(k - p.first_piece[t]) * per;
+    if (blockIdx.x >= p.pieces) return;
+    int t = DOWN ? p.tensors - 1 : 0;
+    const uint32_t turns = (p.pieces - 1 - blockIdx.x) / gridDim.x + 1;
+    for (uint32_t i = 0; i < turns; ++i) {
+        const uint32_t k = blockIdx.x + (DOWN ? turns - 1 - i : i) * gridDim.x;
+        if (DOWN) {
+            while (p.first_piece[t] > k) --t;
+        } else {
+            while (t + 1 < p.tensors && p.first_piece[t + 1] <= k) ++t;
+        }
+        const int64_t per = piece_bytes(U) / (p.bf16[t] ? 2 : 4), b = int64_t(k - p.first_piece[t]) * per;
         f(t, b, min(p.len[t], b + per));
     }
 }
 
-template <typename T, int V>
-__device__ __forceinline__ float piece_squares(const void *in, int64_t b, int64_t e) {
-    constexpr int U = kPieceBytes / kClipThreads / (V * int(sizeof(T)));
-    const char *at = static_cast<const char *>(in) + b * sizeof(T);
-    const int32_t len = int32_t(e - b), full = len / V;
-    float s = 0.0f;
-#pragma unroll(U > 4 ? 4 : U)
-    for (int u = 0; u < U; ++u) {
-        const int32_t i = u * kClipThreads + threadIdx.x;
-        if (i >= full) continue;
-        hagr::Vec<T, V> v;
-        v.template load<hagr::kKeep>(at, i);
+// f(vector, its number) for the vectors of a piece that this thread takes, eight or U of them at a time: all are
+// read before the first is used.
+template <typename T, int V, int U, hagr::CacheOp OP, typename F>
+__device__ __forceinline__ void piece_vectors(const char *at, int32_t len, F f) {
+    constexpr int N = piece_bytes(U) / (kClipThreads * V * int(sizeof(T))), B = N < 8 ? N : 8;
+    const int32_t full = len / V;
+#pragma unroll 1
+    for (int u0 = 0; u0 < N && u0 * kClipThreads < full; u0 += B) {
+        hagr::Vec<T, V> v[B];
+        const bool whole = (u0 + B) * kClipThreads <= full;
 #pragma unroll
-        for (int j = 0; j < V; ++j) s += v.get(j) * v.get(j);
+        for (int u = 0; u < B; ++u) {
+            const int32_t i = (u0 + u) * kClipThreads + int32_t(threadIdx.x);
+            if (!whole) v[u].zero();
+            if (whole || i < full) v[u].template load<OP>(at, i);
+        }
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
+            const int32_t i = (u0 + u) * kClipThreads + int32_t(threadIdx.x);
+            if (whole || i < full) f(v[u], i);
+        }
     }
-    if (V > 1 && int32_t(threadIdx.x) < len - full * V) {
-        hagr::Vec<T, 1> v;
-        v.template load<hagr::kKeep>(at, full * V + threadIdx.x);
-        s += v.get(0) * v.get(0);
-    }
-    return s;
 }
 
-template <typename T, int V>
+template <typename T, int V, int U>
+__device__ __forceinline__ float piece_squares(const void *in, int64_t b, int64_t e) {
+    const char *at = static_cast<const char *>(in) + b * sizeof(T);
+    const int32_t len = int32_t(e - b), done = len / V * V;
+    float2 s0 = make_float2(0.0f, 0.0f), s1 = s0;
+    piece_vectors<T, V, U, hagr::kKeep>(at, len, [&](const hagr::Vec<T, V> &v, int32_t) {
+        if constexpr (V == 1) {
+            s0.x += v.get(0) * v.get(0);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; j += 4) {
+                const float2 p = make_float2(v.get(j), v.get(j + 1)), q = make_float2(v.get(j + 2), v.get(j + 3));
+                s0 = __ffma2_rn(p, p, s0);
+                s1 = __ffma2_rn(q, q, s1);
+            }
+        }
+    });
+    if (V > 1 && int32_t(threadIdx.x) < len - done) {
+        hagr::Vec<T, 1> v;
+        v.template load<hagr::kKeep>(at, done + threadIdx.x);
+        s0.x += v.get(0) * v.get(0);
+    }
+    return (s0.x + s0.y) + (s1.x + s1.y);
+}
+
+template <typename T, int V, int U>
 __device__ __forceinline__ void piece_scale(const void *in, void *out, int64_t b, int64_t e, float c) {
-    constexpr int U = kPieceBytes / kClipThreads / (V * int(sizeof(T)));
     const char *at = static_cast<const char *>(in) + b * sizeof(T);
     char *to = static_cast<char *>(out) + b * sizeof(T);
-    const int32_t len = int32_t(e - b), full = len / V;
-#pragma unroll(U > 4 ? 4 : U)
-    for (int u = 0; u < U; ++u) {
-        const int32_t i = u * kClipThreads + threadIdx.x;
-        if (i >= full) continue;
-        hagr::Vec<T, V> v;
-        v.template load<hagr::kOnce>(at, i);
+    const int32_t len = int32_t(e - b), done = len / V * V;
+    piece_vectors<T, V, U, hagr::kOnce>(at, len, [&](const hagr::Vec<T, V> &v, int32_t i) {
         float f[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = v.get(j) * c;
-        v.set(f);
-        v.store(to, i);
-    }
-    if (V > 1 && int32_t(threadIdx.x) < len - full * V) {
+        hagr::Vec<T, V> o;
+        o.set(f);
+        o.template store<hagr::kOnce>(to, i);
+    });
+    if (V > 1 && int32_t(threadIdx.x) < len - done) {
         hagr::Vec<T, 1> v;
-        v.template load<hagr::kOnce>(at, full * V + threadIdx.x);
+        v.template load<hagr::kOnce>(at, done + threadIdx.x);
         const float f = v.get(0) * c;
         v.set(&f);
-        v.store(to, full * V + threadIdx.x);
+        v.store(to, done + threadIdx.x);
     }
 }
 
-__global__ void __launch_bounds__(kClipThreads) norm_sums_kernel(const __grid_constant__ ClipArgs p) {
+template <int U>
+__global__ void __launch_bounds__(kClipThreads, 2) norm_sums_kernel(const __grid_constant__ ClipArgs p) {
     hagk::pdl_launch_dependents();
     __shared__ double slot[kClipThreads / 32];
     double s = 0.0;       // squares are added in fp32 within a piece, in fp64 from piece to piece
     hagk::pdl_wait();
-    for_pieces(p, [&](int t, int64_t b, int64_t e) {
+    for_pieces<U, false>(p, [&](int t, int64_t b, int64_t e) {
         if (p.bf16[t])
-            s += p.vec[t] ? piece_squares<__nv_bfloat16, 8>(p.in[t], b, e) : piece_squares<__nv_bfloat16, 1>(p.in[t], b, e);
+            s += p.vec[t] ? piece_squares<__nv_bfloat16, 8, U>(p.in[t], b, e) : piece_squares<__nv_bfloat16, 1, U>(p.in[t], b, e);
         else
-            s += p.vec[t] ? piece_squares<float, 4>(p.in[t], b, e) : piece_squares<float, 1>(p.in[t], b, e);
+            s += p.vec[t] ? piece_squares<float, 4, U>(p.in[t], b, e) : piece_squares<float, 1, U>(p.in[t], b, e);
     });
     s = block_sum(s, slot);
     if (threadIdx.x == 0) p.sums[p.first_sum + blockIdx.x] = s;
@@ -140,7 +173,8 @@ __global__ void __launch_bounds__(kClipThreads) norm_join_kernel(const __grid_co
     if (threadIdx.x == 0 && p.norm) *p.norm = norm;
 }
 
-__global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_constant__ ClipArgs p) {
+template <int U>
+__global__ void __launch_bounds__(kClipThreads, 2) clip_scale_kernel(const __grid_constant__ ClipArgs p) {
     hagk::pdl_launch_dependents();
     __shared__ double slot[kClipThreads / 32];
     hagk::pdl_wait();
@@ -148,14 +182,15 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_c
     if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
     const float ratio = p.max_norm / (norm + 1e-6f);
     const float c = ratio >= 1.0f ? 1.0f : ratio;          // a norm that is no number gives a factor that is none
-    for_pieces(p, [&](int t, int64_t b, int64_t e) {
+    // backwards: what the first launch read last is still in the L2
+    for_pieces<U, true>(p, [&](int t, int64_t b, int64_t e) {
         if (c == 1.0f && p.in[t] == p.out[t]) return;      // in place and nothing to change
         if (p.bf16[t]) {
-            if (p.vec[t]) piece_scale<__nv_bfloat16, 8>(p.in[t], p.out[t], b, e, c);
-            else piece_scale<__nv_bfloat16, 1>(p.in[t], p.out[t], b, e, c);
+            if (p.vec[t]) piece_scale<__nv_bfloat16, 8, U>(p.in[t], p.out[t], b, e, c);
+            else piece_scale<__nv_bfloat16, 1, U>(p.in[t], p.out[t], b, e, c);
         } else {
-            if (p.vec[t]) piece_scale<float, 4>(p.in[t], p.out[t], b, e, c);
-            else piece_scale<float, 1>(p.in[t], p.out[t], b, e, c);
+            if (p.vec[t]) piece_scale<float, 4, U>(p.in[t], p.out[t], b, e, c);
+            else piece_scale<float, 1, U>(p.in[t], p.out[t], b, e, c);
         }
     });
 }
@@ -163,13 +198,13 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_c
 int launches_of(int32_t count) { return std::max(1, (count + kClipList - 1) / kClipList); }
 
 // The part of the list that launch `k` handles; false: it has more pieces than a launch can count.
-bool fill(ClipArgs &p, int k, int32_t count, const void *const *in, void *const *out, const int64_t *len, const hag_dtype *dtype) {
+bool fill(ClipArgs &p, int k, int loads, int32_t count, const void *const *in, void *const *out, const int64_t *len, const hag_dtype *dtype) {
     p.tensors = 0;
     int64_t pieces = 0;
     for (int32_t t = k * kClipList; t < std::min(count, (k + 1) * kClipList); ++t) {
         if (len[t] == 0) continue;
         const int i = p.tensors++;
-        const int64_t per = kPieceBytes / (dtype[t] == HAG_BF16 ? 2 : 4);
+        const int64_t per = piece_bytes(loads) / (dtype[t] == HAG_BF16 ? 2 : 4);
         p.in[i] = in[t];
         p.out[i] = out ? out[t] : nullptr;
         p.len[i] = len[t];
@@ -195,10 +230,14 @@ extern "C" hag_status hag_clip_grad_norm(int32_t count, const void *const *grads
     if (count < 0 || !(max_norm >= 0.0f)) return HAG_ERR_ARG;
     if (count > 0 && (!grads || !lengths || !dtypes)) return HAG_ERR_NULL;
     if (!out && !total_norm) return HAG_ERR_NULL;
+    int64_t bytes = 0;
     for (int32_t t = 0; t < count; ++t) {
         if (dtypes[t] != HAG_F32 && dtypes[t] != HAG_BF16) return HAG_ERR_DTYPE;
         if (lengths[t] < 0) return HAG_ERR_ARG;
         if (lengths[t] == 0) continue;
+        if (lengths[t] < kShortList) bytes += lengths[t] * (dtypes[t] == HAG_F32 ? 4 : 2);
+        else bytes = kShortList;
+        bytes = std::min(bytes, kShortList);
         if (!grads[t] || (out && !out[t])) return HAG_ERR_NULL;
         const int elem = dtypes[t] == HAG_F32 ? 4 : 2;
         if (!hagr::element_aligned(grads[t], elem) || (out && !hagr::element_aligned(out[t], elem))) return HAG_ERR_ALIGN;
@@ -207,20 +246,22 @@ extern "C" hag_status hag_clip_grad_norm(int32_t count, const void *const *grads
     if (!workspace) return HAG_ERR_WORKSPACE;
     if (!hagl::aligned16(workspace)) return HAG_ERR_ALIGN;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    const int launches = launches_of(count);
+    const int launches = launches_of(count), loads = bytes < kShortList ? kLoadsShort : kLoadsLong;
+    void (*const sum)(ClipArgs) = loads == kLoadsShort ? norm_sums_kernel<kLoadsShort> : norm_sums_kernel<kLoadsLong>;
+    void (*const scale)(ClipArgs) = loads == kLoadsShort ? clip_scale_kernel<kLoadsShort> : clip_scale_kernel<kLoadsLong>;
     ClipArgs p{};
     p.sums = static_cast<double *>(workspace);
     p.max_norm = max_norm;
     for (int k = 0; k < launches; ++k)      // before the first launch: an error leaves everything as it was
-        if (!fill(p, k, count, grads, out, lengths, dtypes)) return HAG_ERR_TOO_LARGE;
+        if (!fill(p, k, loads, count, grads, out, lengths, dtypes)) return HAG_ERR_TOO_LARGE;
     cudaError_t err = cudaSuccess;
     int32_t sums = 0;
     for (int k = 0; k < launches && err == cudaSuccess; ++k) {
-        if (launches > 1) fill(p, k, count, grads, out, lengths, dtypes);
+        if (launches > 1) fill(p, k, loads, count, grads, out, lengths, dtypes);
         const unsigned grid = unsigned(std::min<int64_t>(std::max<uint32_t>(p.pieces, 1), kClipBlocks));
         p.first_sum = sums;
         sums += int32_t(grid);
-        err = hagl::launch_pdl<ClipArgs>(norm_sums_kernel, grid, unsigned(kClipThreads), p, s);
+        err = hagl::launch_pdl<ClipArgs>(sum, grid, unsigned(kClipThreads), p, s);
     }
     p.n_sums = sums;
     if (err == cudaSuccess && !out) {
@@ -228,10 +269,10 @@ extern "C" hag_status hag_clip_grad_norm(int32_t count, const void *const *grads
         err = hagl::launch_pdl<ClipArgs>(norm_join_kernel, 1u, unsigned(kClipThreads), p, s);
     }
     for (int k = 0; out && k < launches && err == cudaSuccess; ++k) {
-        if (launches > 1) fill(p, k, count, grads, out, lengths, dtypes);
+        if (launches > 1) fill(p, k, loads, count, grads, out, lengths, dtypes);
         p.norm = k == 0 ? total_norm : nullptr;
         const unsigned grid = unsigned(std::min<int64_t>(std::max<uint32_t>(p.pieces, 1), kClipBlocks));
-        err = hagl::launch_pdl<ClipArgs>(clip_scale_kernel, grid, unsigned(kClipThreads), p, s);
+        err = hagl::launch_pdl<ClipArgs>(scale, grid, unsigned(kClipThreads), p, s);
     }
     if (err != cudaSuccess) { cudaGetLastError(); return HAG_ERR_CUDA; }
     return HAG_OK;

@@ -733,7 +733,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) norm_params_join_kernel(const
 
 constexpr int kParts = 64;                // of the kernels for rows of any width
 constexpr int kSms = 148;
-constexpr int kMaxParts = kSms * 8;       // of the other kernels: their blocks
 constexpr int kSmShared = 227 * 1024;     // shared memory of an SM that blocks can use, and of one block
 constexpr int kMostShared = kSmShared - 1024;
 
@@ -751,6 +750,9 @@ cudaError_t launch(void (*kernel)(NormArgs), dim3 grid, unsigned threads, size_t
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
+// Parts of gw and gb, i.e. blocks of the other kernels, at most: wide rows take a block's registers to themselves.
+int most_parts(int32_t D) { return kSms * std::max(1, std::min(8, 8192 / D)); }
+
 // How many blocks of the kernel the device runs at once (asked once per kernel and block size).
 int resident_blocks(void (*kernel)(NormArgs), unsigned threads, size_t shared) {
     int per_sm = 0;
@@ -758,7 +760,7 @@ int resident_blocks(void (*kernel)(NormArgs), unsigned threads, size_t shared) {
         cudaGetLastError();
         per_sm = 1;
     }
-    return std::min(per_sm * kSms, kMaxParts);
+    return per_sm * kSms;
 }
 
 // Lets a kernel use all the shared memory of the current device's SMs (once per kernel and device).
@@ -794,7 +796,7 @@ cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
     static std::atomic<int> resident[kMostThreads / 32 + 1];
     int most = resident[threads / 32].load(std::memory_order_relaxed);
     if (most == 0) resident[threads / 32].store(most = resident_blocks(kernel, threads, shared), std::memory_order_relaxed);
-    if (kRing<T, V> && L > 0) most = std::min(most, kSms * (BWD ? 2 : 1));
+    most = std::min(most, kRing<T, V> && L > 0 ? kSms * (BWD ? 2 : 1) : most_parts(p.D));
     const int64_t rows_per_block = L <= 0 ? 1 : int64_t(threads / 32) * (32 / (L <= 0 ? 32 : L)) * R;
     const int64_t grid = std::max<int64_t>(1, std::min<int64_t>((p.n + rows_per_block - 1) / rows_per_block, most));
     p.parts = int32_t(grid);
@@ -898,7 +900,7 @@ extern "C" hag_status hag_layer_norm_fwd(int64_t n, int32_t D, hag_dtype dtype, 
 
 extern "C" size_t hag_layer_norm_bwd_workspace_bytes(int64_t n, int32_t D) {
     if (n < 0 || D <= 0) return 0;
-    return size_t(D <= kMostInBlock ? kMaxParts : kParts) * 2 * size_t(D) * 4;
+    return size_t(std::max<int64_t>(std::min<int64_t>(D <= kMostInBlock ? most_parts(D) : kParts, n), 1)) * 2 * size_t(D) * 4;
 }
 
 extern "C" hag_status hag_layer_norm_bwd(int64_t n, int32_t D, hag_dtype dtype, const void *grad_y, int64_t ld_grad_y, const void *x,
