@@ -9,6 +9,11 @@ library is missing the first call raises.
     h.to_device(0)
     out = h.aggregate_fwd(x, reduce="mean")     # Algorithm 2
     gx = h.aggregate_bwd(grad_out, reduce="mean")
+
+Around the aggregation, without a handle: ``embedding_fwd`` / ``embedding_bwd``,
+``layer_norm_fwd`` / ``layer_norm_bwd``, ``graph_pool_fwd`` / ``graph_pool_bwd``,
+``clip_grad_norm`` and ``grad_norm``; ``examples/graph_classification.py`` trains
+with all of them.
 """
 from __future__ import annotations
 
@@ -649,13 +654,12 @@ def _ids(ids, index, n=None):
 def embedding_fwd(ids, table, scale=1.0, out=None, dtype=None):
     """``hag_embedding_fwd``: scale * table[ids], one row per id; an id outside the table gives a zero row.  The rows are
     of ``dtype`` (default: the table's)."""
-    import torch
     ld = _rows(table, "table")
     index, (v, d) = table.get_device(), table.shape
     id_type = _ids(ids, index)
     n = ids.shape[0]
     if out is None:
-        out = torch.empty((n, d), dtype=dtype or table.dtype, device=table.device)
+        out = table.new_empty((n, d), dtype=dtype or table.dtype)
         ld_out = d
     else:
         ld_out = _rows(out, "out", (n, d), index, dtype)
@@ -667,12 +671,11 @@ def embedding_fwd(ids, table, scale=1.0, out=None, dtype=None):
 def embedding_bwd(ids, grad_out, n_rows: int, scale=1.0, out=None, dtype=None, workspace=None):
     """``hag_embedding_bwd``: the gradient of ``embedding_fwd`` with respect to a table of n_rows rows, of ``dtype``
     (default: grad_out's)."""
-    import torch
     ld = _rows(grad_out, "grad_out")
     index, device, (n, d) = grad_out.get_device(), grad_out.device, grad_out.shape
     id_type = _ids(ids, index, n)
     if out is None:
-        out = torch.empty((n_rows, d), dtype=dtype or grad_out.dtype, device=device)
+        out = grad_out.new_empty((n_rows, d), dtype=dtype or grad_out.dtype)
         ld_out = d
     else:
         ld_out = _rows(out, "out", (n_rows, d), index, dtype)
@@ -692,13 +695,13 @@ def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None, stats=True):
     w = None if weight is None else _vector(weight, "weight", d, index)
     b = None if bias is None else _vector(bias, "bias", d, index, wdt)
     if out is None:
-        out = torch.empty((n, d), dtype=dtype, device=x.device)
+        out = x.new_empty((n, d))
         ld_out = d
     else:
         ld_out = _rows(out, "out", x.shape, index, dtype)
     mean = rstd = m = r = None
     if stats:
-        both = torch.empty((2, n), dtype=torch.float32, device=x.device)
+        both = x.new_empty((2, n), dtype=torch.float32)
         mean, rstd = both.unbind()
         m = both.data_ptr()
         r = m + 4 * n
@@ -719,14 +722,14 @@ def layer_norm_bwd(grad_out, x, mean, rstd, weight=None, out=None, param_grads=T
     wdt = weight.dtype if weight is not None else param_dtype or torch.float32
     m, r = _vector(mean, "mean", n, index, torch.float32), _vector(rstd, "rstd", n, index, torch.float32)
     if out is None:
-        out = torch.empty((n, d), dtype=dtype, device=device)
+        out = x.new_empty((n, d))
         ld_out = d
     else:
         ld_out = _rows(out, "out", shape, index, dtype)
     gw = gb = ws = gwp = gbp = None
     code = _code(wdt)
     if param_grads:
-        both = torch.empty((2, d), dtype=wdt, device=device)
+        both = x.new_empty((2, d), dtype=wdt)
         gw, gb = both.unbind()
         gwp = both.data_ptr()
         gbp = gwp + d * (4 if code == HAG_F32 else 2)
@@ -776,7 +779,7 @@ def _clip(grads, max_norm, out, workspace):
         to = array("Q", to)
     addresses, lengths, codes = array("Q", ptrs), array("q", lens), array("i", [HAG_BF16 if k is torch.bfloat16 else HAG_F32 for k in kinds])
     ws = _scratch_for(workspace, load_library().hag_clip_grad_norm_workspace_bytes(count), device)
-    norm = torch.empty((), dtype=torch.float32, device=device)
+    norm = grads[0].new_empty((), dtype=torch.float32)
     _call("hag_clip_grad_norm", index, count, addresses.buffer_info()[0], None if out is None else to.buffer_info()[0],
           lengths.buffer_info()[0], codes.buffer_info()[0], max_norm, norm.data_ptr(), ws.data_ptr())
     return out, norm
