@@ -701,9 +701,10 @@ struct TileArgs {
     int32_t D;
     float scale;
     int32_t lanes;               // per worker
-    float *partial;              // [tiles][n_rows][D], or null: one tile, whose sums are the result
+    float *partial;              // [tiles][n_rows][pitch], or null: one tile, whose sums are the result
+    int32_t pitch;               // D up to a multiple of 4: rows of a table start on 16 bytes
     int32_t parts;
-    hagr::Divisor per_row;       // D (table_join_kernel)
+    hagr::Divisor per_row;       // the pitch (table_join_kernel)
 };
 constexpr int kTileBatch = 4;    // rows in flight per worker: 32 warps of them
 
@@ -713,6 +714,23 @@ __device__ __forceinline__ void store_scalar(const TileArgs &p, int32_t row, int
     v *= p.scale;
     o.set(&v);
     o.store(static_cast<TO *>(p.out) + int64_t(row) * p.ld_out, col);
+}
+
+// A row's sum to this tile's table, or to the result.
+template <typename TO, int V>
+__device__ __forceinline__ void store_sum(const TileArgs &p, int32_t row, int vec, const float *acc) {
+    if (p.partial) {
+        hagr::Vec<float, V> o;
+        o.set(acc);
+        o.store(p.partial + (int64_t(blockIdx.x) * p.sort.n_rows + row) * p.pitch, vec);
+    } else {
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = acc[j] * p.scale;
+        hagr::Vec<TO, V> o;
+        o.set(v);
+        o.store(static_cast<TO *>(p.out) + int64_t(row) * p.ld_out, vec);
+    }
 }
 
 template <typename TG, typename TO, int V>
@@ -732,12 +750,10 @@ __global__ void __launch_bounds__(kSortThreads) embedding_tile_kernel(const __gr
         for (int k = 0; k < kSortItems; ++k)
             if (k < items) pair[k] = mine + 32 * k < len ? sort_pair(p.sort, begin + mine + 32 * k) : make_uint2(0xffffffffu, 0);
         // rows that no token of the tile names: cleared while the ids are on their way
-        const int c0 = blockIdx.y * p.lanes * V, width = min(p.D - c0, p.lanes * V);
-        for (int r = t / p.lanes; r < rows; r += kSortThreads / p.lanes)
-            for (int c = t % p.lanes; c < width; c += p.lanes) {
-                if (p.partial) p.partial[(int64_t(blockIdx.x) * rows + r) * p.D + c0 + c] = 0.0f;
-                else store_scalar<TO>(p, r, c0 + c, 0.0f);
-            }
+        const int vec = blockIdx.y * p.lanes + t % p.lanes;
+        const float zeros[V] = {};
+        if (vec < p.D / V)
+            for (int r = t / p.lanes; r < rows; r += kSortThreads / p.lanes) store_sum<TO, V>(p, r, vec, zeros);
         for (int pass = 0; pass < p.sort.passes; ++pass) {
             if (pass) {
 #pragma unroll
@@ -754,15 +770,7 @@ __global__ void __launch_bounds__(kSortThreads) embedding_tile_kernel(const __gr
     const int i0 = min(worker * stretch, len), i1 = min(i0 + stretch, len);
     const uint32_t none = 0xffffffffu;
     auto finish = [&](uint32_t key, const float *acc) {
-        if (!column || key >= uint32_t(rows)) return;
-        if (p.partial) {
-            float *to = p.partial + (int64_t(blockIdx.x) * rows + key) * p.D + int64_t(vec) * V;
-#pragma unroll
-            for (int j = 0; j < V; ++j) to[j] = acc[j];
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) store_scalar<TO>(p, int32_t(key), vec * V + j, acc[j]);
-        }
+        if (column && key < uint32_t(rows)) store_sum<TO, V>(p, int32_t(key), vec, acc);
     };
     float *head = open_rows, *tail = open_rows + kSortThreads * V;       // element j of thread t at [j][t]
     uint32_t cur = none, after = none;
@@ -837,7 +845,7 @@ __global__ void __launch_bounds__(1024) table_join_kernel(const __grid_constant_
     hagk::pdl_launch_dependents();
     __shared__ float sum[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int64_t values = int64_t(p.sort.n_rows) * p.D, i = int64_t(blockIdx.x) * 32 + lane;
+    const int64_t values = int64_t(p.sort.n_rows) * p.pitch, i = int64_t(blockIdx.x) * 32 + lane;
     hagk::pdl_wait();
     float v = 0.0f;
     if (i < values) {
@@ -849,7 +857,8 @@ __global__ void __launch_bounds__(1024) table_join_kernel(const __grid_constant_
     if (warp == 0 && i < values) {
         for (int w = 1; w < warps; ++w) v += sum[w][lane];
         const uint32_t row = hagr::quotient(uint32_t(i), p.per_row);
-        store_scalar<TO>(p, int32_t(row), int32_t(i - int64_t(row) * p.D), v);
+        const int32_t col = int32_t(i - int64_t(row) * p.pitch);
+        if (col < p.D) store_scalar<TO>(p, int32_t(row), col, v);
     }
 }
 
@@ -884,11 +893,12 @@ cudaError_t launch_tiles(TileArgs p, int tiles, cudaStream_t s) {
     p.sort.stretch = int32_t((int64_t(p.sort.n) + use - 1) / use);
     p.parts = int32_t((int64_t(p.sort.n) + p.sort.stretch - 1) / p.sort.stretch);
     if (tiles == 1) p.partial = nullptr;
-    p.per_row = hagr::make_divisor(uint32_t(p.D));
+    p.pitch = (p.D + 3) & ~3;
+    p.per_row = hagr::make_divisor(uint32_t(p.pitch));
     cudaError_t err = launch_with(embedding_tile_kernel<TG, TO, V>, dim3(unsigned(p.parts), unsigned(columns)), kSortThreads,
                                   sizeof(SortShared) + 2 * kSortThreads * V * 4, p, s);
     if (err == cudaSuccess && p.partial) {
-        const int64_t values = int64_t(p.sort.n_rows) * p.D;
+        const int64_t values = int64_t(p.sort.n_rows) * p.pitch;
         int warps = 1;
         while (warps < 32 && warps < p.parts) warps *= 2;
         err = launch_with(table_join_kernel<TO>, dim3(unsigned((values + 31) / 32)), unsigned(32 * warps), 0, p, s);
@@ -898,7 +908,7 @@ cudaError_t launch_tiles(TileArgs p, int tiles, cudaStream_t s) {
 
 template <typename TG, typename TO>
 cudaError_t launch_tiles_v(const TileArgs &p, int tiles, cudaStream_t s) {
-    const hagr::Operand ops[] = {{p.grad, p.ld_grad, int(sizeof(TG))}};
+    const hagr::Operand ops[] = {{p.grad, p.ld_grad, int(sizeof(TG))}, {tiles == 1 ? p.out : nullptr, p.ld_out, int(sizeof(TO))}};
     switch (hagr::vector_elems(16 / int(sizeof(TG)), p.D, ops)) {
         case 8: if constexpr (sizeof(TG) == 2) return launch_tiles<TG, TO, 8>(p, tiles, s);
         case 4: return launch_tiles<TG, TO, 4>(p, tiles, s);
@@ -979,7 +989,7 @@ extern "C" hag_status hag_embedding_fwd(const void *ids, hag_id_type id_type, in
 extern "C" size_t hag_embedding_bwd_workspace_bytes(int64_t n, int64_t n_rows, int32_t D) {
     if (n <= 0 || n > 0x7fffffffLL - kSortTile || n_rows < 0 || D <= 0) return 0;
     return std::max(2 * list_bytes(n) + up256(size_t(kSortMaxBlocks) * kSortBins * 4) + 2 * up256(size_t(partial_floats(n, D)) * 4),
-                    size_t(tile_count(int32_t(n), int32_t(n_rows), D)) * size_t(n_rows) * size_t(D) * 4);
+                    size_t(tile_count(int32_t(n), int32_t(n_rows), D)) * size_t(n_rows) * ((size_t(D) + 3) / 4 * 4) * 4);
 }
 
 extern "C" hag_status hag_embedding_bwd(const void *ids, hag_id_type id_type, int64_t n, int64_t n_rows, hag_dtype dtype, int32_t D,
@@ -1005,7 +1015,7 @@ extern "C" hag_status hag_embedding_bwd(const void *ids, hag_id_type id_type, in
     const SortPlan plan = sort_plan(int32_t(n), int32_t(n_rows));
     if (const int tiles = tile_count(int32_t(n), int32_t(n_rows), D)) {
         const SortArgs a{ids, id_type == HAG_ID64, int32_t(n_rows), nullptr, nullptr, nullptr, int32_t(n), 0, 0, plan.bits, plan.passes, 0, fill};
-        const TileArgs p{a, grad_out, ld_grad_out, grad_table, ld_grad_table, D, scale, 0, static_cast<float *>(workspace), 0, {}};
+        const TileArgs p{a, grad_out, ld_grad_out, grad_table, ld_grad_table, D, scale, 0, static_cast<float *>(workspace), 0, 0, {}};
         if (dtype == HAG_F32)
             err = table_dtype == HAG_F32 ? launch_tiles_v<float, float>(p, tiles, s) : launch_tiles_v<float, __nv_bfloat16>(p, tiles, s);
         else

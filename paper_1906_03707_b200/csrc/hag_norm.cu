@@ -9,6 +9,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdint>
+#include <type_traits>
 
 #include "hag.h"
 #include "hag_kernels.cuh"
@@ -162,11 +163,11 @@ __global__ void __launch_bounds__(32 * kStripRows) norm_params_any_kernel(const 
 //   L = 8, 16, 32: that many lanes of a warp per row, R rows per group at a time
 //   L = 0 or -1  : a whole block per row (of up to kMostThreads or kFewThreads threads), sums over the block through
 //                  shared memory
-// With 16-byte vectors the rows ahead are on their way into a ring of slots in shared memory (asynchronous copies, each
-// thread its own), so what is in flight does not depend on registers.  Narrower vectors (unaligned rows) are read one
-// turn ahead into registers: with 4-byte asynchronous copies 100 000 x 1433 fp32 forward takes 350 us, so 209.
-// The weights stay with the thread over all its rows: in registers, or from 16 columns per thread on in shared memory
-// (ring) or registers.
+// The rows ahead are on their way into a ring in shared memory (asynchronous copies), so what is in flight does not
+// depend on registers.  With 16-byte vectors every thread copies its own vectors into its own slots (Slots); rows that
+// do not start on 16 bytes are copied as the 16-byte pieces they touch, and the group reads its elements out of
+// those, narrow vectors at any place (Pieces).
+// The weights stay with the thread over all its rows: in registers, or from 16 columns per thread on in shared memory.
 constexpr int kMostThreads = 1024;        // of a block per row; up to kFewThreads the compiler may use 128 registers
 constexpr int kFewThreads = 512;
 // Stages of the ring.  What is in flight per SM matters more than how many warps are there: about 64 KB (one block of
@@ -176,11 +177,13 @@ constexpr int kFwdStages = 3, kBwdStages = 4, kBlockStages = 2;
 template <typename T, int V> constexpr bool kRing = V * int(sizeof(T)) == 16;
 constexpr int kWarpThreads = 256;
 template <int L> constexpr int kThreads = L == 0 ? kMostThreads : L < 0 ? kFewThreads : kWarpThreads;
+// narrow vectors keep the parameters in registers, but for the widest rows
+template <typename T, int L, int V, int K> constexpr bool kShared = V * K >= 16 && (kRing<T, V> || L == 0);
 template <typename T, int L, int V, int K, bool BWD> constexpr int kLeastBlocks = L < 0 && !BWD && kRing<T, V> ? 2 : 1;    // per SM
 // Rows per turn: 64 bytes per lane and turn (both operands of the backward pass together), but at least one row.
 constexpr int rows_per_turn(int bytes, int most) { return bytes >= 64 ? 1 : 64 / bytes < most ? 64 / bytes : most; }
 template <typename T, int L, int V, int K> constexpr int kFwdRows = L <= 0 ? 1 : kRing<T, V> ? rows_per_turn(K * V * int(sizeof(T)), 4) : V * K >= 16 ? 1 : 16 / (V * K) < 4 ? 16 / (V * K) : 4;
-template <typename T, int L, int V, int K> constexpr int kBwdRows = L > 0 && V * K <= 8 ? V * K <= 4 && kRing<T, V> ? 2 : 2 : 1;
+template <typename T, int L, int V, int K> constexpr int kBwdRows = L > 0 && V * K <= 8 ? 2 : 1;
 
 // Sums of R values per lane over the L lanes of a group: lanes trade halves of the list while it has more than one
 // value (4 sums over 32 lanes take 6 shuffles, not 20), and each lane ends with ONE of the sums: number (gl * R / L).
@@ -271,63 +274,105 @@ __device__ __forceinline__ Pairs<V> widen(const hagr::Vec<T, V> &a) {
     return f;
 }
 
-// The rows that a thread has ahead: slots in shared memory (stages x OPS matrices x R rows x K vectors; those of the
-// threads lie side by side), or one turn in registers.  THREADS is the block's size where it is fixed, else 0.
-template <typename T, int V, int K, int R, int OPS, int THREADS>
-struct Ahead {
-    static constexpr bool RING = kRing<T, V>;
-    static constexpr int kSlot = V * int(sizeof(T)), kStage = RING ? OPS * R * K * kSlot : 0;         // bytes per thread
-    hagr::Vec<T, V> next[RING ? 1 : OPS * R * K];
+// Waits until the oldest of the stages has arrived (a launch has fewer stages where a row fills the shared memory).
+__device__ __forceinline__ void wait_oldest(int stages) {
+    if (stages == 4) hagr::wait_copies<3>();
+    else if (stages == 3) hagr::wait_copies<2>();
+    else if (stages == 2) hagr::wait_copies<1>();
+    else hagr::wait_copies<0>();
+}
+
+// The rows ahead, 16-byte vectors: slots of the thread (stages x OPS matrices x R rows x K vectors; those of the threads
+// lie side by side).  THREADS is the block's size where it is fixed, else 0.
+template <typename T, int V, int K, int R, int OPS, int L, int THREADS>
+struct Slots {
+    static constexpr int kSlot = V * int(sizeof(T)), kStage = OPS * R * K * kSlot;         // bytes per thread
     char *mine;
     int write = 0, read = 0, end;                              // offsets of the stages in turn
+    int first, step, n_vec;
 
     static __device__ __forceinline__ int threads() { return THREADS ? THREADS : int(blockDim.x); }
-    __device__ __forceinline__ Ahead(char *base, int stages) : mine(base + threadIdx.x * kSlot), end(stages * kStage * threads()) {}
+    __device__ __forceinline__ Slots(char *base, const NormArgs &p, int first_, int step_)
+        : mine(base + threadIdx.x * kSlot), end(p.stages * kStage * threads()), first(first_), step(step_), n_vec(p.D / V) {}
     __device__ __forceinline__ char *slot(int stage, int op, int i, int k) const { return mine + stage + ((op * R + i) * K + k) * (threads() * kSlot); }
     // row i of the turn being issued starts at `row`; a row that does not exist is read as zeros
-    __device__ __forceinline__ void issue(int op, int i, const char *row, bool live, int first, int step, int32_t n_vec) {
+    __device__ __forceinline__ void issue(int op, int i, const char *row, bool live) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const bool column = first + k * step < n_vec;
-            if constexpr (RING) {
-                char *to = slot(write, op, i, k);
-                if (live && column) hagr::copy_async<kSlot>(to, row + int64_t(first + k * step) * kSlot);
-                else *reinterpret_cast<hagr::Words<kSlot> *>(to) = hagr::Words<kSlot>{};
-            } else {
-                hagr::Vec<T, V> &to = next[(op * R + i) * K + k];
-                to.zero();
-                if (live && column) to.template load<hagr::kOnce>(row, first + k * step);
-            }
+            char *to = slot(write, op, i, k);
+            if (live && first + k * step < n_vec) hagr::copy_async<kSlot>(to, row + int64_t(first + k * step) * kSlot);
+            else *reinterpret_cast<hagr::Words<kSlot> *>(to) = hagr::Words<kSlot>{};
         }
     }
     __device__ __forceinline__ void issued() {                 // the turn is complete
-        if constexpr (RING) {
-            hagr::commit_copies();
-            write = write + kStage * threads() == end ? 0 : write + kStage * threads();
-        }
+        hagr::commit_copies();
+        write = write + kStage * threads() == end ? 0 : write + kStage * threads();
     }
-    __device__ __forceinline__ hagr::Vec<T, V> get(int op, int i, int k) const {
-        if constexpr (RING) {
-            hagr::Vec<T, V> v;
-            v.raw = *reinterpret_cast<const hagr::Words<kSlot> *>(slot(read, op, i, k));
-            return v;
-        } else {
-            return next[(op * R + i) * K + k];
-        }
+    __device__ __forceinline__ const char *at(int op, int i, const char *) const { return slot(read, op, i, 0); }
+    __device__ __forceinline__ hagr::Vec<T, V> get(const char *row, int k) const {
+        hagr::Vec<T, V> v;
+        v.raw = *reinterpret_cast<const hagr::Words<kSlot> *>(row + k * (threads() * kSlot));
+        return v;
     }
-    __device__ __forceinline__ void done() {                   // with the oldest turn's slots
-        if constexpr (RING) read = read + kStage * threads() == end ? 0 : read + kStage * threads();
-    }
-    // until the oldest of the stages has arrived (a launch has fewer stages where a row fills the shared memory)
-    static __device__ __forceinline__ void wait(int stages) {
-        if constexpr (RING) {
-            if (stages == 4) hagr::wait_copies<3>();
-            else if (stages == 3) hagr::wait_copies<2>();
-            else if (stages == 2) hagr::wait_copies<1>();
-            else hagr::wait_copies<0>();
-        }
+    __device__ __forceinline__ void wait(int stages) const { wait_oldest(stages); }
+    template <bool BARRIER> __device__ __forceinline__ void done() {       // with the oldest turn's slots
+        read = read + kStage * threads() == end ? 0 : read + kStage * threads();
     }
 };
+
+// The rows ahead, at any alignment: per stage, matrix and row the 16-byte pieces that the row touches, and zeros up to
+// the last place that a thread looks at.  The last piece is read up to the row's end; the first one from its 16-byte
+// boundary on, which never leaves the allocation that holds the row (allocations start on 16 bytes).  The group copies
+// together, so it meets before it reads and before a stage is written again.
+template <typename T, int V, int K, int R, int OPS, int L>
+struct Pieces {
+    static constexpr int kBytes = V * int(sizeof(T));
+    char *area;                                                // of this group
+    int write = 0, read = 0, end, pitch, len;
+    int first, step;
+
+    static __host__ __device__ constexpr int row_bytes(int step) { return (K * step * kBytes + 15) / 16 * 16 + 16; }
+    __device__ __forceinline__ Pieces(char *base, const NormArgs &p, int first_, int step_)
+        : pitch(row_bytes(step_)), len(p.D * int(sizeof(T))), first(first_), step(step_) {
+        end = p.stages * (OPS * R) * pitch;
+        area = base + (L > 0 ? int(threadIdx.x >> 5) * end : 0);
+    }
+    __device__ __forceinline__ void issue(int op, int i, const char *row, bool live) {
+        const int off = int(uint32_t(reinterpret_cast<uintptr_t>(row)) & 15u), bytes = live ? off + len : 0;
+        char *to = area + write + (op * R + i) * pitch;
+        const char *from = row - off;
+        for (int c = first * 16; c < pitch; c += step * 16) {
+            const int here = min(16, bytes - c);
+            hagr::copy_async_part(to + c, from + (here > 0 ? c : 0), max(here, 0));
+        }
+    }
+    __device__ __forceinline__ void issued() {
+        hagr::commit_copies();
+        write = write + OPS * R * pitch == end ? 0 : write + OPS * R * pitch;
+    }
+    // where this thread's part of row i, which started at `row`, lies, and vector k of it
+    __device__ __forceinline__ const char *at(int op, int i, const char *row) const {
+        return area + read + (op * R + i) * pitch + (uint32_t(reinterpret_cast<uintptr_t>(row)) & 15u) + first * kBytes;
+    }
+    __device__ __forceinline__ hagr::Vec<T, V> get(const char *row, int k) const {
+        hagr::Vec<T, V> v;
+        v.raw = *reinterpret_cast<const hagr::Words<kBytes> *>(row + k * step * kBytes);
+        return v;
+    }
+    __device__ __forceinline__ void wait(int n) const {
+        wait_oldest(n);
+        if (L > 0) __syncwarp(); else __syncthreads();
+    }
+    // BARRIER: the threads of a block have not met since they read
+    template <bool BARRIER> __device__ __forceinline__ void done() {
+        if (L > 0) __syncwarp();
+        else if (BARRIER) __syncthreads();
+        read = read + OPS * R * pitch == end ? 0 : read + OPS * R * pitch;
+    }
+};
+
+template <typename T, int V, int K, int R, int OPS, int L>
+using Ahead = std::conditional_t<kRing<T, V>, Slots<T, V, K, R, OPS, L, (L > 0 ? kThreads<L> : 0)>, Pieces<T, V, K, R, OPS, L>>;
 
 // The rows of a group of threads: R at a time, `stride` rows from one turn to the next.
 template <int L, int R>
@@ -354,9 +399,9 @@ struct Turns {
 
 // Parameters of a thread's columns, N vectors of them (weights, or weights and biases), in registers or in shared
 // memory in planes of up to four columns (so that neighbours read neighbouring words).
-template <int V, int K, int N, bool RING>
+template <int V, int K, int N, bool SHARED>
 struct Params {
-    static constexpr bool kShared = RING && V * K >= 16;
+    static constexpr bool kShared = SHARED;
     static constexpr int W = V < 4 ? V : 4;
     struct alignas(4 * W) Piece { float v[W]; };
     float own[kShared ? 1 : N * K * V];
@@ -455,15 +500,15 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, false>)
     const int lane = threadIdx.x & 31, first = turns.first, step = turns.step;
     const int32_t n_vec = p.D / V;
     const float cols = float(p.D), inverse = 1.0f / cols;
-    Params<V, K, 2, kRing<T, V>> wb(raw, first, step);
-    Ahead<T, V, K, R, 1, (L > 0 ? kThreads<L> : 0)> ahead(raw + Params<V, K, 2, kRing<T, V>>::bytes(step), p.stages);
+    Params<V, K, 2, kShared<T, L, V, K>> wb(raw, first, step);
+    Ahead<T, V, K, R, 1, L> ahead(raw + Params<V, K, 2, kShared<T, L, V, K>>::bytes(step), p, first, step);
     const int64_t ld_x = p.ld_x * int64_t(sizeof(T)), ld_y = p.ld_y * int64_t(sizeof(T));
-    const char *x_next = static_cast<const char *>(p.x) + turns.row * ld_x;
+    const char *x_next = static_cast<const char *>(p.x) + turns.row * ld_x, *x_row = x_next;
     char *y = static_cast<char *>(p.y) + turns.row * ld_y;
     const int64_t step_x = turns.stride * ld_x, step_y = turns.stride * ld_y;
     auto issue = [&](int32_t turn) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) ahead.issue(0, i, x_next + i * ld_x, turn < turns.live[i], first, step, n_vec);
+        for (int i = 0; i < R; ++i) ahead.issue(0, i, x_next + i * ld_x, turn < turns.live[i]);
         ahead.issued();
         x_next += step_x;
     };
@@ -480,15 +525,17 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, false>)
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             s[i] = 0.0f;
+            const char *row = ahead.at(0, i, x_row + i * ld_x);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                x[i][k] = widen(ahead.get(0, i, k));
+                x[i][k] = widen(ahead.get(row, k));
                 s[i] += x[i][k].sum();                         // places beyond the row hold zeros
             }
         }
-        ahead.done();
-        issue(turn + p.stages);                                // into the slots just read
         const float my_mean = group_sums<L, R>(s, first, slots[0]) / cols;     // a division: constant rows give exact zeros
+        ahead.template done<false>();
+        issue(turn + p.stages);                                // into the stage just read
+        x_row += step_x;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const float mean = L <= 0 ? my_mean : spread_get<L <= 0 ? 32 : L, R>(my_mean, i, lane);
@@ -532,22 +579,22 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
     __shared__ float2 slots[2][32];
     constexpr int R = kBwdRows<T, L, V, K>, S = L <= 0 ? 32 : L;
     constexpr bool HOLD = L != 0 && R * K * V <= 16;                     // keep xh and g * w between their two uses
-    constexpr bool RAW = !HOLD && !kRing<T, V>;                // keep the raw row (the ring still has it)
     const Turns<L, R> turns(p.n);
     const int lane = threadIdx.x & 31, first = turns.first, step = turns.step;
     const int32_t n_vec = p.D / V;
     const float inverse = 1.0f / float(p.D);
-    Params<V, K, 1, kRing<T, V>> weights(raw, first, step);
-    Ahead<T, V, K, R, 2, (L > 0 ? kThreads<L> : 0)> ahead(raw + Params<V, K, 1, kRing<T, V>>::bytes(step), p.stages);
+    Params<V, K, 1, kShared<T, L, V, K>> weights(raw, first, step);
+    Ahead<T, V, K, R, 2, L> ahead(raw + Params<V, K, 1, kShared<T, L, V, K>>::bytes(step), p, first, step);
     const int64_t ld_x = p.ld_x * int64_t(sizeof(T)), ld_g = p.ld_g * int64_t(sizeof(T)), ld_y = p.ld_y * int64_t(sizeof(T));
     const char *x_next = static_cast<const char *>(p.x) + turns.row * ld_x, *g_next = static_cast<const char *>(p.g) + turns.row * ld_g;
+    const char *x_row = x_next, *g_row = g_next;               // of the turn being worked on
     char *y = static_cast<char *>(p.y) + turns.row * ld_y;
     const int64_t step_x = turns.stride * ld_x, step_g = turns.stride * ld_g, step_y = turns.stride * ld_y;
     auto issue = [&](int32_t turn) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            ahead.issue(0, i, x_next + i * ld_x, turn < turns.live[i], first, step, n_vec);
-            ahead.issue(1, i, g_next + i * ld_g, turn < turns.live[i], first, step, n_vec);
+            ahead.issue(0, i, x_next + i * ld_x, turn < turns.live[i]);
+            ahead.issue(1, i, g_next + i * ld_g, turn < turns.live[i]);
         }
         ahead.issued();
         x_next += step_x;
@@ -586,7 +633,6 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
             statistics(turn + S);
         }
         ahead.wait(p.stages);
-        hagr::Vec<T, V> rx[RAW ? R * K : 1], rg[RAW ? R * K : 1];
         Pairs<V> xh[R][K], gw[R][K];
         float m[R], q[R], s[2 * R];
         // where the thread is beyond the row g is zero and its terms vanish
@@ -595,14 +641,10 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
             m[i] = __shfl_sync(0xffffffffu, mean[i], (lane & ~(S - 1)) + turn % S);
             q[i] = __shfl_sync(0xffffffffu, rstd[i], (lane & ~(S - 1)) + turn % S);
             s[2 * i] = s[2 * i + 1] = 0.0f;
+            const char *xs = ahead.at(0, i, x_row + i * ld_x), *gs = ahead.at(1, i, g_row + i * ld_g);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const hagr::Vec<T, V> vx = ahead.get(0, i, k), vg = ahead.get(1, i, k);
-                if (RAW) {
-                    rx[RAW ? i * K + k : 0] = vx;
-                    rg[RAW ? i * K + k : 0] = vg;
-                }
-                Pairs<V> a = widen(vx), t = widen(vg);
+                Pairs<V> a = widen(ahead.get(xs, k)), t = widen(ahead.get(gs, k));
                 a.shift_scale(-m[i], q[i]);
                 ab[k].add(t);
                 aw[k].fma(t, a);
@@ -614,10 +656,6 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
                     gw[i][k] = t;
                 }
             }
-        }
-        if (HOLD || RAW) {
-            ahead.done();
-            issue(turn + p.stages);
         }
         float s1[R], s2[R];
         if constexpr (L <= 0) {
@@ -632,9 +670,14 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
                 s2[i] = spread_get<L, 2 * R>(mine, 2 * i + 1, lane);
             }
         }
+        if (HOLD) {
+            ahead.template done<false>();
+            issue(turn + p.stages);
+        }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const bool live = turn < turns.live[i];
+            const char *xs = ahead.at(0, i, x_row + i * ld_x), *gs = ahead.at(1, i, g_row + i * ld_g);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 Pairs<V> a, t;
@@ -642,8 +685,8 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
                     a = xh[i][k];
                     t = gw[i][k];
                 } else {
-                    a = widen(RAW ? rx[RAW ? i * K + k : 0] : ahead.get(0, i, k));
-                    t = widen(RAW ? rg[RAW ? i * K + k : 0] : ahead.get(1, i, k));
+                    a = widen(ahead.get(xs, k));
+                    t = widen(ahead.get(gs, k));
                     a.shift_scale(-m[i], q[i]);
                     t.mul(weights.get(0, k));
                 }
@@ -655,10 +698,12 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
                 if (live && first + k * step < n_vec) o.store(y + i * ld_y, first + k * step);
             }
         }
-        if (!HOLD && !RAW) {
-            ahead.done();
+        if (!HOLD) {
+            ahead.template done<true>();
             issue(turn + p.stages);
         }
+        x_row += step_x;
+        g_row += step_g;
         y += step_y;
     }
     hagr::wait_copies<0>();
@@ -750,8 +795,8 @@ cudaError_t launch(void (*kernel)(NormArgs), dim3 grid, unsigned threads, size_t
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-// Parts of gw and gb, i.e. blocks of the other kernels, at most: wide rows take a block's registers to themselves.
-int most_parts(int32_t D) { return kSms * std::max(1, std::min(8, 8192 / D)); }
+// Parts of gw and gb, i.e. blocks of the other kernels, at most: the wider the rows, the fewer blocks fit an SM.
+int most_parts(int32_t D) { return kSms * std::max(1, std::min(8, 16384 / D)); }
 
 // How many blocks of the kernel the device runs at once (asked once per kernel and block size).
 int resident_blocks(void (*kernel)(NormArgs), unsigned threads, size_t shared) {
@@ -783,12 +828,13 @@ cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
     cudaError_t err = allow_shared<kernel>();
     if (err != cudaSuccess) return err;
     const int threads = L <= 0 ? ((p.D / V + K - 1) / K + 31) / 32 * 32 : kThreads<L>;
-    const size_t params = Params<V, K, BWD ? 1 : 2, kRing<T, V>>::bytes(L <= 0 ? threads : L);
-    const size_t stage = size_t(Ahead<T, V, K, R, OPS, 0>::kStage) * threads;
+    const size_t params = Params<V, K, BWD ? 1 : 2, kShared<T, L, V, K>>::bytes(L <= 0 ? threads : L);
+    size_t stage;
+    if constexpr (kRing<T, V>) stage = size_t(Ahead<T, V, K, R, OPS, L>::kStage) * threads;
+    else stage = size_t(OPS) * R * Ahead<T, V, K, R, OPS, L>::row_bytes(L > 0 ? 32 : threads) * (L > 0 ? threads / 32 : 1);
     // as many stages as leave room for the blocks that the registers allow
-    const int blocks = L <= 0 ? std::max(1, std::min(8, 768 / threads)) : BWD ? 2 : 1;
+    const int blocks = L <= 0 ? std::max(1, std::min(8, 768 / threads)) : BWD || !kRing<T, V> ? 2 : 1;
     p.stages = L <= 0 ? kBlockStages : BWD ? kBwdStages : kFwdStages;
-    if (!kRing<T, V>) p.stages = 1;
     while (p.stages > 1 && (params + p.stages * stage + 1024) * blocks > size_t(kSmShared)) --p.stages;
     size_t shared = params + p.stages * stage;
     if (BWD && L > 0) shared = std::max(shared, size_t(threads / 32) * 2 * (L > 0 ? L : 0) * K * V * 4);
@@ -815,8 +861,7 @@ cudaError_t launch_width(NormArgs &p, cudaStream_t s) {
     }
     if (n_vec <= 32) return launch_rows<T, V, 32, 1, BWD>(p, s);
     if (n_vec <= 64) return launch_rows<T, V, 32, 2, BWD>(p, s);
-    // vectors per lane of a warp; narrow vectors of the backward pass: 8 columns per thread (300 000 x 333 bf16 takes
-    // 249 us, with 16 columns 600: too many registers), of the forward pass 16 (138 us, with 8 215)
+    // vectors per lane of a warp; narrow vectors of the backward pass: 8 columns per thread (with 16 too many registers)
     constexpr int kMost = (kRing<T, V> ? 32 : BWD ? 8 : 16) / V;
     if constexpr (kMost >= 4)
         if (n_vec <= 128) return launch_rows<T, V, 32, 4, BWD>(p, s);
