@@ -19,6 +19,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 
 import numpy as np
 
@@ -575,13 +576,24 @@ def graph_pool_bwd(seg_ptr, grad_out, n_rows: int, reduce="mean", out=None):
 
 # -- around the aggregation: embedding, layer norm, clipping by the global norm -------------------------------------- #
 # Small graphs make these calls a matter of host time: each check below is one cheap attribute of the tensor.
-def _code(dtype) -> int:
+_codes = {}          # torch type -> hag_dtype / hag_id_type; filled with the first call, which imports torch
+_id_codes = {}
+
+
+def _runtime():
     import torch
-    if dtype is torch.float32:
-        return HAG_F32
-    if dtype is torch.bfloat16:
-        return HAG_BF16
-    raise TypeError(f"values must be float32 or bfloat16, got {dtype}")
+    load_library()
+    _codes.update({torch.float32: HAG_F32, torch.bfloat16: HAG_BF16})
+    _id_codes.update({torch.int64: HAG_ID64, torch.int32: HAG_ID32})
+
+
+def _code(dtype) -> int:
+    if not _codes:
+        _runtime()
+    code = _codes.get(dtype)
+    if code is None:
+        raise TypeError(f"values must be float32 or bfloat16, got {dtype}")
+    return code
 
 
 def _rows(t, what, like=None, index=None, dtype=None):
@@ -621,34 +633,32 @@ def _scratch_for(workspace, need, device):
 def _call(name, index, *args):
     """One C call on the current stream of device `index`."""
     import torch
-    fn = getattr(_lib or load_library(), name)
+    fn = getattr(_lib, name)
     if torch.cuda.current_device() == index:
-        st = fn(*args, _stream(index))
+        st = fn(*args, _stream(torch, index))
     else:
         with torch.cuda.device(index):
-            st = fn(*args, _stream(index))
+            st = fn(*args, _stream(torch, index))
     if st != 0:
         _check(st, name)
 
 
-def _stream(index):
+def _stream(torch, index):
     """The current stream's handle: what torch.cuda.current_stream(index).cuda_stream gives, without the Stream object
     (1.3 us of a call's 10)."""
-    import torch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 def _ids(ids, index, n=None):
-    import torch
     if ids.dim() != 1 or not ids.is_contiguous() or ids.get_device() != index or (n is not None and ids.shape[0] != n):
         raise ValueError(f"ids must be a contiguous 1-D tensor{'' if n is None else f' of {n} values'} on cuda:{index}")
-    dtype = ids.dtype
-    if dtype is torch.int64:
-        return HAG_ID64
-    if dtype is torch.int32:
-        return HAG_ID32
-    raise TypeError(f"ids must be int32 or int64, got {dtype}")
+    if not _id_codes:
+        _runtime()
+    code = _id_codes.get(ids.dtype)
+    if code is None:
+        raise TypeError(f"ids must be int32 or int64, got {ids.dtype}")
+    return code
 
 
 def embedding_fwd(ids, table, scale=1.0, out=None, dtype=None):
@@ -764,7 +774,6 @@ def grad_norm(grads, workspace=None):
 
 def _clip(grads, max_norm, out, workspace):
     import torch
-    from array import array
     if not grads or not grads[0].is_cuda:
         raise ValueError("gradients must be a list of device tensors, not empty")
     device, index, count = grads[0].device, grads[0].get_device(), len(grads)
@@ -773,11 +782,11 @@ def _clip(grads, max_norm, out, workspace):
         to, to_lens, to_kinds = (ptrs, lens, kinds) if out is grads else _tensor_list(out, index)
         if to_lens != lens or to_kinds != kinds:
             raise ValueError("out must be tensors with the lengths and types of the gradients")
-        for addresses in (ptrs, to):
-            if len(set(addresses)) != count and len({p for p, m in zip(addresses, lens) if m}) != sum(m > 0 for m in lens):
+        for at in (ptrs, to):
+            if len(set(at)) != count and len({p for p, m in zip(at, lens) if m}) != sum(m > 0 for m in lens):
                 raise ValueError("a tensor is named twice")
         to = array("Q", to)
-    addresses, lengths, codes = array("Q", ptrs), array("q", lens), array("i", [HAG_BF16 if k is torch.bfloat16 else HAG_F32 for k in kinds])
+    addresses, lengths, codes = array("Q", ptrs), array("q", lens), array("i", [_codes[k] for k in kinds])
     ws = _scratch_for(workspace, load_library().hag_clip_grad_norm_workspace_bytes(count), device)
     norm = grads[0].new_empty((), dtype=torch.float32)
     _call("hag_clip_grad_norm", index, count, addresses.buffer_info()[0], None if out is None else to.buffer_info()[0],
