@@ -3,6 +3,7 @@
 // Two launches: every block sums the squares of its pieces of the list; then every block adds up those sums (the
 // same order everywhere: the same bits everywhere) and scales its pieces.  The list travels as a kernel parameter,
 // so no descriptor is copied to the device first and the calls can be captured in a graph.
+#include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -23,6 +24,7 @@ constexpr int kClipBlocks = 148 * 4;
 // 664 MB: 322 us, with 16 KB pieces 347); short ones 8 KB, which more SMs share.
 constexpr int kLoadsLong = 8, kLoadsShort = 2;
 constexpr int64_t kShortList = 8 << 20;        // bytes
+constexpr int64_t kClusterList = 256 << 10;    // a list for one cluster
 __host__ __device__ constexpr int piece_bytes(int loads) { return kClipThreads * 16 * loads; }
 
 struct ClipArgs {
@@ -31,6 +33,7 @@ struct ClipArgs {
     double *sums;                              // [launches][kClipBlocks]
     int32_t first_sum, n_sums;                 // where this launch's blocks put theirs; how many there are in all
     float max_norm;
+    int32_t scales;                            // clip_cluster_kernel: whether there are outputs
     float *norm;
     const void *in[kClipList];
     void *out[kClipList];
@@ -142,18 +145,25 @@ __device__ __forceinline__ void piece_scale(const void *in, void *out, int64_t b
     }
 }
 
+// Squares are added in fp32 within a piece, in fp64 from piece to piece.
 template <int U>
-__global__ void __launch_bounds__(kClipThreads, 2) norm_sums_kernel(const __grid_constant__ ClipArgs p) {
-    hagk::pdl_launch_dependents();
-    __shared__ double slot[kClipThreads / 32];
-    double s = 0.0;       // squares are added in fp32 within a piece, in fp64 from piece to piece
-    hagk::pdl_wait();
+__device__ __forceinline__ double piece_sums(const ClipArgs &p) {
+    double s = 0.0;
     for_pieces<U, false>(p, [&](int t, int64_t b, int64_t e) {
         if (p.bf16[t])
             s += p.vec[t] ? piece_squares<__nv_bfloat16, 8, U>(p.in[t], b, e) : piece_squares<__nv_bfloat16, 1, U>(p.in[t], b, e);
         else
             s += p.vec[t] ? piece_squares<float, 4, U>(p.in[t], b, e) : piece_squares<float, 1, U>(p.in[t], b, e);
     });
+    return s;
+}
+
+template <int U>
+__global__ void __launch_bounds__(kClipThreads, 2) norm_sums_kernel(const __grid_constant__ ClipArgs p) {
+    hagk::pdl_launch_dependents();
+    __shared__ double slot[kClipThreads / 32];
+    hagk::pdl_wait();
+    double s = piece_sums<U>(p);
     s = block_sum(s, slot);
     if (threadIdx.x == 0) p.sums[p.first_sum + blockIdx.x] = s;
 }
@@ -173,13 +183,9 @@ __global__ void __launch_bounds__(kClipThreads) norm_join_kernel(const __grid_co
     if (threadIdx.x == 0 && p.norm) *p.norm = norm;
 }
 
+// The pieces of this block times the factor.
 template <int U>
-__global__ void __launch_bounds__(kClipThreads, 2) clip_scale_kernel(const __grid_constant__ ClipArgs p) {
-    hagk::pdl_launch_dependents();
-    __shared__ double slot[kClipThreads / 32];
-    hagk::pdl_wait();
-    const float norm = total_norm(p, slot);
-    if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
+__device__ __forceinline__ void scale_pieces(const ClipArgs &p, float norm) {
     const float ratio = p.max_norm / (norm + 1e-6f);
     const float c = ratio >= 1.0f ? 1.0f : ratio;          // a norm that is no number gives a factor that is none
     // backwards: what the first launch read last is still in the L2
@@ -193,6 +199,38 @@ __global__ void __launch_bounds__(kClipThreads, 2) clip_scale_kernel(const __gri
             else piece_scale<float, 1, U>(p.in[t], p.out[t], b, e, c);
         }
     });
+}
+
+template <int U>
+__global__ void __launch_bounds__(kClipThreads, 2) clip_scale_kernel(const __grid_constant__ ClipArgs p) {
+    hagk::pdl_launch_dependents();
+    __shared__ double slot[kClipThreads / 32];
+    hagk::pdl_wait();
+    const float norm = total_norm(p, slot);
+    if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
+    scale_pieces<U>(p, norm);
+}
+
+// Short lists in one launch: a cluster of blocks exchanges its sums through shared memory.  Its barrier is the
+// hardware's, so nothing waits in a loop.
+constexpr int kCluster = 8;
+__global__ void __launch_bounds__(kClipThreads, 2) __cluster_dims__(kCluster, 1, 1) clip_cluster_kernel(const __grid_constant__ ClipArgs p) {
+    hagk::pdl_launch_dependents();
+    namespace cg = cooperative_groups;
+    __shared__ double slot[kClipThreads / 32], mine;
+    cg::cluster_group cluster = cg::this_cluster();
+    hagk::pdl_wait();
+    double s = piece_sums<kLoadsLong>(p);
+    s = block_sum(s, slot);
+    if (threadIdx.x == 0) mine = s;
+    cluster.sync();
+    s = 0.0;
+#pragma unroll
+    for (unsigned b = 0; b < kCluster; ++b) s += *cluster.map_shared_rank(&mine, b);
+    cluster.sync();                                        // no block leaves while another reads its sum
+    const float norm = float(sqrt(s));
+    if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
+    if (p.scales) scale_pieces<kLoadsLong>(p, norm);
 }
 
 int launches_of(int32_t count) { return std::max(1, (count + kClipList - 1) / kClipList); }
@@ -246,7 +284,9 @@ extern "C" hag_status hag_clip_grad_norm(int32_t count, const void *const *grads
     if (!workspace) return HAG_ERR_WORKSPACE;
     if (!hagl::aligned16(workspace)) return HAG_ERR_ALIGN;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    const int launches = launches_of(count), loads = bytes < kShortList ? kLoadsShort : kLoadsLong;
+    const int launches = launches_of(count);
+    const bool cluster = launches == 1 && bytes <= kClusterList;
+    const int loads = bytes < kShortList && !cluster ? kLoadsShort : kLoadsLong;
     void (*const sum)(ClipArgs) = loads == kLoadsShort ? norm_sums_kernel<kLoadsShort> : norm_sums_kernel<kLoadsLong>;
     void (*const scale)(ClipArgs) = loads == kLoadsShort ? clip_scale_kernel<kLoadsShort> : clip_scale_kernel<kLoadsLong>;
     ClipArgs p{};
@@ -255,6 +295,13 @@ extern "C" hag_status hag_clip_grad_norm(int32_t count, const void *const *grads
     for (int k = 0; k < launches; ++k)      // before the first launch: an error leaves everything as it was
         if (!fill(p, k, loads, count, grads, out, lengths, dtypes)) return HAG_ERR_TOO_LARGE;
     cudaError_t err = cudaSuccess;
+    if (cluster) {
+        p.norm = total_norm;
+        p.scales = out != nullptr;
+        err = hagl::launch_pdl<ClipArgs>(clip_cluster_kernel, unsigned(kCluster), unsigned(kClipThreads), p, s);
+        if (err != cudaSuccess) { cudaGetLastError(); return HAG_ERR_CUDA; }
+        return HAG_OK;
+    }
     int32_t sums = 0;
     for (int k = 0; k < launches && err == cudaSuccess; ++k) {
         if (launches > 1) fill(p, k, loads, count, grads, out, lengths, dtypes);

@@ -572,6 +572,12 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, false>)
     hagr::wait_copies<0>();
 }
 
+// A block's sum for column c of gw (0) or gb (1): a part of it, or, from the only block, the result.
+__device__ __forceinline__ void leave_param(const NormArgs &p, int which, int32_t c, float v) {
+    if (p.parts > 1) p.partial[(int64_t(blockIdx.x) * 2 + which) * p.D + c] = v;
+    else if (void *to = which ? p.gb : p.gw) store_param(to, p.w_bf16, c, v);
+}
+
 template <typename T, int V, int L, int K>
 __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>)) norm_bwd_kernel(const NormArgs p) {
     hagk::pdl_launch_dependents();
@@ -715,8 +721,8 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
             for (int j = 0; j < V; ++j) {
                 const int32_t c = (first + k * step) * V + j;
                 if (c >= p.D) continue;
-                p.partial[int64_t(blockIdx.x) * 2 * p.D + c] = aw[k].v[j];
-                p.partial[(int64_t(blockIdx.x) * 2 + 1) * p.D + c] = ab[k].v[j];
+                leave_param(p, 0, c, aw[k].v[j]);
+                leave_param(p, 1, c, ab[k].v[j]);
             }
     } else {
         // groups of the warp, then warps of the block, in a fixed order
@@ -748,7 +754,7 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
             float v = 0.0f;
 #pragma unroll
             for (int w = 0; w < kThreads<L> / 32; ++w) v += joined[w * 2 * C + c];
-            p.partial[(int64_t(blockIdx.x) * 2 + which) * p.D + col] = v;
+            leave_param(p, which, col, v);
         }
     }
 }
@@ -808,6 +814,10 @@ int resident_blocks(void (*kernel)(NormArgs), unsigned threads, size_t shared) {
     return per_sm * kSms;
 }
 
+// Values of a gradient that one block takes alone: 34 x 64 2.8 us, two launches 5; 64 x 1024 would be 15 us, two
+// launches 8.
+constexpr int64_t kFewValues = 16384;
+
 // Lets a kernel use all the shared memory of the current device's SMs (once per kernel and device).
 template <auto KERNEL>
 cudaError_t allow_shared() {
@@ -844,7 +854,9 @@ cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
     if (most == 0) resident[threads / 32].store(most = resident_blocks(kernel, threads, shared), std::memory_order_relaxed);
     most = std::min(most, kRing<T, V> && L > 0 ? kSms * (BWD ? 2 : 1) : most_parts(p.D));
     const int64_t rows_per_block = L <= 0 ? 1 : int64_t(threads / 32) * (32 / (L <= 0 ? 32 : L)) * R;
-    const int64_t grid = std::max<int64_t>(1, std::min<int64_t>((p.n + rows_per_block - 1) / rows_per_block, most));
+    int64_t grid = std::max<int64_t>(1, std::min<int64_t>((p.n + rows_per_block - 1) / rows_per_block, most));
+    // few rows: one block does without the second launch
+    if (BWD && L > 0 && p.partial && p.n * p.D <= kFewValues) grid = 1;
     p.parts = int32_t(grid);
     return launch(kernel, dim3(unsigned(grid)), unsigned(threads), shared, p, s);
 }
@@ -972,7 +984,7 @@ extern "C" hag_status hag_layer_norm_bwd(int64_t n, int32_t D, hag_dtype dtype, 
     if (!params) p.partial = nullptr;
     if (D <= kMostInBlock) {
         if (n > 0 || params) err = f32 ? launch_typed<float, true>(p, s) : launch_typed<__nv_bfloat16, true>(p, s);
-        if (params && err == cudaSuccess) err = launch(norm_params_join_kernel, join_grid, 32 * kJoinWarps, 0, p, s);
+        if (params && p.parts > 1 && err == cudaSuccess) err = launch(norm_params_join_kernel, join_grid, 32 * kJoinWarps, 0, p, s);
     } else {
         if (params) {      // first: grad_x may take the place of grad_y or x
             p.parts = int(std::min<int64_t>(std::max<int64_t>((n + kStripRows - 1) / kStripRows, 1), kParts));
