@@ -463,7 +463,8 @@ hag_status hag_test_fail_allocation(int32_t kind, int32_t countdown);
  * These calls have no handle: device pointers, sizes and a stream, on the current device, no allocation.  Unlike the
  * aggregation they take any width D, row strides and element-aligned pointers; the widest loads that the
  * width, the strides and the pointers allow are used (16 bytes where D, the strides and the pointers are multiples
- * of 16 bytes).  `ld_*` is the distance between the starts of consecutive rows in elements: at least D for what is
+ * of 16 bytes; elsewhere a row may be read from the 16-byte boundary before it on, which lies in its own allocation).
+ * `ld_*` is the distance between the starts of consecutive rows in elements: at least D for what is
  * written (unless it has one row), any value >= 0 for what is read (0: the same row every time).  Sums and statistics
  * are fp32, or fp64 where said; each result is rounded once, when it is stored.  No floating-point atomics and a
  * fixed order of additions: the same inputs give the same bits.  Matrices that are written must not overlap anything

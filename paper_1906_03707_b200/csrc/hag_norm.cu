@@ -4,6 +4,12 @@
 //             gw = sum over rows of g * xh,  gb = sum over rows of g
 // The variance is the mean of squared differences from the mean (two steps over the row, never
 // E[x^2] - mu^2, which cancels when the mean is large against the spread).
+//
+// Both directions are bound by memory: a row is read once (x, and g backward) and written once.  Measured on B200
+// against a copy at 6.45 TB/s: forward 233 000 x 128 fp32 40 us (5.96 TB/s), 10^6 x 256 bf16 160 us (6.45), 32 768 x 4096
+// bf16 102 us (5.3); backward with both parameter gradients 10^6 x 256 bf16 232 us in isolation (6.65) and 260 us in a long
+// run (5.9), 200 000 x 512 fp32 206 us (6.0).  Rows of odd widths take narrower loads and stores: 300 000 x 333 fp32
+// forward 173 us (4.6), bf16 169 us (2.4).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -69,7 +75,8 @@ __device__ __forceinline__ float block_sum(float v, float *slot) {
     return s;
 }
 
-// Rows of any width: one block per row, which it reads three times (the second and third time out of the caches).
+// Rows of more than kMostInBlock columns: one block per row, which it reads three times (the second and third time out
+// of the caches).
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) norm_fwd_any_kernel(const NormArgs p) {
     hagk::pdl_launch_dependents();
@@ -338,12 +345,16 @@ struct Pieces {
         area = base + (L > 0 ? int(threadIdx.x >> 5) * end : 0);
     }
     __device__ __forceinline__ void issue(int op, int i, const char *row, bool live) {
-        const int off = int(uint32_t(reinterpret_cast<uintptr_t>(row)) & 15u), bytes = live ? off + len : 0;
         char *to = area + write + (op * R + i) * pitch;
-        const char *from = row - off;
-        for (int c = first * 16; c < pitch; c += step * 16) {
-            const int here = min(16, bytes - c);
-            hagr::copy_async_part(to + c, from + (here > 0 ? c : 0), max(here, 0));
+        if (live) {
+            const int off = int(uint32_t(reinterpret_cast<uintptr_t>(row)) & 15u), bytes = off + len;
+            const char *from = row - off;
+            for (int c = first * 16; c < pitch; c += step * 16) {      // behind the row: copies of no bytes, i.e. zeros
+                const int here = min(16, bytes - c);
+                hagr::copy_async_part(to + c, from + (here > 0 ? c : 0), max(here, 0));
+            }
+        } else {
+            for (int c = first * 16; c < pitch; c += step * 16) *reinterpret_cast<uint4 *>(to + c) = make_uint4(0, 0, 0, 0);
         }
     }
     __device__ __forceinline__ void issued() {
@@ -855,14 +866,15 @@ cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
     most = std::min(most, kRing<T, V> && L > 0 ? kSms * (BWD ? 2 : 1) : most_parts(p.D));
     const int64_t rows_per_block = L <= 0 ? 1 : int64_t(threads / 32) * (32 / (L <= 0 ? 32 : L)) * R;
     int64_t grid = std::max<int64_t>(1, std::min<int64_t>((p.n + rows_per_block - 1) / rows_per_block, most));
-    // few rows: one block does without the second launch
+    // one block does without the second launch
     if (BWD && L > 0 && p.partial && p.n * p.D <= kFewValues) grid = 1;
     p.parts = int32_t(grid);
     return launch(kernel, dim3(unsigned(grid)), unsigned(threads), shared, p, s);
 }
 
-// Rows of up to 1024 elements (narrow vectors: 512) go to a warp or a part of one, rows of up to 1024 * kPerThread to
-// a block.
+// Rows of up to 1024 elements (narrow vectors: 512 forward, 256 backward) go to a warp or a part of one, rows of up to
+// 1024 * kPerThread to a block.  A warp needs no barrier: 65 536 x 1024 bf16 forward takes 54 us with a warp per row and
+// 96 with a block of 64 threads.
 constexpr int kPerThread = 16;
 template <typename T, int V, bool BWD>
 cudaError_t launch_width(NormArgs &p, cudaStream_t s) {

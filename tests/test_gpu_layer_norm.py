@@ -199,6 +199,16 @@ def test_runs_repeat_and_no_rows():
     assert gx.shape == (0, 100) and not gw.any() and not gb.any()
 
 
+@pytest.mark.parametrize("d", [1, 7, 100, 333, 1433, 9001])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_no_rows_of_any_width(d, dtype):
+    empty, w, none = torch.empty(0, d, device="cuda", dtype=dtype), _randn(31, d), torch.empty(0, device="cuda")
+    y, m, r = hb.layer_norm_fwd(empty, w)
+    assert y.shape == (0, d) and m.shape == (0,)
+    gx, gw, gb = hb.layer_norm_bwd(empty, empty, none, none, w)
+    assert gx.shape == (0, d) and not gw.any() and not gb.any()
+
+
 def test_one_of_the_parameter_gradients():
     lib, vp = hb.load_library(), ctypes.c_void_p
     x, g, w = _randn(24, 500, 72), _randn(25, 500, 72), _randn(26, 72)
