@@ -3,6 +3,10 @@
 // Two launches: every block sums the squares of its pieces of the list; then every block adds up those sums (the
 // same order everywhere: the same bits everywhere) and scales its pieces.  The list travels as a kernel parameter,
 // so no descriptor is copied to the device first and the calls can be captured in a graph.
+//
+// Bound by memory: the list is read twice and written once, but for what is still in the L2 the second time.  Measured
+// on B200: 40 tensors of 664 MB 322 us (6.2 TB/s over the three), 20 tensors of 80 MB 40 us, 12 tensors of 0.2 MB in one
+// launch 6.7 us.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -24,7 +28,9 @@ constexpr int kClipBlocks = 148 * 4;
 // 664 MB: 322 us, with 16 KB pieces 347); short ones 8 KB, which more SMs share.
 constexpr int kLoadsLong = 8, kLoadsShort = 2;
 constexpr int64_t kShortList = 8 << 20;        // bytes
-constexpr int64_t kClusterList = 256 << 10;    // a list for one cluster
+// A list for one cluster: 0.2 MB takes 6.7 us and one launch of 2.7 us on the host, by two launches 6.2 us and 5.4; 0.4 MB
+// 10.4 us by the cluster, 7 by two launches.
+constexpr int64_t kClusterList = 256 << 10;
 __host__ __device__ constexpr int piece_bytes(int loads) { return kClipThreads * 16 * loads; }
 
 struct ClipArgs {
