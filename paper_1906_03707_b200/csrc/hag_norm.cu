@@ -8,8 +8,8 @@
 // Both directions are bound by memory: a row is read once (x, and g backward) and written once.  Measured on B200
 // against a copy at 6.45 TB/s: forward 233 000 x 128 fp32 40 us (5.96 TB/s), 10^6 x 256 bf16 160 us (6.45), 32 768 x 4096
 // bf16 102 us (5.3); backward with both parameter gradients 10^6 x 256 bf16 232 us in isolation (6.65) and 260 us in a long
-// run (5.9), 200 000 x 512 fp32 206 us (6.0).  Rows of odd widths take narrower loads and stores: 300 000 x 333 fp32
-// forward 173 us (4.6), bf16 169 us (2.4).
+// run (5.9), 200 000 x 512 fp32 206 us (6.0).  Contiguous rows of odd widths: 200 000 x 501 fp32 forward 138 us (5.8),
+// 300 000 x 333 backward fp32 198 us (6.1), bf16 175 (3.4: bound by instructions, as is its forward, 139 us).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(32 * kStripRows) norm_params_any_kernel(const 
 //            `hop` apart are misaligned alike; a group keeps to those, so a thread's vectors have the same columns in
 //            all its rows.  The up to 2 (V - 1) elements around the vectors are one more element for some threads (Edge).
 //   Pieces : else.  Rows are copied as the 16-byte pieces they touch, and the group reads narrow vectors out of those
-//            at any place.  (300 000 x 333 bf16: forward 169 us, by EDGE EDGE_FWD; backward 286, by EDGE EDGE_BWD.)
+//            at any place.  (300 000 x 333 bf16: forward 177 us, by EDGE 139; backward 286, by EDGE 175.)
 // The weights stay with the thread over all its rows: in registers, or from 16 columns per thread on in shared memory.
 constexpr int kMostThreads = 1024;        // of a block per row; up to kFewThreads the compiler may use 128 registers
 constexpr int kFewThreads = 512;
@@ -196,6 +196,10 @@ template <typename T, int L, int V, int K, bool BWD> constexpr int kLeastBlocks 
 // Rows per turn: 64 bytes per lane and turn (both operands of the backward pass together), but at least one row.
 constexpr int rows_per_turn(int bytes, int most) { return bytes >= 64 ? 1 : 64 / bytes < most ? 64 / bytes : most; }
 template <typename T, int L, int V, int K> constexpr int kFwdRows = L <= 0 ? 1 : kRing<T, V> ? rows_per_turn(K * V * int(sizeof(T)), 4) : V * K >= 16 ? 1 : 16 / (V * K) < 4 ? 16 / (V * K) : 4;
+// rows with edges: more to do per row, so two rows and two blocks per SM (10^6 x 129 fp32 forward 184 us, with four rows
+// and one block 208), but with 16 columns per thread one block (200 000 x 501 138 us, with two 167)
+template <typename T, int L, int V, int K, bool EDGE> constexpr int kFwdTurn = EDGE && L > 0 && V * K < 16 ? 2 : kFwdRows<T, L, V, K>;
+template <int L, int V, int K, bool EDGE> constexpr int kFwdBlocks = EDGE && L > 0 && V * K < 16 ? 2 : 1;
 template <typename T, int L, int V, int K> constexpr int kBwdRows = L > 0 && V * K <= 8 ? 2 : 1;
 
 // Sums of R values per lane over the L lanes of a group: lanes trade halves of the list while it has more than one
@@ -542,11 +546,11 @@ __device__ __forceinline__ float2 block_sum2(float a, float b, float2 *slot) {
 }
 
 template <typename T, int V, int L, int K, bool EDGE>
-__global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, false>)) norm_fwd_kernel(const NormArgs p) {
+__global__ void __launch_bounds__(kThreads<L>, (L > 0 ? kFwdBlocks<L, V, K, EDGE> : kLeastBlocks<T, L, V, K, false>)) norm_fwd_kernel(const NormArgs p) {
     hagk::pdl_launch_dependents();
     extern __shared__ __align__(16) char raw[];
     __shared__ float2 slots[2][32];
-    constexpr int R = kFwdRows<T, L, V, K>;
+    constexpr int R = kFwdTurn<T, L, V, K, EDGE>;
     const int32_t hop = EDGE ? p.hop : 1;
     const Turns<L, R> turns(p.n, hop);
     const int lane = threadIdx.x & 31, first = turns.first, step = turns.step;
@@ -928,7 +932,7 @@ cudaError_t allow_shared() {
 
 template <typename T, int V, int L, int K, bool BWD, bool EDGE>
 cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
-    constexpr int R = BWD ? kBwdRows<T, L, V, K> : kFwdRows<T, L, V, K>, OPS = BWD ? 2 : 1;
+    constexpr int R = BWD ? kBwdRows<T, L, V, K> : kFwdTurn<T, L, V, K, EDGE>, OPS = BWD ? 2 : 1;
     constexpr auto kernel = BWD ? norm_bwd_kernel<T, V, L, K, EDGE> : norm_fwd_kernel<T, V, L, K, EDGE>;
     cudaError_t err = allow_shared<kernel>();
     if (err != cudaSuccess) return err;
@@ -939,7 +943,7 @@ cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
     else stage = size_t(OPS) * R * Ahead<T, V, K, R, OPS, L>::row_bytes(L > 0 ? 32 : threads) * (L > 0 ? threads / 32 : 1);
     const size_t edges = EDGE ? size_t(OPS) * R * 4 * threads : 0;        // of a stage
     // as many stages as leave room for the blocks that the registers allow
-    const int blocks = L <= 0 ? std::max(1, std::min(8, 768 / threads)) : BWD || !kRing<T, V> ? 2 : 1;
+    const int blocks = L <= 0 ? std::max(1, std::min(8, 768 / threads)) : BWD || !kRing<T, V> ? 2 : kFwdBlocks<L, V, K, EDGE>;
     p.stages = L <= 0 ? kBlockStages : BWD ? kBwdStages : kFwdStages;
     while (p.stages > 1 && (params + p.stages * (stage + edges) + 1024) * blocks > size_t(kSmShared)) --p.stages;
     p.edge_at = int32_t(params + p.stages * stage);
@@ -949,7 +953,7 @@ cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
     static std::atomic<int> resident[kMostThreads / 32 + 1];
     int most = resident[threads / 32].load(std::memory_order_relaxed);
     if (most == 0) resident[threads / 32].store(most = resident_blocks(kernel, threads, shared), std::memory_order_relaxed);
-    most = std::min(most, kRing<T, V> && L > 0 ? kSms * (BWD ? 2 : 1) : most_parts(p.D));
+    most = std::min(most, kRing<T, V> && L > 0 ? kSms * (BWD ? 2 : kFwdBlocks<L, V, K, EDGE>) : most_parts(p.D));
     const int64_t rows_per_block = L <= 0 ? 1 : int64_t(threads / 32) * (32 / (L <= 0 ? 32 : L)) * R;
     int64_t grid = std::max<int64_t>(1, std::min<int64_t>((p.n + rows_per_block - 1) / rows_per_block, most));
     // one block does without the second launch
