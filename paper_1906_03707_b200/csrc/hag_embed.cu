@@ -487,23 +487,39 @@ __device__ __forceinline__ void store_row(const SumArgs &p, uint32_t key, int ve
     o.store(static_cast<TO *>(p.out) + int64_t(key) * p.ld_out, vec);
 }
 
-template <typename TG, typename TO, int V>
+// K: vectors per lane, 32 apart (narrow vectors: a row's loads would else be too small to keep the memory busy).
+template <typename TG, typename TO, int V, int K>
 __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArgs p) {
     hagk::pdl_launch_dependents();
     const int worker = (blockIdx.x * kSumThreads + threadIdx.x) / p.lanes;
-    const int vec = blockIdx.y * 32 + (threadIdx.x & (p.lanes - 1));
-    const bool column = vec < p.D / V;                         // lanes beyond the row only keep step
+    const int vec = blockIdx.y * (32 * K) + (threadIdx.x & (p.lanes - 1)), n_vec = p.D / V;      // lanes beyond the row only keep step
     const int32_t t0 = worker < p.workers ? worker * p.stretch : p.n;
     const int32_t t1 = int32_t(min(int64_t(p.n), int64_t(t0) + p.stretch));
     hagk::pdl_wait();
     if (t0 >= t1) return;
     const uint32_t none = 0xffffffffu, rows = uint32_t(p.n_rows);
     const uint32_t before = t0 > 0 ? list_key(p, t0 - 1) : none, after = t1 < p.n ? list_key(p, t1) : none;
-    const int64_t part = int64_t(worker) * ((p.D + 3) & ~3) + int64_t(vec) * V;
-    auto leave = [&](float *at, const float *acc) {
-        if (!column) return;
+    const int64_t part = int64_t(worker) * ((p.D + 3) & ~3);
+    float acc[K][V];
+    auto clear = [&]() {
 #pragma unroll
-        for (int j = 0; j < V; ++j) at[part + j] = acc[j];
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[k][j] = 0.0f;
+    };
+    auto leave = [&](float *at) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            hagr::Vec<float, V> o;
+            o.set(acc[k]);
+            if (vec + 32 * k < n_vec) o.store(at + part, vec + 32 * k);
+        }
+    };
+    auto finish = [&](uint32_t row) {
+        if (row >= rows) return;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (vec + 32 * k < n_vec) store_row<TO, V>(p, row, vec + 32 * k, acc[k]);
     };
     uint32_t key[kSumBatch], place[kSumBatch];
     auto fetch = [&](int32_t t) {
@@ -516,46 +532,50 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
     fetch(t0);
     uint32_t cur = key[0];
     bool from_left = cur == before;                            // the current run began in an earlier stretch
-    float acc[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] = 0.0f;
+    clear();
     for (int32_t t = t0; t < t1; t += kSumBatch) {
-        hagr::Vec<TG, V> g[kSumBatch];
-        uint32_t k[kSumBatch];
+        hagr::Vec<TG, V> g[kSumBatch][K];
+        uint32_t id[kSumBatch];
 #pragma unroll
         for (int u = 0; u < kSumBatch; ++u) {
-            k[u] = t + u < t1 ? key[u] : none;
-            g[u].zero();
-            if (k[u] < rows && column) g[u].template load<hagr::kOnce>(static_cast<const TG *>(p.grad) + int64_t(place[u]) * p.ld_grad, vec);
+            id[u] = t + u < t1 ? key[u] : none;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                g[u][k].zero();
+                if (id[u] < rows && vec + 32 * k < n_vec)
+                    g[u][k].template load<hagr::kOnce>(static_cast<const TG *>(p.grad) + int64_t(place[u]) * p.ld_grad, vec + 32 * k);
+            }
         }
         if (t + kSumBatch < t1) fetch(t + kSumBatch);          // the next ids while the rows are on their way
-        if (k[kSumBatch - 1] == cur) {                         // sorted: the whole batch belongs to the run
-            float v[V];
+        if (id[kSumBatch - 1] == cur) {                        // sorted: the whole batch belongs to the run
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[j] = (g[0].get(j) + g[4].get(j)) + (g[2].get(j) + g[6].get(j));
-                v[j] += (g[1].get(j) + g[5].get(j)) + (g[3].get(j) + g[7].get(j));
-                acc[j] += v[j];
-            }
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float even = (g[0][k].get(j) + g[4][k].get(j)) + (g[2][k].get(j) + g[6][k].get(j));
+                    const float odd = (g[1][k].get(j) + g[5][k].get(j)) + (g[3][k].get(j) + g[7][k].get(j));
+                    acc[k][j] += even + odd;
+                }
             continue;
         }
 #pragma unroll
         for (int u = 0; u < kSumBatch; ++u) {
-            if (t + u < t1 && k[u] != cur) {
-                if (from_left) leave(p.head, acc);
-                else if (column && cur < rows) store_row<TO, V>(p, cur, vec, acc);
+            if (t + u < t1 && id[u] != cur) {
+                if (from_left) leave(p.head);
+                else finish(cur);
                 from_left = false;
-                cur = k[u];
-#pragma unroll
-                for (int j = 0; j < V; ++j) acc[j] = 0.0f;
+                cur = id[u];
+                clear();
             }
 #pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] += g[u].get(j);
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[k][j] += g[u][k].get(j);
         }
     }
-    if (from_left) leave(p.head, acc);
-    else if (cur == after) leave(p.tail, acc);
-    else if (column && cur < rows) store_row<TO, V>(p, cur, vec, acc);
+    if (from_left) leave(p.head);
+    else if (cur == after) leave(p.tail);
+    else finish(cur);
 }
 
 // Rows whose runs cross stretches: the tail of the stretch where the run begins and the heads of the following
@@ -655,16 +675,16 @@ __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const SumA
 // Warps for the sums: 16 per SM with kSumBatch 16-byte loads per lane in flight keep 64 KB per SM on their way.
 constexpr int kSumWarps = 148 * 16;
 
-template <typename TG, typename TO, int V>
-cudaError_t launch_sum(SumArgs &p, cudaStream_t s) {
+template <typename TG, typename TO, int V, int K>
+cudaError_t launch_sum_columns(SumArgs &p, cudaStream_t s) {
     const int n_vec = p.D / V;
     p.lanes = hagl::lanes_per_row(n_vec);
-    const int column_blocks = (n_vec + 31) / 32;
+    const int column_blocks = (n_vec + 32 * K - 1) / (32 * K);
     const int64_t most = std::max<int64_t>(int64_t(kSumWarps) / column_blocks, 1) * (32 / p.lanes);
     const int64_t batches = (int64_t(p.n) + kSumBatch - 1) / kSumBatch;
     p.stretch = int32_t((batches + most - 1) / most * kSumBatch);
     p.workers = int32_t((int64_t(p.n) + p.stretch - 1) / p.stretch);
-    cudaError_t err = launch_with(embedding_sum_kernel<TG, TO, V>,
+    cudaError_t err = launch_with(embedding_sum_kernel<TG, TO, V, K>,
                                   dim3(unsigned((int64_t(p.workers) * p.lanes + kSumThreads - 1) / kSumThreads), unsigned(column_blocks)),
                                   kSumThreads, 0, p, s);
     if (err == cudaSuccess && p.workers > 1)
@@ -672,6 +692,18 @@ cudaError_t launch_sum(SumArgs &p, cudaStream_t s) {
                           dim3(unsigned((p.workers + kJoinWarps - 1) / kJoinWarps), unsigned(((p.D + 3) / 4 + kJoinQuads - 1) / kJoinQuads)),
                           kJoinThreads, 0, p, s);
     return err;
+}
+
+template <typename TG, typename TO, int V>
+cudaError_t launch_sum(SumArgs &p, cudaStream_t s) {
+    // up to 16 bytes per lane and row, as far as the row fills them
+    constexpr int kMost = V * int(sizeof(TG)) >= 8 ? 1 : 4;
+    const int n_vec = p.D / V;
+    if constexpr (kMost == 4) {
+        if (n_vec > 64) return launch_sum_columns<TG, TO, V, 4>(p, s);
+        if (n_vec > 32) return launch_sum_columns<TG, TO, V, 2>(p, s);
+    }
+    return launch_sum_columns<TG, TO, V, 1>(p, s);
 }
 
 template <typename TG, typename TO>
