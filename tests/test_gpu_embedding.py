@@ -235,3 +235,28 @@ def test_refusals():
     assert lib.hag_embedding_fwd(vp(ids.data_ptr()), 0, 1, 3, vp(table.data_ptr()), 0, 8, 0, 8, 1.0, vp(table.data_ptr()), 8, None) == hb.HAG_ERR_ARG
     torch.cuda.synchronize()
     assert (out == 5).all()
+
+
+@pytest.mark.parametrize("n,v,d", [(40, 7, 12), (5000, 90, 33), (30_000, 40_000, 20)])
+def test_a_batch_without_a_single_token(n, v, d):
+    table = torch.full((v, d), float("nan"), device="cuda")
+    for ids in (torch.full((n,), -1, device="cuda"), torch.full((n,), v, dtype=torch.int32, device="cuda")):
+        assert not hb.embedding_fwd(ids, table).any()
+        out = torch.full((v, d), float("nan"), device="cuda")
+        hb.embedding_bwd(ids, torch.full((n, d), float("inf"), device="cuda"), v, out=out)
+        assert not out.any()
+
+
+@pytest.mark.parametrize("offset", [1, 3])
+@pytest.mark.parametrize("n,v,d", [(200, 30, 24), (3000, 100, 72), (20_000, 9000, 65)])
+def test_matrices_that_begin_anywhere(n, v, d, offset):
+    ids = _ids(22, n, v, "holes", torch.int32)
+    for dtype in (F32, BF16):
+        grad = torch.randn(n * d + offset, generator=_gen(23), device="cuda").to(dtype)[offset:].view(n, d)
+        buf = torch.full((v * d + offset + 9,), 3.0, device="cuda", dtype=dtype)
+        out = buf[offset:offset + v * d].view(v, d)
+        _check_backward(ids, grad, v, 0.5, dtype, out=out)
+        assert (buf[:offset] == 3).all() and (buf[offset + v * d:] == 3).all()
+        rows = torch.full((n * d + offset + 9,), 3.0, device="cuda", dtype=dtype)
+        got = hb.embedding_fwd(ids, out, 2.0, out=rows[offset:offset + n * d].view(n, d))
+        assert torch.equal(got, _forward_want(ids, out, 2.0, dtype)) and (rows[:offset] == 3).all() and (rows[offset + n * d:] == 3).all()

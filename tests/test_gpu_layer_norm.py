@@ -278,3 +278,29 @@ def test_refusals():
     with pytest.raises(hb.HagError) as e:
         hb.layer_norm_fwd(x, w, out=torch.empty(1, 8, device="cuda").expand(4, 8))
     assert e.value.status == hb.HAG_ERR_ARG
+
+
+def _at(t, offset):
+    """A contiguous copy of t that begins `offset` elements into its storage, with a guard value on both sides."""
+    buf = torch.full((t.numel() + offset + 9,), 3.0, device="cuda", dtype=t.dtype)
+    view = buf[offset:offset + t.numel()].view(t.shape)
+    view.copy_(t)
+    return view, buf
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d", [(1, 129), (3, 333), (77, 130), (300, 256), (41, 515), (19, 1433), (9, 5363), (5, 9999), (23, 1024)])
+@pytest.mark.parametrize("x_at,g_at,y_at", [(1, 1, 1), (0, 0, 0), (5, 5, 5), (3, 11, 3), (2, 0, 7), (6, 6, 1)])
+def test_matrices_that_begin_anywhere(n, d, dtype, x_at, g_at, y_at):
+    """The same misalignment in all matrices (vectors with edges), and different ones (pieces); nothing outside the
+    result is written."""
+    x, _ = _at((_randn(32, n, d) * 1.5 + _randn(33, d)).to(dtype), x_at)
+    g, _ = _at(_randn(34, n, d).to(dtype), g_at)
+    w, b = 1 + 0.2 * _randn(35, d), 0.3 * _randn(36, d)
+    for check in (lambda o: _check_forward(x, w, b, out=o), lambda o: _check_backward(g, x, w, out=o)):
+        out, buf = _at(torch.zeros(n, d, device="cuda", dtype=dtype), y_at)
+        check(out)
+        assert (buf[:y_at] == 3).all() and (buf[y_at + n * d:] == 3).all()
+    xin, buf = _at(x, x_at)
+    want = hb.layer_norm_fwd(x, w, b, eps=EPS, out=_at(x, x_at)[0])[0]
+    assert torch.equal(hb.layer_norm_fwd(xin, w, b, eps=EPS, out=xin)[0], want) and (buf[:x_at] == 3).all() and (buf[x_at + n * d:] == 3).all()
