@@ -621,12 +621,13 @@ def _vector(t, what, count, index, dtype=None):
     return t.data_ptr()
 
 
-def _scratch_for(workspace, need, device):
+def _scratch_for(workspace, need, like):
+    """`need` bytes on the device of `like`: the caller's, or new ones."""
     import torch
     if workspace is None:
-        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    if not workspace.is_contiguous() or workspace.device != device or workspace.numel() * workspace.element_size() < need:
-        raise ValueError(f"workspace must be a contiguous tensor of at least {need} bytes on {device}")
+        return like.new_empty(need, dtype=torch.uint8) if need else None
+    if not workspace.is_contiguous() or workspace.device != like.device or workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"workspace must be a contiguous tensor of at least {need} bytes on {like.device}")
     return workspace
 
 
@@ -682,14 +683,14 @@ def embedding_bwd(ids, grad_out, n_rows: int, scale=1.0, out=None, dtype=None, w
     """``hag_embedding_bwd``: the gradient of ``embedding_fwd`` with respect to a table of n_rows rows, of ``dtype``
     (default: grad_out's)."""
     ld = _rows(grad_out, "grad_out")
-    index, device, (n, d) = grad_out.get_device(), grad_out.device, grad_out.shape
+    index, (n, d) = grad_out.get_device(), grad_out.shape
     id_type = _ids(ids, index, n)
     if out is None:
         out = grad_out.new_empty((n_rows, d), dtype=dtype or grad_out.dtype)
         ld_out = d
     else:
         ld_out = _rows(out, "out", (n_rows, d), index, dtype)
-    ws = _scratch_for(workspace, load_library().hag_embedding_bwd_workspace_bytes(n, n_rows, d), device)
+    ws = _scratch_for(workspace, load_library().hag_embedding_bwd_workspace_bytes(n, n_rows, d), grad_out)
     _call("hag_embedding_bwd", index, ids.data_ptr(), id_type, n, n_rows, _code(grad_out.dtype), d, grad_out.data_ptr(), ld, scale,
           out.data_ptr(), _code(out.dtype), ld_out, None if ws is None else ws.data_ptr())
     return out
@@ -725,7 +726,7 @@ def layer_norm_bwd(grad_out, x, mean, rstd, weight=None, out=None, param_grads=T
     is false.  ``out`` may be grad_out or x."""
     import torch
     ld = _rows(x, "x")
-    index, device, dtype, shape = x.get_device(), x.device, x.dtype, x.shape
+    index, dtype, shape = x.get_device(), x.dtype, x.shape
     n, d = shape
     ld_g = _rows(grad_out, "grad_out", shape, index, dtype)
     w = None if weight is None else _vector(weight, "weight", d, index, param_dtype)
@@ -743,7 +744,7 @@ def layer_norm_bwd(grad_out, x, mean, rstd, weight=None, out=None, param_grads=T
         gw, gb = both.unbind()
         gwp = both.data_ptr()
         gbp = gwp + d * (4 if code == HAG_F32 else 2)
-        ws = _scratch_for(workspace, load_library().hag_layer_norm_bwd_workspace_bytes(n, d), device)
+        ws = _scratch_for(workspace, load_library().hag_layer_norm_bwd_workspace_bytes(n, d), x)
     _call("hag_layer_norm_bwd", index, n, d, _code(dtype), grad_out.data_ptr(), ld_g, x.data_ptr(), ld, m, r, w, code, out.data_ptr(),
           ld_out, gwp, gbp, None if ws is None else ws.data_ptr())
     return out, gw, gb
@@ -778,7 +779,7 @@ def _clip(grads, max_norm, out, workspace):
     import torch
     if not grads or not grads[0].is_cuda:
         raise ValueError("gradients must be a list of device tensors, not empty")
-    device, index, count = grads[0].device, grads[0].get_device(), len(grads)
+    index, count = grads[0].get_device(), len(grads)
     ptrs, lens, kinds = _tensor_list(grads, index)
     if out is not None:
         to, to_lens, to_kinds = (ptrs, lens, kinds) if out is grads else _tensor_list(out, index)
@@ -789,7 +790,7 @@ def _clip(grads, max_norm, out, workspace):
                 raise ValueError("a tensor is named twice")
         to = array("Q", to)
     addresses, lengths, codes = array("Q", ptrs), array("q", lens), array("i", [_codes[k] for k in kinds])
-    ws = _scratch_for(workspace, load_library().hag_clip_grad_norm_workspace_bytes(count), device)
+    ws = _scratch_for(workspace, load_library().hag_clip_grad_norm_workspace_bytes(count), grads[0])
     norm = grads[0].new_empty((), dtype=torch.float32)
     _call("hag_clip_grad_norm", index, count, addresses.buffer_info()[0], None if out is None else to.buffer_info()[0],
           lengths.buffer_info()[0], codes.buffer_info()[0], max_norm, norm.data_ptr(), ws.data_ptr())
