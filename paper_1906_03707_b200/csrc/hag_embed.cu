@@ -9,7 +9,7 @@
 //
 // Both are bound by memory.  Measured on B200 (copy rate 6.45 TB/s): lookup of 500 000 x 64 fp32 from 119 rows 23 us (the
 // 128 MB written at 5.6 TB/s), of 10^6 x 256 fp32 into bf16 from 50 257 rows 138 us (it reads 1 GB out of the L1 and L2
-// besides 591 MB of DRAM traffic).  Gradient of 500 000 x 64 fp32 into 119 rows 33 us (128 MB read); of 10^6 x 256 bf16 into
+// besides 591 MB of DRAM traffic).  Gradient of 500 000 x 64 fp32 into 119 rows 29 us (128 MB read); of 10^6 x 256 bf16 into
 // 50 257 fp32 rows 151 us: 94 for the sums (512 MB read, 51 MB written), 9 for the joins, 48 for two sorting passes and
 // the zeros.
 #include <cuda_runtime.h>
@@ -730,7 +730,7 @@ int64_t partial_floats(int64_t n, int32_t D) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Few rows: no sort of the whole list (500 000 x 64 into 119 rows takes 33 us this way and 52 by the sort, 100 000 x 64 13
+// Few rows: no sort of the whole list (500 000 x 64 into 119 rows takes 29 us this way and 52 by the sort, 100 000 x 64 13
 // and 32; 10^6 x 128 into 3000 rows would take 294 us and takes 120 by the sort: its tables are larger than its rows).
 // Every block sorts a tile of the tokens in shared memory, adds up its runs as
 // above (its groups of lanes are the workers, heads and tails stay in shared memory), and leaves a table of its own:
@@ -750,6 +750,10 @@ struct TileArgs {
     hagr::Divisor per_row;       // the pitch (table_join_kernel)
 };
 constexpr int kTileBatch = 4;    // rows in flight per worker: 32 warps of them
+// Of a tile's gradient rows, what is asked into the L2 while the ids are sorted, when the memory would be idle: 500 000 x 64
+// into 119 rows takes 29.2 us with it and 32.8 without (128 KB 29.7, 384 KB 29.9).  In the launches of the full sort the
+// same slowed the sort by what it saved.
+constexpr int kTileAhead = 224 << 10;
 
 template <typename TO>
 __device__ __forceinline__ void store_scalar(const TileArgs &p, int32_t row, int32_t col, float v) {
@@ -793,6 +797,16 @@ __global__ void __launch_bounds__(kSortThreads) embedding_tile_kernel(const __gr
         for (int k = 0; k < kSortItems; ++k)
             if (k < items) pair[k] = mine + 32 * k < len ? sort_pair(p.sort, begin + mine + 32 * k) : make_uint2(0xffffffffu, 0);
         // rows that no token of the tile names: cleared while the ids are on their way
+        if (p.partial) {
+            constexpr int kLine = 128;
+            const int from = blockIdx.y * p.lanes * V, bytes = min(p.D - from, p.lanes * V) * int(sizeof(TG));
+            const int per_row = (bytes + kLine - 1) / kLine, lines = min(len, kTileAhead / bytes) * per_row;
+            const char *first = static_cast<const char *>(p.grad) + (begin * p.ld_grad + from) * int64_t(sizeof(TG));
+            for (int i = t; i < lines; i += kSortThreads) {
+                const int row = i / per_row;
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(first + row * p.ld_grad * int64_t(sizeof(TG)) + (i - row * per_row) * kLine));
+            }
+        }
         const int vec = blockIdx.y * p.lanes + t % p.lanes;
         const float zeros[V] = {};
         if (vec < p.D / V)
