@@ -352,7 +352,7 @@ struct Pieces {
     __device__ __forceinline__ Pieces(char *base, const NormArgs &p, int first_, int step_, int)
         : pitch(row_bytes(step_)), len(p.D * int(sizeof(T))), first(first_), step(step_) {
         end = p.stages * (OPS * R) * pitch;
-        area = base + (L > 0 ? int(threadIdx.x >> 5) * end : 0);
+        area = base + (L > 0 ? int(threadIdx.x) / (L > 0 ? L : 1) * end : 0);
     }
     __device__ __forceinline__ void issue(int op, int i, const char *row, bool live) {
         char *to = area + write + (op * R + i) * pitch;
@@ -940,7 +940,7 @@ cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
     const size_t params = Params<V, K, BWD ? 1 : 2, kShared<T, L, V, K, EDGE>>::bytes(L <= 0 ? threads : L);
     size_t stage;
     if constexpr (kRing<T, V>) stage = size_t(Ahead<T, V, K, R, OPS, L>::kStage) * threads;
-    else stage = size_t(OPS) * R * Ahead<T, V, K, R, OPS, L>::row_bytes(L > 0 ? 32 : threads) * (L > 0 ? threads / 32 : 1);
+    else stage = size_t(OPS) * R * Ahead<T, V, K, R, OPS, L>::row_bytes(L > 0 ? L : threads) * (L > 0 ? threads / (L > 0 ? L : 1) : 1);
     const size_t edges = EDGE ? size_t(OPS) * R * 4 * threads : 0;        // of a stage
     // as many stages as leave room for the blocks that the registers allow
     const int blocks = L <= 0 ? std::max(1, std::min(8, 768 / threads)) : BWD || !kRing<T, V> ? 2 : kFwdBlocks<L, V, K, EDGE>;
@@ -965,14 +965,24 @@ cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
 
 // Rows of up to 1024 elements (narrow vectors: 512 forward, 256 backward) go to a warp or a part of one, rows of up to
 // 1024 * kPerThread to a block.  A warp needs no barrier: 65 536 x 1024 bf16 forward takes 54 us with a warp per row and
-// 96 with a block of 64 threads.
+// 96 with a block of 64 threads.  Narrow vectors are bound by the instructions around a row, so that a warp takes several
+// rows and a lane several vectors: 1 175 089 x 13 bf16 runs forward in 38 us with 8 lanes and two vectors each, in 59
+// with 16 lanes and one, in 121 with 32 (backward 65, 96, 185); 1 175 089 x 29 fp32 in 61 with 8 lanes, 69 with 16, 115
+// with 32; 775 089 x 49 bf16 in 66 with 16 lanes, 71 with 8, 96 with 32.  Wide vectors are near the memory's rate with
+// one each.
 constexpr int kPerThread = 16;
 template <typename T, int V, bool BWD, bool EDGE = false>
 cudaError_t launch_width(NormArgs &p, cudaStream_t s) {
     const int32_t n_vec = p.D / V;
-    if constexpr (V * int(sizeof(T)) == 16 && !EDGE) {
+    if constexpr (!EDGE) {
         if (n_vec <= 8) return launch_rows<T, V, 8, 1, BWD, EDGE>(p, s);
-        if (n_vec <= 16) return launch_rows<T, V, 16, 1, BWD, EDGE>(p, s);
+        if constexpr (kRing<T, V>) {
+            if (n_vec <= 16) return launch_rows<T, V, 16, 1, BWD, EDGE>(p, s);
+        } else {
+            if (n_vec <= 16) return launch_rows<T, V, 8, 2, BWD, EDGE>(p, s);
+            if (n_vec <= 32) return launch_rows<T, V, 8, 4, BWD, EDGE>(p, s);
+            if (n_vec <= 64) return launch_rows<T, V, 16, 4, BWD, EDGE>(p, s);
+        }
     }
     if (n_vec <= 32) return launch_rows<T, V, 32, 1, BWD, EDGE>(p, s);
     if (n_vec <= 64) return launch_rows<T, V, 32, 2, BWD, EDGE>(p, s);

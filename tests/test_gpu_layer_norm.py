@@ -304,3 +304,17 @@ def test_matrices_that_begin_anywhere(n, d, dtype, x_at, g_at, y_at):
     xin, buf = _at(x, x_at)
     want = hb.layer_norm_fwd(x, w, b, eps=EPS, out=_at(x, x_at)[0])[0]
     assert torch.equal(hb.layer_norm_fwd(xin, w, b, eps=EPS, out=xin)[0], want) and (buf[:x_at] == 3).all() and (buf[x_at + n * d:] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d", [(1, 13), (2, 2), (20_011, 5), (9001, 8), (30_005, 13), (17, 16), (7003, 17), (5001, 29), (11, 30), (4001, 33), (3001, 49), (2003, 62), (1001, 64), (907, 65)])
+@pytest.mark.parametrize("x_at,g_at,y_at", [(0, 1, 2), (7, 3, 5)])
+def test_narrow_rows_that_begin_anywhere(n, d, dtype, x_at, g_at, y_at):
+    """Several rows to a warp, each row's pieces in a place of its own; nothing outside the result is written."""
+    x, _ = _at((_randn(37, n, d) * 1.5 + _randn(38, d)).to(dtype), x_at)
+    g, _ = _at(_randn(39, n, d).to(dtype), g_at)
+    w, b = 1 + 0.2 * _randn(40, d), 0.3 * _randn(41, d)
+    for check in (lambda o: _check_forward(x, w, b, out=o), lambda o: _check_backward(g, x, w, out=o)):
+        out, buf = _at(torch.zeros(n, d, device="cuda", dtype=dtype), y_at)
+        check(out)
+        assert (buf[:y_at] == 3).all() and (buf[y_at + n * d:] == 3).all()
