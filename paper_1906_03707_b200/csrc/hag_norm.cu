@@ -963,22 +963,27 @@ cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
     return launch(kernel, dim3(unsigned(grid)), unsigned(threads), shared, p, s);
 }
 
-// Rows of up to 1024 elements (narrow vectors: 512 forward, 256 backward) go to a warp or a part of one, rows of up to
+// Rows of up to 1024 elements (narrow vectors: 512) go to a warp or a part of one, rows of up to
 // 1024 * kPerThread to a block.  A warp needs no barrier: 65 536 x 1024 bf16 forward takes 54 us with a warp per row and
 // 96 with a block of 64 threads.  Narrow vectors are bound by the instructions around a row, so that a warp takes several
 // rows and a lane several vectors: 1 175 089 x 13 bf16 runs forward in 38 us with 8 lanes and two vectors each, in 59
 // with 16 lanes and one, in 121 with 32 (backward 65, 96, 185); 1 175 089 x 29 fp32 in 61 with 8 lanes, 69 with 16, 115
 // with 32; 775 089 x 49 bf16 in 66 with 16 lanes, 71 with 8, 96 with 32.  Wide vectors are near the memory's rate with
-// one each.
+// one each, but where they leave most of the lanes without one: 1 047 213 x 8 bf16 in 20 us with 4 lanes, 41 with 8
+// (backward 35 and 60), 32 bf16 in 25 and 42.  Narrow rows of 280 bf16 backward, 123 218 of them, take 95 us with 12
+// columns per lane, 117 with 16 and 123 with a block per row (forward 60, 75 with 16); 500 fp32 130 with 16, 140 with a
+// block.
 constexpr int kPerThread = 16;
 template <typename T, int V, bool BWD, bool EDGE = false>
 cudaError_t launch_width(NormArgs &p, cudaStream_t s) {
     const int32_t n_vec = p.D / V;
     if constexpr (!EDGE) {
-        if (n_vec <= 8) return launch_rows<T, V, 8, 1, BWD, EDGE>(p, s);
+        if (n_vec <= 4) return launch_rows<T, V, 4, 1, BWD, EDGE>(p, s);
         if constexpr (kRing<T, V>) {
+            if (n_vec <= 8) return launch_rows<T, V, 8, 1, BWD, EDGE>(p, s);
             if (n_vec <= 16) return launch_rows<T, V, 16, 1, BWD, EDGE>(p, s);
         } else {
+            if (n_vec <= 8) return launch_rows<T, V, 4, 2, BWD, EDGE>(p, s);
             if (n_vec <= 16) return launch_rows<T, V, 8, 2, BWD, EDGE>(p, s);
             if (n_vec <= 32) return launch_rows<T, V, 8, 4, BWD, EDGE>(p, s);
             if (n_vec <= 64) return launch_rows<T, V, 16, 4, BWD, EDGE>(p, s);
@@ -986,12 +991,13 @@ cudaError_t launch_width(NormArgs &p, cudaStream_t s) {
     }
     if (n_vec <= 32) return launch_rows<T, V, 32, 1, BWD, EDGE>(p, s);
     if (n_vec <= 64) return launch_rows<T, V, 32, 2, BWD, EDGE>(p, s);
-    // vectors per lane of a warp; narrow vectors of the backward pass: 8 columns per thread (with 16 too many registers)
-    constexpr int kMost = (kRing<T, V> ? EDGE ? 16 : 32 : BWD ? 8 : 16) / V;
+    constexpr int kMost = (kRing<T, V> && !EDGE ? 32 : 16) / V;       // vectors per lane of a warp
     if constexpr (kMost >= 4)
         if (n_vec <= 128) return launch_rows<T, V, 32, 4, BWD, EDGE>(p, s);
     if constexpr (kMost >= 8)
         if (n_vec <= 256) return launch_rows<T, V, 32, 8, BWD, EDGE>(p, s);
+    if constexpr (kMost >= 16 && !kRing<T, V>)
+        if (n_vec <= 384) return launch_rows<T, V, 32, 12, BWD, EDGE>(p, s);
     if constexpr (kMost >= 16)
         if (n_vec <= 512) return launch_rows<T, V, 32, 16, BWD, EDGE>(p, s);
     constexpr int kFew = (kRing<T, V> || !BWD ? kPerThread : 8) / V;

@@ -318,3 +318,17 @@ def test_narrow_rows_that_begin_anywhere(n, d, dtype, x_at, g_at, y_at):
         out, buf = _at(torch.zeros(n, d, device="cuda", dtype=dtype), y_at)
         check(out)
         assert (buf[:y_at] == 3).all() and (buf[y_at + n * d:] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [1, 3, 4, 8, 12, 16, 24, 32, 36, 257, 280, 380, 384, 385, 500, 512, 513])
+@pytest.mark.parametrize("n", [1, 31, 6007, 60_001])
+def test_rows_per_warp(n, d, dtype):
+    """Widths around each number of lanes and of vectors per lane; aligned rows, and rows five elements apart."""
+    n = n if d < 64 else min(n, 6007)
+    x, g = (_randn(42, n, d) * 1.5 + _randn(43, d)).to(dtype), _randn(44, n, d).to(dtype)
+    w, b = 1 + 0.2 * _randn(45, d), 0.3 * _randn(46, d)
+    far = torch.empty(n, d + 5, device="cuda", dtype=dtype)
+    for out in (None, far[:, :d]):
+        _check_forward(x, w, b, out=out)
+        _check_backward(g, x, w, out=out)
