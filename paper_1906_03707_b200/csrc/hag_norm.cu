@@ -972,7 +972,7 @@ cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
 // one each, but where they leave most of the lanes without one: 1 047 213 x 8 bf16 in 20 us with 4 lanes, 41 with 8
 // (backward 35 and 60), 32 bf16 in 25 and 42.  Narrow rows of 280 bf16 backward, 123 218 of them, take 95 us with 12
 // columns per lane, 117 with 16 and 123 with a block per row (forward 60, 75 with 16); 500 fp32 130 with 16, 140 with a
-// block.
+// block; 223 218 x 150 fp32 84 with 6, 132 with 8; 423 218 x 80 fp32 90 with 3, 123 with 4.
 constexpr int kPerThread = 16;
 template <typename T, int V, bool BWD, bool EDGE = false>
 cudaError_t launch_width(NormArgs &p, cudaStream_t s) {
@@ -992,8 +992,12 @@ cudaError_t launch_width(NormArgs &p, cudaStream_t s) {
     if (n_vec <= 32) return launch_rows<T, V, 32, 1, BWD, EDGE>(p, s);
     if (n_vec <= 64) return launch_rows<T, V, 32, 2, BWD, EDGE>(p, s);
     constexpr int kMost = (kRing<T, V> && !EDGE ? 32 : 16) / V;       // vectors per lane of a warp
+    if constexpr (!kRing<T, V>)
+        if (n_vec <= 96) return launch_rows<T, V, 32, 3, BWD, EDGE>(p, s);
     if constexpr (kMost >= 4)
         if (n_vec <= 128) return launch_rows<T, V, 32, 4, BWD, EDGE>(p, s);
+    if constexpr (kMost >= 8 && !kRing<T, V>)
+        if (n_vec <= 192) return launch_rows<T, V, 32, 6, BWD, EDGE>(p, s);
     if constexpr (kMost >= 8)
         if (n_vec <= 256) return launch_rows<T, V, 32, 8, BWD, EDGE>(p, s);
     if constexpr (kMost >= 16 && !kRing<T, V>)

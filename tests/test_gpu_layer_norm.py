@@ -332,3 +332,15 @@ def test_rows_per_warp(n, d, dtype):
     for out in (None, far[:, :d]):
         _check_forward(x, w, b, out=out)
         _check_backward(g, x, w, out=out)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [66, 80, 95, 96, 97, 150, 186, 191, 192, 193, 250])
+@pytest.mark.parametrize("n", [1, 7, 5003])
+def test_rows_of_three_or_six_vectors_per_lane(n, d, dtype):
+    x, g = (_randn(47, n, d) * 1.5 + _randn(48, d)).to(dtype), _randn(49, n, d).to(dtype)
+    w, b = 1 + 0.2 * _randn(50, d), 0.3 * _randn(51, d)
+    far = torch.empty(n, d + 5, device="cuda", dtype=dtype)
+    for out in (None, far[:, :d]):
+        _check_forward(x, w, b, out=out)
+        _check_backward(g, x, w, out=out)
