@@ -344,3 +344,14 @@ def test_rows_of_three_or_six_vectors_per_lane(n, d, dtype):
     for out in (None, far[:, :d]):
         _check_forward(x, w, b, out=out)
         _check_backward(g, x, w, out=out)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d", [(1, 4097), (5, 6050), (301, 7944), (3, 8190), (2, 8191), (2, 8192), (2, 8193)])
+def test_blocks_of_eight_or_sixteen_columns_per_thread(n, d, dtype):
+    x, g = (_randn(52, n, d) * 1.5 + _randn(53, d)).to(dtype), _randn(54, n, d).to(dtype)
+    w, b = 1 + 0.2 * _randn(55, d), 0.3 * _randn(56, d)
+    far = torch.empty(n, d + 5, device="cuda", dtype=dtype)
+    for out in (None, far[:, :d]):
+        _check_forward(x, w, b, out=out)
+        _check_backward(g, x, w, out=out)
