@@ -749,6 +749,26 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
                     gw[i][k] = t;
                 }
             }
+            // beyond the row xh is (0 - mean) * rstd: where that overflows, 0 times it is no number, and the sum is
+            // taken again without those places (280 bf16 columns, the worst case: 98 us with this test per row, 105 with a
+            // selection per vector, 95 without either)
+            if (__builtin_expect(s[2 * i + 1] != s[2 * i + 1], 0)) {
+                s[2 * i + 1] = ge[i] * xe[i];
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    Pairs<V> a, t;
+                    if constexpr (HOLD) {
+                        a = xh[i][k];
+                        t = gw[i][k];
+                    } else {
+                        a = widen(ahead.get(xs, k));
+                        t = widen(ahead.get(gs, k));
+                        a.shift_scale(-m[i], q[i]);
+                        t.mul(weights.get(0, k));
+                    }
+                    if (first + k * step < n_vec) s[2 * i + 1] += t.dot(a);
+                }
+            }
         }
         float s1[R], s2[R];
         if constexpr (L <= 0) {
