@@ -523,7 +523,7 @@ hag_status hag_layer_norm_bwd(int64_t n, int32_t D, hag_dtype dtype, const void 
  * is applied as it stands: N = inf gives c = 0 (and inf * 0 = NaN), N = NaN gives NaN everywhere.
  * workspace: hag_clip_grad_norm_workspace_bytes(count) bytes, 16-byte aligned; carries nothing between calls.
  * Errors: NULL, ARG (count < 0, a negative length, max_norm negative or no number), DTYPE, ALIGN (pointer not on its
- * element), WORKSPACE, TOO_LARGE (about 2^44 elements), CUDA. */
+ * element), WORKSPACE, TOO_LARGE (count > 2^28; 128 consecutive tensors with about 2^44 elements), CUDA. */
 size_t hag_clip_grad_norm_workspace_bytes(int32_t count);
 hag_status hag_clip_grad_norm(int32_t count, const void *const *grads, void *const *out, const int64_t *lengths,
                               const hag_dtype *dtypes, float max_norm, float *total_norm, void *workspace,

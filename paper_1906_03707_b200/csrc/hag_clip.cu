@@ -239,6 +239,7 @@ __global__ void __launch_bounds__(kClipThreads, 2) __cluster_dims__(kCluster, 1,
     if (p.scales) scale_pieces<kLoadsLong>(p, norm);
 }
 
+constexpr int32_t kClipMost = 1 << 28;         // tensors of a call: the number of their blocks' sums fits in 31 bits
 int launches_of(int32_t count) { return std::max(1, (count + kClipList - 1) / kClipList); }
 
 // The part of the list that launch `k` handles; false: it has more pieces than a launch can count.
@@ -247,16 +248,16 @@ bool fill(ClipArgs &p, int k, int loads, int32_t count, const void *const *in, v
     int64_t pieces = 0;
     for (int32_t t = k * kClipList; t < std::min(count, (k + 1) * kClipList); ++t) {
         if (len[t] == 0) continue;
+        const int64_t per = piece_bytes(loads) / (dtype[t] == HAG_BF16 ? 2 : 4), here = len[t] / per + (len[t] % per != 0);
+        if (pieces + here > 0x7fffffffLL) return false;
         const int i = p.tensors++;
-        const int64_t per = piece_bytes(loads) / (dtype[t] == HAG_BF16 ? 2 : 4);
         p.in[i] = in[t];
         p.out[i] = out ? out[t] : nullptr;
         p.len[i] = len[t];
         p.first_piece[i] = uint32_t(pieces);
         p.bf16[i] = dtype[t] == HAG_BF16;
         p.vec[i] = hagl::aligned16(in[t]) && (!out || hagl::aligned16(out[t]));
-        pieces += (len[t] + per - 1) / per;
-        if (pieces > 0x7fffffffLL) return false;
+        pieces += here;
     }
     p.pieces = uint32_t(pieces);
     return true;
@@ -265,7 +266,7 @@ bool fill(ClipArgs &p, int k, int loads, int32_t count, const void *const *in, v
 }  // namespace
 
 extern "C" size_t hag_clip_grad_norm_workspace_bytes(int32_t count) {
-    return count < 0 ? 0 : size_t(launches_of(count)) * kClipBlocks * sizeof(double);
+    return count < 0 || count > kClipMost ? 0 : size_t(launches_of(count)) * kClipBlocks * sizeof(double);
 }
 
 extern "C" hag_status hag_clip_grad_norm(int32_t count, const void *const *grads, void *const *out, const int64_t *lengths,
@@ -274,6 +275,7 @@ extern "C" hag_status hag_clip_grad_norm(int32_t count, const void *const *grads
     if (count < 0 || !(max_norm >= 0.0f)) return HAG_ERR_ARG;
     if (count > 0 && (!grads || !lengths || !dtypes)) return HAG_ERR_NULL;
     if (!out && !total_norm) return HAG_ERR_NULL;
+    if (count > kClipMost) return HAG_ERR_TOO_LARGE;
     int64_t bytes = 0;
     for (int32_t t = 0; t < count; ++t) {
         if (dtypes[t] != HAG_F32 && dtypes[t] != HAG_BF16) return HAG_ERR_DTYPE;
