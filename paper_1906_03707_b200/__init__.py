@@ -607,8 +607,11 @@ def _rows(t, what, like=None, index=None, dtype=None):
     if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
     rs, cs = t.stride()
-    if cs != 1 and t.shape[1] > 1:
+    cols = t.shape[1]
+    if cs != 1 and cols > 1:
         raise ValueError(f"the rows of {what} must be contiguous")
+    if cols > 0x7fffffff:                                       # the calls count columns in 32 bits
+        raise HagError(HAG_ERR_TOO_LARGE, what)
     return rs
 
 

@@ -38,3 +38,14 @@ def test_layer_norm_gradient_of_large_constant_rows(d, dtype, pad):
     bound = U * rs * (4 * q.abs() + (64 + d / 256 + 4) * q.abs().mean(1, keepdim=True)) + (2.0 ** -8 * want.abs() if dtype == BF16 else 0)
     assert ((gx.double() - want).abs() <= bound).all()
     assert not gw.any() and ((gb.double() - g.double().sum(0)).abs() <= 8 * U * g.double().abs().sum(0)).all()
+
+
+def test_more_columns_than_32_bits_are_refused():
+    """2^32 + 8 columns are not the 8 that their lower 32 bits say."""
+    x = torch.zeros(1, (1 << 32) + 8, device="cuda", dtype=BF16)
+    one = torch.zeros(1, device="cuda")
+    for call in (lambda: hb.layer_norm_fwd(x, out=x), lambda: hb.layer_norm_bwd(x, x, one, one, out=x, param_grads=False),
+                 lambda: hb.embedding_fwd(one.int(), x), lambda: hb.embedding_bwd(one.int(), x, 1)):
+        with pytest.raises(hb.HagError) as e:
+            call()
+        assert e.value.status == hb.HAG_ERR_TOO_LARGE
