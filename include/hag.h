@@ -517,8 +517,9 @@ hag_status hag_layer_norm_bwd(int64_t n, int32_t D, hag_dtype dtype, const void 
  *   N = sqrt(sum over all tensors and elements of g^2), c = min(1, max_norm / (N + 1e-6)), out_t = c * grads_t.
  * grads, out, lengths, dtypes: HOST arrays of `count` entries (read during the call, not kept); grads[t] and out[t]
  * are DEVICE pointers to lengths[t] contiguous elements of dtypes[t].  In place: out[t] may be grads[t] (it is then
- * left untouched when c = 1); a tensor must not be named twice.  out NULL: the norm alone.  total_norm: DEVICE
- * pointer to one float that receives N (may be NULL if out is not).  Tensors of length 0 are skipped and may be NULL.
+ * left untouched when c = 1), but no other entry of grads; a tensor must not be named twice.  out NULL: the norm
+ * alone.  total_norm: DEVICE pointer to one float that receives N (may be NULL if out is not).  Tensors of length 0 are
+ * skipped and may be NULL.
  * Squares are fp32 and are added in fp32 over 64 values at most, then in fp64; a value whose square overflows fp32 gives N = inf.  The formula
  * is applied as it stands: N = inf gives c = 0 (and inf * 0 = NaN), N = NaN gives NaN everywhere.
  * workspace: hag_clip_grad_norm_workspace_bytes(count) bytes, 16-byte aligned; carries nothing between calls.

@@ -20,6 +20,7 @@ from __future__ import annotations
 import ctypes
 import os
 from array import array
+from operator import eq
 
 import numpy as np
 
@@ -767,8 +768,8 @@ def _tensor_list(tensors, index):
 
 def clip_grad_norm(grads, max_norm, out=None, workspace=None):
     """``hag_clip_grad_norm``: (the gradients scaled so that their global norm is at most max_norm, that norm as it was).
-    ``out`` is a list of tensors with the lengths and types of ``grads``, or ``grads`` itself (in place); default: new
-    tensors."""
+    ``out`` is a list of tensors with the lengths and types of ``grads``, or ``grads`` itself (in place; out[t] may be
+    grads[t], but no other gradient); default: new tensors."""
     import torch
     return _clip(grads, max_norm, [torch.empty_like(g) for g in grads] if out is None else out, workspace)
 
@@ -776,6 +777,13 @@ def clip_grad_norm(grads, max_norm, out=None, workspace=None):
 def grad_norm(grads, workspace=None):
     """The global norm alone (``hag_clip_grad_norm`` without outputs): a float32 tensor of one value."""
     return _clip(grads, float("inf"), None, workspace)[1]
+
+
+def _named_twice(ptrs, to, lens):
+    """Whether the address of a tensor that is not empty occurs twice in either list, or in both at different places."""
+    p, q = ([x for x, m in zip(at, lens) if m] for at in (ptrs, to))
+    a, b = set(p), set(q)
+    return len(a) != len(p) or len(b) != len(q) or len(a & b) != sum(map(eq, p, q))
 
 
 def _clip(grads, max_norm, out, workspace):
@@ -788,9 +796,8 @@ def _clip(grads, max_norm, out, workspace):
         to, to_lens, to_kinds = (ptrs, lens, kinds) if out is grads else _tensor_list(out, index)
         if to_lens != lens or to_kinds != kinds:
             raise ValueError("out must be tensors with the lengths and types of the gradients")
-        for at in (ptrs, to):
-            if len(set(at)) != count and len({p for p, m in zip(at, lens) if m}) != sum(m > 0 for m in lens):
-                raise ValueError("a tensor is named twice")
+        if len({*ptrs, *to}) != (count if out is grads else 2 * count) and _named_twice(ptrs, to, lens):
+            raise ValueError("a tensor is named twice, or an output is another tensor's gradient")
         to = array("Q", to)
     addresses, lengths, codes = array("Q", ptrs), array("q", lens), array("i", [_codes[k] for k in kinds])
     ws = _scratch_for(workspace, load_library().hag_clip_grad_norm_workspace_bytes(count), grads[0])

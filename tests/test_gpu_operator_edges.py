@@ -49,3 +49,20 @@ def test_more_columns_than_32_bits_are_refused():
         with pytest.raises(hb.HagError) as e:
             call()
         assert e.value.status == hb.HAG_ERR_TOO_LARGE
+
+
+def test_clipping_refuses_outputs_that_are_other_gradients():
+    a, b, c, none = _randn(3, 5000), _randn(4, 5000), _randn(5, 5000), torch.empty(0, device="cuda")
+    before = [t.clone() for t in (a, b, c)]
+    for grads, out in (([a, b], [b, a]), ([a, b], [c, a]), ([a, b, c], [b, c, a]), ([a, none, b], [b, none, c])):
+        with pytest.raises(ValueError):
+            hb.clip_grad_norm(grads, 0.1, out=out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, s) for t, s in zip((a, b, c), before))
+    # some in place and some not, and several empty ones, are fine
+    out, norm = hb.clip_grad_norm([a, none, none, b], 0.1, out=[a, none, none, c])
+    want = torch.cat(before[:2]).double()
+    assert abs(float(norm) - float(want.norm())) <= 33 * U * float(want.norm())
+    got = torch.cat([a, c]).double()
+    want *= 0.1 / (float(want.norm()) + 1e-6)
+    assert ((got - want).abs() <= 40 * U * want.abs() + 1e-45).all() and torch.equal(b, before[1])
