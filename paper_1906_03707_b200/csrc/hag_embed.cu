@@ -919,8 +919,11 @@ __global__ void __launch_bounds__(1024) table_join_kernel(const __grid_constant_
     }
 }
 
-constexpr int64_t kTileValues = 1 << 20;         // of a table
-constexpr int64_t kTileAlone = 1 << 16;          // of the result that one block clears by itself
+constexpr int64_t kTileValues = 1 << 20;         // of the result that one tile writes
+constexpr int64_t kTileTable = 1 << 17;          // of a table, where there are several
+// Of the values that one block clears by itself, its columns (at most 128 of fp32) of all the rows: alone and for up to
+// kTileLeast tokens, when the sort's second and third launch count; else.
+constexpr int64_t kTileAlone = 1 << 17, kTileShare = 5 << 14;
 // Tokens per tile of a short list.  256: 1000 x 16 into 100 rows takes 8.0 us, 4000 x 64 into 119 rows 8.9 us; with 1024
 // they take 8.8 and 11.4 us.
 constexpr int kTileLeast = 256, kTileMost = 2048;
@@ -929,12 +932,20 @@ constexpr int kTileBlocks = 148;
 // 8.0, but 2.7 us less on the host, which is what such calls wait for.
 constexpr int64_t kTileFew = 32768;
 
-// Tiles for a list, or 0 where the tables would be too large: all of them together up to 4 MB (they stay in the L2), or
-// a quarter of the gradient rows' values.
+// Tiles for a list, or 0: the sort.  A table costs its clearing, by one block per 128 columns, and its part of the join,
+// so that large tables lose however few the tokens are; the sort's zeros are written by up to 592 blocks.  In us, by tiles /
+// by the sort (up to 4096 ids whole calls with the host, else the device alone):
+//   one tile    64 ids into 1040 x 64 12.2 / 14.1, 2048 x 64 15.3 / 14.0, 16 384 x 64 74 / 14.1, 600 x 336 12.2 / 14.2, 1024 x 1024 15.4 / 14.1
+//               256 ids into 1040 x 64 12.2 / 16.4, 2048 x 64 16.1 / 16.1, 600 x 336 13.7 / 16.2; 1024 into 2050 x 32 13.7 / 16.1
+//   several     700 ids into 2048 x 64 20.7 / 16.3, 4096 into 2048 x 64 23.2 / 16.3
+//               8192 ids into 1024 x 64 18.6 / 24.7, 2048 x 64 26.3 / 26.5, 128 x 1024 18.6 / 22.2, 256 x 1024 25.6 / 26.4
+//               10^6 ids into 844 x 64 71 / 82, 1689 x 64 96 / 82, 422 x 128 77 / 87, 844 x 128 105 / 87, 1689 x 128 186 / 89
+// All tables together take up to 4 MB (they stay in the L2), or a quarter of the gradient rows' values.
 int tile_count(int32_t n, int32_t n_rows, int32_t D) {
-    const int64_t values = int64_t(n_rows) * D;
-    if ((n <= kTileLeast || (n <= kSortThreads && int64_t(n) * D <= kTileFew)) && values <= kTileAlone) return 1;
-    if (values > kTileValues) return 0;
+    const int64_t values = int64_t(n_rows) * D, columns = (int64_t(D) + 127) / 128;
+    if (values > kTileValues || values > (n <= kTileLeast ? kTileAlone : kTileShare) * columns) return 0;
+    if (n <= kTileLeast || (n <= kSortThreads && int64_t(n) * D <= kTileFew)) return 1;
+    if (values > kTileTable) return 0;
     const int64_t most = std::max<int64_t>(1 << 20, int64_t(n) * D / 4);
     const int64_t waves = (int64_t(n) + kTileBlocks * int64_t(kSortTile) - 1) / (kTileBlocks * int64_t(kSortTile));
     int64_t tiles = waves > 1 ? waves * kTileBlocks : std::min<int64_t>(kTileBlocks, (int64_t(n) + kTileLeast - 1) / kTileLeast);

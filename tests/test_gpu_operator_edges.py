@@ -1,4 +1,6 @@
 """Embedding, layer norm and clipping where sizes and values are extreme: against plain 64-bit forms, u = 2^-24."""
+import ctypes
+
 import pytest
 
 import paper_1906_03707_b200 as hb
@@ -66,3 +68,78 @@ def test_clipping_refuses_outputs_that_are_other_gradients():
     got = torch.cat([a, c]).double()
     want *= 0.1 / (float(want.norm()) + 1e-6)
     assert ((got - want).abs() <= 40 * U * want.abs() + 1e-45).all() and torch.equal(b, before[1])
+
+
+class _KernelNode(ctypes.Structure):
+    """CUDA_KERNEL_NODE_PARAMS of the driver interface."""
+    _fields_ = [("func", ctypes.c_void_p), ("grid", ctypes.c_uint * 3), ("block", ctypes.c_uint * 3), ("shared", ctypes.c_uint),
+                ("params", ctypes.c_void_p), ("extra", ctypes.c_void_p), ("kernel", ctypes.c_void_p), ("context", ctypes.c_void_p)]
+
+
+def _launches(call):
+    """[(kernel name, (x, y, z) blocks)] of what the call enqueues, read from a captured graph."""
+    call()                                                          # one-time setup outside the capture
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    cuda, raw, count = ctypes.CDLL("libcuda.so.1"), ctypes.c_void_p(graph.raw_cuda_graph()), ctypes.c_size_t()
+    assert cuda.cuGraphGetNodes(raw, None, ctypes.byref(count)) == 0
+    nodes = (ctypes.c_void_p * count.value)()
+    assert cuda.cuGraphGetNodes(raw, nodes, ctypes.byref(count)) == 0
+    out = []
+    for node in nodes:
+        kind, p, name = ctypes.c_int(), _KernelNode(), ctypes.c_char_p()
+        assert cuda.cuGraphNodeGetType(ctypes.c_void_p(node), ctypes.byref(kind)) == 0
+        if kind.value != 0:                                         # not a kernel
+            continue
+        assert cuda.cuGraphKernelNodeGetParams_v2(ctypes.c_void_p(node), ctypes.byref(p)) == 0
+        assert cuda.cuFuncGetName(ctypes.byref(name), ctypes.c_void_p(p.func)) == 0
+        out.append((name.value.decode(), tuple(p.grid)))
+    return out
+
+
+def _ids(seed, n, v, kind):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    if kind == "one":
+        return torch.full((n,), v // 2, device="cuda", dtype=torch.int32)
+    if kind == "skewed":
+        return (torch.rand(n, generator=gen, device="cuda", dtype=torch.float64) ** 6 * v).long().clamp(0, v - 1)
+    ids = torch.randint(0, v, (n,), generator=gen, device="cuda")
+    if kind == "holes":
+        ids = torch.where(torch.rand(n, generator=gen, device="cuda") < 0.3, -1, ids)
+        ids[::7] = v
+        ids[::13] = (1 << 40) + 1
+    return ids
+
+
+def _check_embedding_gradient(ids, grad, v, dtype):
+    """A row of k terms goes through at most k + 2 fp32 roundings, each 2^-24 of the sum of magnitudes; bf16 adds 2^-8."""
+    got = hb.embedding_bwd(ids, grad, v, scale=0.5, dtype=dtype)
+    key = ids.long()
+    ok = (key >= 0) & (key < v)
+    rows, place = torch.unique(key[ok], return_inverse=True)        # only the rows that are named: v may be large
+    g = grad[ok].double() * 0.5
+    want = torch.zeros(len(rows), grad.shape[1], device="cuda", dtype=torch.float64).index_add_(0, place, g)
+    mag = torch.zeros_like(want).index_add_(0, place, g.abs())
+    k = torch.bincount(place, minlength=len(rows)).double()[:, None]
+    bound = (k + 2) * U * mag + (2.0 ** -8 * want.abs() if dtype == BF16 else 0)
+    assert ((got[rows].double() - want).abs() <= bound).all()
+    got[rows] = 0
+    assert not got.any()
+
+
+@pytest.mark.parametrize("n,v,d", [(1, 16_384, 64), (64, 2048, 64), (64, 2049, 64), (64, 16_384, 64), (200, 65_536, 16), (256, 1024, 1024), (700, 1024, 512),
+                                   (1000, 2560, 32), (1000, 2561, 32), (2000, 16_384, 64), (2000, 1 << 20, 1), (2048, 8000, 128), (4096, 8000, 64),
+                                   (4978, 400, 336), (60_000, 1500, 128)])
+def test_no_block_clears_a_large_table_alone(n, v, d):
+    """2^17 values at most for a block of the embedding's gradient, 5 * 2^14 for more than 256 ids, and its result on both
+    sides of that."""
+    ids, grad = _ids(6, n, v, "uniform"), _randn(7, n, d)
+    launches = _launches(lambda: hb.embedding_bwd(ids, grad, v))
+    for name, grid in launches:
+        if "embedding_tile" in name:
+            assert v * d <= grid[1] * (1 << 17 if n <= 256 else 5 << 14), launches
+        if "sort_small" in name:
+            assert grid[0] > v * d * 4 >> 15                        # 32 KB of zeros per block besides the one that sorts
+    for kind, gdt, odt in (("holes", F32, F32), ("skewed", BF16, F32), ("one", F32, BF16)):
+        _check_embedding_gradient(_ids(8, n, v, kind), grad.to(gdt), v, odt)
