@@ -482,7 +482,7 @@ typedef enum { HAG_ID32 = 0, HAG_ID64 = 1 } hag_id_type; /* int32_t / int64_t id
  * nothing between calls.
  * ids, out / grad_out may be NULL when n = 0, the table when n_rows = 0.
  * Errors: NULL, ARG (D <= 0, n < 0, n_rows < 0, a stride, out == table), DTYPE (also id_type), ALIGN (pointer not on
- * its element), WORKSPACE, TOO_LARGE (D > 2^20, n_rows >= 2^31 - 1; backward: n >= 2^31 - 4096), CUDA. */
+ * its element), WORKSPACE, TOO_LARGE (D > 2^20, n_rows >= 2^31 - 1; backward: n >= 2^31 - 8192), CUDA. */
 hag_status hag_embedding_fwd(const void *ids, hag_id_type id_type, int64_t n, int64_t n_rows, const void *table,
                              hag_dtype table_dtype, int64_t ld_table, hag_dtype dtype, int32_t D, float scale, void *out,
                              int64_t ld_out, void *cuda_stream);
