@@ -2,7 +2,6 @@
 from __future__ import annotations
 
 import os
-import shutil
 import subprocess
 import sys
 import tempfile
@@ -35,9 +34,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(len(SOURCES)) as pool:
         objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
         list(pool.map(lambda p: subprocess.check_call(common + flags + ["-c", "-o", p[1], os.path.join(CSRC, p[0])]), zip(SOURCES, objects)))
-        linked = os.path.join(tmp, "library.so")
-        subprocess.check_call(common + ["-shared", "-o", linked] + objects + ["-ldl"])     # -ldl: the header-only NVTX ranges load their tool lazily
-        shutil.move(linked, LIB)
+        linked = f"{os.path.splitext(LIB)[0]}.{os.getpid()}.so"      # beside the library, whose place it takes in one step: a process
+        try:                                                         # that has the old file mapped keeps it
+            subprocess.check_call(common + ["-shared", "-o", linked] + objects + ["-ldl"])     # -ldl: the header-only NVTX ranges load their tool lazily
+            os.replace(linked, LIB)
+        finally:
+            if os.path.exists(linked):
+                os.remove(linked)
     return LIB
 
 
