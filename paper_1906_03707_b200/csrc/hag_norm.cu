@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(32 * kStripRows) norm_params_any_kernel(const 
 // ---------------------------------------------------------------------------------------------------------------
 // Rows read once.  A group of threads owns a row, K vectors of V elements per thread, and reads ahead of the rows it
 // works on.
-//   L = 8, 16, 32: that many lanes of a warp per row, R rows per group at a time
+//   L = 4, 8, 16, 32: that many lanes of a warp per row, R rows per group at a time
 //   L = 0 or -1  : a whole block per row (of up to kMostThreads or kFewThreads threads), sums over the block through
 //                  shared memory
 // The rows ahead are on their way into a ring in shared memory (asynchronous copies), so what is in flight does not
@@ -597,7 +597,9 @@ __global__ void __launch_bounds__(kThreads<L>, (L > 0 ? kFwdBlocks<L, V, K, EDGE
                 s[i] += x[i][k].sum();                         // places beyond the row hold zeros
             }
         }
-        const float my_mean = group_sums<L, R>(s, first, slots[0]) / cols;     // a division: constant rows give exact zeros
+        // divided, not times 1 / D: where the row's sum is exact, the mean of equal values is that value and y the bias
+        // (else, as of 72 times 1000.1, the mean is off by the sum's rounding, and rstd is up to 1 / sqrt(eps))
+        const float my_mean = group_sums<L, R>(s, first, slots[0]) / cols;
         ahead.template done<false>();
         edge_read = edge.next(edge_read);
         issue(turn + p.stages);                                // into the stage just read

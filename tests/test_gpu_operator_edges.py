@@ -143,3 +143,21 @@ def test_no_block_clears_a_large_table_alone(n, v, d):
             assert grid[0] > v * d * 4 >> 15                        # 32 KB of zeros per block besides the one that sorts
     for kind, gdt, odt in (("holes", F32, F32), ("skewed", BF16, F32), ("one", F32, BF16)):
         _check_embedding_gradient(_ids(8, n, v, kind), grad.to(gdt), v, odt)
+
+
+@pytest.mark.parametrize("value", [0.1, 1000.1, -3e-5])
+@pytest.mark.parametrize("d", [9, 72, 100, 333, 384, 1433, 20_001])
+def test_constant_rows_whose_sum_is_rounded(value, d):
+    """The mean is off by at most h u |value|, h = 64 + d/256 the longest chain of additions, plus its own rounding, and all
+    differences from it by as much; y is that times rstd, which is 1 / sqrt(eps) at most.  Given that mean, the variance is
+    the square of the difference, and rstd good to (h/2 + 10) u."""
+    x = torch.full((6, d), value, device="cuda")
+    eps = 1e-5
+    y, mean, rstd = hb.layer_norm_fwd(x, eps=eps)
+    dm = (65 + d / 256) * U * abs(value)
+    assert ((mean.double() - x[:, 0].double()).abs() <= dm).all() and (rstd <= eps ** -0.5 * (1 + 8 * U)).all()
+    assert (y.double().abs() <= dm * eps ** -0.5 * (1 + 12 * U)).all()
+    want = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    assert ((y.double() - want).abs() <= 4 * U * want.abs()).all()
+    off = x[:, 0].double() - mean.double()
+    assert ((rstd.double() * (off.square() + eps).sqrt() - 1).abs() <= (42 + d / 512) * U).all()
