@@ -161,3 +161,55 @@ def test_constant_rows_whose_sum_is_rounded(value, d):
     assert ((y.double() - want).abs() <= 4 * U * want.abs()).all()
     off = x[:, 0].double() - mean.double()
     assert ((rstd.double() * (off.square() + eps).sqrt() - 1).abs() <= (42 + d / 512) * U).all()
+
+
+def test_parameter_gradients_beyond_32_bits():
+    """gw and gb of 2.46e9 elements: no chain of additions over n rows is longer than k = 128 + n/32, so (4 + k) u of the
+    sum of magnitudes for gw and k u for gb."""
+    n, d = 150_000, 16_384
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.empty(n, d, dtype=BF16, device="cuda").normal_(generator=gen)
+    g = torch.empty(n, d, dtype=BF16, device="cuda").normal_(generator=gen)
+    y, mean, rstd = hb.layer_norm_fwd(x)
+    gx, gw, gb = hb.layer_norm_bwd(g, x, mean, rstd, out=y)
+    sums = torch.zeros(4, d, device="cuda", dtype=torch.float64)
+    for a in range(0, n, 5000):
+        gd = g[a:a + 5000].double()
+        t = gd * (x[a:a + 5000].double() - mean[a:a + 5000].double()[:, None]) * rstd[a:a + 5000].double()[:, None]
+        sums += torch.stack([t.sum(0), t.abs().sum(0), gd.sum(0), gd.abs().sum(0)])
+    k = 128 + n / 32
+    assert ((gw.double() - sums[0]).abs() <= (4 + k) * U * sums[1]).all() and ((gb.double() - sums[2]).abs() <= k * U * sums[3]).all()
+
+
+@pytest.mark.parametrize("n,v,d,ld", [(9000, 50, 16, 300_000), (200, 30, 24, 15_000_000)])
+def test_table_gradient_of_few_rows_beyond_32_bits(n, v, d, ld):
+    """Gradient rows so far apart that their offsets pass 32 bits, in tiles and in one tile."""
+    wide = torch.empty(n, ld, dtype=BF16, device="cuda")
+    grad = wide[:, 5:5 + d]
+    grad.copy_(_randn(10, n, d))
+    ids = _ids(11, n, v, "uniform")
+    assert any("embedding_tile" in name for name, _ in _launches(lambda: hb.embedding_bwd(ids, grad, v)))
+    for kind in ("uniform", "holes"):
+        _check_embedding_gradient(_ids(11, n, v, kind), grad, v, F32)
+
+
+@pytest.mark.parametrize("kind", ["uniform", "one", "skewed", "holes"])
+@pytest.mark.parametrize("n,v,d", [(1, 50_257, 64), (65, 50_257, 33), (300, 50_257, 96), (1024, 40_000, 40), (1025, 70_000, 20), (4096, 50_257, 128),
+                                   (8192, 1 << 18, 8), (8191, 20_000, 333), (5001, 300_001, 5), (700, 1 << 21, 1)])
+def test_short_lists_into_large_tables(kind, n, v, d):
+    """All passes of the sort in one launch, from one key per thread to eight, one to three digits."""
+    ids, grad = _ids(13, n, v, kind), _randn(12, n, d)
+    assert any("sort_small" in name for name, _ in _launches(lambda: hb.embedding_bwd(ids, grad, v)))
+    for gdt, odt in ((F32, F32), (BF16, F32), (F32, BF16)):
+        _check_embedding_gradient(ids, grad.to(gdt), v, odt)
+
+
+@pytest.mark.parametrize("n", [6000, 100_001])
+def test_four_digits(n):
+    """2^25 rows, 26 bits of key in four passes, in one launch and in two per pass; among the ids the first and the last."""
+    v = 1 << 25
+    ids = _ids(14, n, v, "uniform")
+    ids[5], ids[77], ids[n - 1], ids[n - 2] = 0, v - 1, v - 1, -1
+    ids[100:1100] = 1 << 24
+    for d in (1, 2):
+        _check_embedding_gradient(ids, _randn(15, n, d), v, F32)
