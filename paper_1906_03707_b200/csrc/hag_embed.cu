@@ -796,7 +796,7 @@ __global__ void __launch_bounds__(kSortThreads) embedding_tile_kernel(const __gr
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k)
             if (k < items) pair[k] = mine + 32 * k < len ? sort_pair(p.sort, begin + mine + 32 * k) : make_uint2(0xffffffffu, 0);
-        // rows that no token of the tile names: cleared while the ids are on their way
+        // while the ids are on their way: what the sums will read first, asked into the L2 ...
         if (p.partial) {
             constexpr int kLine = 128;
             const int from = blockIdx.y * p.lanes * V, bytes = min(p.D - from, p.lanes * V) * int(sizeof(TG));
@@ -807,6 +807,7 @@ __global__ void __launch_bounds__(kSortThreads) embedding_tile_kernel(const __gr
                 asm volatile("prefetch.global.L2 [%0];" ::"l"(first + row * p.ld_grad * int64_t(sizeof(TG)) + (i - row * per_row) * kLine));
             }
         }
+        // ... and zeros for all rows, of which those that tokens name are written again
         const int vec = blockIdx.y * p.lanes + t % p.lanes;
         const float zeros[V] = {};
         if (vec < p.D / V)
