@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <cstdint>
 #include <type_traits>
 
@@ -687,7 +688,10 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
     };
     // The rows' statistics: each lane of a group (or warp) reads those of another turn, S turns at once and S turns
     // ahead, and hands them round when the turn comes.
+    // Beyond the row xh is (0 - mean) * rstd: where that overflows, 0 times it is no number, and `careful` turns take the
+    // sum again without those places.
     float mean[R], rstd[R], mean_next[R], rstd_next[R];
+    bool careful = false;
     auto statistics = [&](int32_t turn) {
         const int32_t mine = turn + lane % S;
         const int64_t at = turns.row + int64_t(mine) * turns.stride;
@@ -711,11 +715,14 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
     if (L > 0 && weights.kShared) __syncthreads();
     for (int32_t turn = 0; turn < turns.all; ++turn) {
         if (turn % S == 0) {
+            bool overflows = false;
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 mean[i] = mean_next[i];
                 rstd[i] = rstd_next[i];
+                overflows |= !(fabsf(mean[i] * rstd[i]) <= FLT_MAX);
             }
+            careful = __any_sync(0xffffffffu, overflows);
             statistics(turn + S);
         }
         ahead.wait(p.stages);
@@ -751,12 +758,10 @@ __global__ void __launch_bounds__(kThreads<L>, (kLeastBlocks<T, L, V, K, true>))
                     gw[i][k] = t;
                 }
             }
-            // beyond the row xh is (0 - mean) * rstd: where that overflows, 0 times it is no number, and the sum is
-            // taken again without those places (280 bf16 columns, the worst case: 98 us with this test per row, 105 with a
-            // selection per vector, 95 without either)
-            if (__builtin_expect(s[2 * i + 1] != s[2 * i + 1], 0)) {
+            if (careful) {
+                constexpr int kTimes = !HOLD && kShared<T, L, V, K, EDGE> ? 1 : K;         // a rare loop: no registers for it
                 s[2 * i + 1] = ge[i] * xe[i];
-#pragma unroll
+#pragma unroll kTimes
                 for (int k = 0; k < K; ++k) {
                     Pairs<V> a, t;
                     if constexpr (HOLD) {
