@@ -8,10 +8,12 @@
 // stretch of them.  No atomics on floats: the same inputs give the same bits.
 //
 // Both are bound by memory.  Measured on B200 (copy rate 6.45 TB/s): lookup of 500 000 x 64 fp32 from 119 rows 23 us (the
-// 128 MB written at 5.6 TB/s), of 10^6 x 256 fp32 into bf16 from 50 257 rows 138 us (it reads 1 GB out of the L1 and L2
-// besides 591 MB of DRAM traffic).  Gradient of 500 000 x 64 fp32 into 119 rows 29 us (128 MB read); of 10^6 x 256 bf16 into
-// 50 257 fp32 rows 151 us: 94 for the sums (512 MB read, 51 MB written), 9 for the joins, 48 for two sorting passes and
-// the zeros.
+// 128 MB written at 5.6 TB/s), of 10^6 x 256 fp32 into bf16 from 50 257 rows 140 us (1 GB of rows out of the L1 and L2
+// besides 543 MB of DRAM traffic; none of the three is above half of its rate: the warps, 32 per SM at 64 registers, wait
+// for their rows half of the time).  Gradient of 500 000 x 64 fp32 into 119 rows 29 us (128 MB read); of 10^6 x 256 bf16
+// into 50 257 fp32 rows 151 us: 94 for the sums (512 MB read, 51 MB written), 9 for the joins, 48 for two sorting passes
+// and the zeros; of 4096 x 768 bf16 into that table, which is mostly zeros, 39 us.  Widths without 16-byte vectors go by 4
+// or 2 bytes: lookup of 300 000 x 333 106 us, fp32 and bf16 alike.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -730,11 +732,10 @@ int64_t partial_floats(int64_t n, int32_t D) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Few rows: no sort of the whole list (500 000 x 64 into 119 rows takes 29 us this way and 52 by the sort, 100 000 x 64 13
-// and 32; 10^6 x 128 into 3000 rows would take 294 us and takes 120 by the sort: its tables are larger than its rows).
-// Every block sorts a tile of the tokens in shared memory, adds up its runs as
-// above (its groups of lanes are the workers, heads and tails stay in shared memory), and leaves a table of its own:
-// all rows, its columns.  table_join_kernel adds up the blocks' tables in order.  One tile alone writes the result.
+// Few rows (tile_count says which): no sort of the whole list (500 000 x 64 into 119 rows takes 29 us this way and 52 by
+// the sort, 100 000 x 64 13 and 32).  Every block sorts a tile of the tokens in shared memory, adds up its runs as above
+// (its groups of lanes are the workers, heads and tails stay in shared memory), and leaves a table of its own: all rows,
+// its columns.  table_join_kernel adds up the blocks' tables in order.  One tile alone writes the result.
 struct TileArgs {
     SortArgs sort;               // ids, n, digits; stretch: tokens per tile
     const void *grad;
@@ -749,7 +750,7 @@ struct TileArgs {
     int32_t parts;
     hagr::Divisor per_row;       // the pitch (table_join_kernel)
 };
-constexpr int kTileBatch = 4;    // rows in flight per worker: 32 warps of them
+constexpr int kTileBatch = 4;    // rows in flight per worker: 32 warps of them (at 64 registers, with 32 bytes spilled by the sort)
 // Of a tile's gradient rows, what is asked into the L2 while the ids are sorted, when the memory would be idle: 500 000 x 64
 // into 119 rows takes 29.2 us with it and 32.8 without (128 KB 29.7, 384 KB 29.9).  In the launches of the full sort the
 // same slowed the sort by what it saved.

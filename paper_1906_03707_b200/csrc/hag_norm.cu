@@ -9,7 +9,8 @@
 // against a copy at 6.45 TB/s: forward 233 000 x 128 fp32 40 us (5.96 TB/s), 10^6 x 256 bf16 160 us (6.45), 32 768 x 4096
 // bf16 102 us (5.3); backward with both parameter gradients 10^6 x 256 bf16 232 us in isolation (6.65) and 260 us in a long
 // run (5.9), 200 000 x 512 fp32 206 us (6.0).  Contiguous rows of odd widths: 200 000 x 501 fp32 forward 138 us (5.8),
-// 300 000 x 333 backward fp32 198 us (6.1), bf16 175 (3.4: bound by instructions, as is its forward, 139 us).
+// 300 000 x 333 backward fp32 198 us (6.1), bf16 177 (3.4; forward 139 us): there the two warps of a scheduler wait for their
+// own instructions, half of its slots are empty, and the memory is at a third of its rate.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -182,7 +183,8 @@ __global__ void __launch_bounds__(32 * kStripRows) norm_params_any_kernel(const 
 //   Pieces : else.  Rows are copied as the 16-byte pieces they touch, and the group reads narrow vectors out of those
 //            at any place.  (300 000 x 333 bf16: forward 177 us, by EDGE 139; backward 286, by EDGE 175.)
 // The weights stay with the thread over all its rows: in registers, or from 16 columns per thread on in shared memory.
-constexpr int kMostThreads = 1024;        // of a block per row; up to kFewThreads the compiler may use 128 registers
+constexpr int kMostThreads = 1024;        // of a block per row; up to kFewThreads the compiler may use 128 registers (with more
+                                          // threads the backward pass with 16 narrow columns each spills 116 bytes)
 constexpr int kFewThreads = 512;
 // Stages of the ring.  What is in flight per SM matters more than how many warps are there: about 64 KB (one block of
 // eight warps, 64 bytes per lane and turn) is best; with three blocks 10^6 x 256 bf16 forward takes 196 us, with one 160.
@@ -997,9 +999,10 @@ cudaError_t launch_rows(NormArgs &p, cudaStream_t s) {
 // with 16 lanes and one, in 121 with 32 (backward 65, 96, 185); 1 175 089 x 29 fp32 in 61 with 8 lanes, 69 with 16, 115
 // with 32; 775 089 x 49 bf16 in 66 with 16 lanes, 71 with 8, 96 with 32.  Wide vectors are near the memory's rate with
 // one each, but where they leave most of the lanes without one: 1 047 213 x 8 bf16 in 20 us with 4 lanes, 41 with 8
-// (backward 35 and 60), 32 bf16 in 25 and 42.  Narrow rows of 280 bf16 backward, 123 218 of them, take 95 us with 12
+// (backward 35 and 60), 32 bf16 in 25 and 42.  Narrow rows of 280 bf16 backward, 123 218 of them, take 97 us with 12
 // columns per lane, 117 with 16 and 123 with a block per row (forward 60, 75 with 16); 500 fp32 130 with 16, 140 with a
-// block; 223 218 x 150 fp32 84 with 6, 132 with 8; 423 218 x 80 fp32 90 with 3, 123 with 4.
+// block; 223 218 x 150 fp32 86 with 6, 132 with 8; 423 218 x 80 fp32 92 with 3, 123 with 4.
+// Rows of more columns are read one element at a time: 4000 x 32 768 bf16 614 us forward and 872 backward.
 constexpr int kPerThread = 16;
 template <typename T, int V, bool BWD, bool EDGE = false>
 cudaError_t launch_width(NormArgs &p, cudaStream_t s) {
