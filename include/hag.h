@@ -530,6 +530,81 @@ hag_status hag_clip_grad_norm(int32_t count, const void *const *grads, void *con
                               const hag_dtype *dtypes, float max_norm, float *total_norm, void *workspace,
                               void *cuda_stream);
 
+/* Root-mean-square norm over the D columns of each of n rows, with the addition of the residual stream in front of it.
+ *   forward : h = x + residual (residual NULL: h = x), rstd = 1 / sqrt(sum h^2 / D + eps), y = h * rstd * weight.
+ *             h is added in fp32; rstd and y are those of the sum as it is, `total` receives it rounded to its type.
+ *   forward with an 8-bit output: instead of y, q = round(y / scale) and the scales, one per `block` columns (32, 64 or
+ *             128; the last one of a row may have fewer) or, with block 0, one per row: scale = max(|y|) / top, at least
+ *             2^-126, top = 448 (HAG_E4M3) or 127 (HAG_I8).  scales: n x ceil(D / block), contiguous.  The quotient is
+ *             good to 2^-21 before it is rounded.  A block with a y that is not finite gets a scale that is not finite.
+ *   backward: with hh = total * rstd and t = grad_y * weight: grad = rstd * (t - hh * sum(t * hh) / D) + grad_total is the
+ *             gradient of x and of the residual alike, grad_weight = sum over rows of grad_y * hh.  grad_total: what
+ *             arrives along the residual stream (NULL: nothing).
+ * Types: x of x_dtype, residual, total, grad_total and grad_residual of stream_dtype, y and grad_y of y_dtype.  Allowed
+ * (x, stream, y): all of one type; bf16 around an fp32 stream (bf16, fp32, bf16); (fp32, fp32, bf16).  Without a residual
+ * x_dtype must be stream_dtype.  weight and grad_weight: D values of weight_dtype; weight NULL stands for ones.
+ *   total and rstd may be NULL (not wanted).  grad_x: the gradient once more, in bf16, where x is narrower than an fp32
+ * stream; else NULL.  grad_weight may be NULL; with n = 0 it is zeros.
+ * In place (same pointer, type and row stride): y or total in the place of x or residual; grad_residual in the place of
+ * grad_total, total or grad_y.
+ * Squares are fp32: magnitudes above 1.8e19 give rstd = 0.
+ * hag_rms_norm_bwd_workspace_bytes: 16-byte aligned scratch, needed when grad_weight is wanted; carries nothing between
+ * calls.
+ * Errors: NULL, ARG (n < 0, D <= 0, eps negative or no number, a stride, block, kind), DTYPE, ALIGN (pointer not on its
+ * element), WORKSPACE, TOO_LARGE (D > 2^30), CUDA. */
+typedef enum { HAG_E4M3 = 0, HAG_I8 = 1 } hag_quant;
+hag_status hag_rms_norm_fwd(int64_t n, int32_t D, const void *x, hag_dtype x_dtype, int64_t ld_x, const void *residual,
+                            hag_dtype stream_dtype, int64_t ld_residual, const void *weight, hag_dtype weight_dtype, float eps,
+                            void *y, hag_dtype y_dtype, int64_t ld_y, void *total, int64_t ld_total, float *rstd, void *cuda_stream);
+hag_status hag_rms_norm_quant_fwd(int64_t n, int32_t D, const void *x, hag_dtype x_dtype, int64_t ld_x, const void *residual,
+                                  hag_dtype stream_dtype, int64_t ld_residual, const void *weight, hag_dtype weight_dtype,
+                                  float eps, hag_quant kind, int32_t block, void *q, int64_t ld_q, float *scales, void *total,
+                                  int64_t ld_total, float *rstd, void *cuda_stream);
+size_t hag_rms_norm_bwd_workspace_bytes(int64_t n, int32_t D);
+hag_status hag_rms_norm_bwd(int64_t n, int32_t D, const void *grad_y, hag_dtype y_dtype, int64_t ld_grad_y, const void *total,
+                            hag_dtype stream_dtype, int64_t ld_total, const float *rstd, const void *weight,
+                            hag_dtype weight_dtype, const void *grad_total, int64_t ld_grad_total, void *grad_residual,
+                            int64_t ld_grad_residual, void *grad_x, int64_t ld_grad_x, void *grad_weight, void *workspace,
+                            void *cuda_stream);
+
+/* One step of Adam with decoupled weight decay (AdamW) over a list of tensors, in place.  With t the number of the step
+ * (1 for the first), g = c * grads_i, c = min(1, max_norm / (*total_norm + 1e-6)), or 1 where total_norm is NULL:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr decay_i) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
+ * params, param_dtypes, grads, grad_dtypes, copies, lengths, decays: HOST arrays of `count` entries (read during the call,
+ * not kept); params[i] and grads[i]: DEVICE pointers to lengths[i] contiguous elements.  grads[i] NULL: tensor i and its
+ * states stay as they are.  copies (may be NULL, and so may its entries): copies[i] receives the new parameters in bf16.
+ * No two tensors may overlap, and no tensor may be named twice, but that grads may share memory.
+ * The states of all tensors lie in one array of blocks of HAG_ADAMW_BLOCK elements, the blocks of tensor i behind those of
+ * tensor i - 1, ceil(lengths[i] / HAG_ADAMW_BLOCK) of them; hag_adamw_state_blocks gives their number (-1 on bad
+ * arguments).  Places behind a tensor's end are neither read nor written.
+ * Before the first step everything is zeros.
+ *   HAG_STATE32: mean is m, square is v, both fp32; scales is not used.
+ *   HAG_STATE8 : mean is m, square is sqrt(v), both as e4m3 with a scale per block: scales[2 b] and scales[2 b + 1] are
+ *                those of block b.  scale = largest finite magnitude / 448, at least 2^-126; each value is rounded to
+ *                nearest after the step has been taken with the new m and v in fp32; a positive root is stored as 2^-9
+ *                at least; a value that is not finite is stored as NaN and does not touch the rest of its block.
+ * options: numbers that change from step to step may be given on the device, so that a captured call replays with new
+ * ones: lr_device in the place of lr, step_device in the place of step (read by the call; who counts it up is the caller;
+ * a step below 1 counts as 1).
+ * Errors: NULL, ARG (count < 0, a negative length or decay, lr or max_norm negative or no number, a beta outside [0, 1), eps
+ * negative or no number, step < 1), DTYPE, ALIGN (pointer not on its element; states not on 16 bytes, scales not on 8),
+ * TOO_LARGE (a tensor of more than 2^39 - 256 elements), CUDA. */
+#define HAG_ADAMW_BLOCK 256
+typedef enum { HAG_STATE32 = 0, HAG_STATE8 = 1 } hag_state_type;
+typedef struct hag_adamw_options {
+    double lr, beta1, beta2, eps, max_norm;
+    int64_t step;
+    const float *lr_device;
+    const int64_t *step_device;
+    const float *total_norm;
+} hag_adamw_options;
+int64_t hag_adamw_state_blocks(int32_t count, const int64_t *lengths);
+hag_status hag_adamw_step(int32_t count, void *const *params, const hag_dtype *param_dtypes, const void *const *grads,
+                          const hag_dtype *grad_dtypes, void *const *copies, const int64_t *lengths, const double *decays,
+                          hag_state_type state, void *mean, void *square, float *scales, const hag_adamw_options *options,
+                          void *cuda_stream);
+
 /* Number of kernels the last aggregate call on this handle enqueued. */
 int32_t hag_last_launch_count(const hag_t *h);
 

@@ -11,9 +11,11 @@ library is missing the first call raises.
     gx = h.aggregate_bwd(grad_out, reduce="mean")
 
 Around the aggregation, without a handle: ``embedding_fwd`` / ``embedding_bwd``,
-``layer_norm_fwd`` / ``layer_norm_bwd``, ``graph_pool_fwd`` / ``graph_pool_bwd``,
-``clip_grad_norm`` and ``grad_norm``; ``examples/graph_classification.py`` trains
-with all of them.
+``layer_norm_fwd`` / ``layer_norm_bwd``, ``rms_norm_fwd`` / ``rms_norm_bwd`` with
+the residual's addition and ``rms_norm_quant_fwd`` with an 8-bit output,
+``graph_pool_fwd`` / ``graph_pool_bwd``, ``clip_grad_norm``, ``grad_norm`` and
+``adamw_step``.  ``examples/graph_classification.py`` and
+``examples/residual_adamw.py`` train with them.
 """
 from __future__ import annotations
 
@@ -21,6 +23,7 @@ import ctypes
 import os
 from array import array
 from operator import eq
+from typing import NamedTuple, Optional
 
 import numpy as np
 
@@ -30,6 +33,9 @@ LIB_PATH = os.path.join(_HERE, "libhag_b200.so")
 HAG_SUM, HAG_MEAN, HAG_GCN = 0, 1, 2
 HAG_F32, HAG_BF16 = 0, 1
 HAG_ID32, HAG_ID64 = 0, 1
+HAG_E4M3, HAG_I8 = 0, 1
+HAG_STATE32, HAG_STATE8 = 0, 1
+HAG_ADAMW_BLOCK = 256
 (HAG_OK, HAG_ERR_NULL, HAG_ERR_ARG, HAG_ERR_GRAPH, HAG_ERR_OOM_HOST, HAG_ERR_OOM_DEVICE, HAG_ERR_CUDA, HAG_ERR_DTYPE,
  HAG_ERR_ALIGN, HAG_ERR_WORKSPACE, HAG_ERR_TIMEOUT, HAG_ERR_NOT_ON_DEVICE, HAG_ERR_TOO_LARGE) = range(13)
 
@@ -42,6 +48,8 @@ EXPORTED_SYMBOLS = [
     "hag_embedding_fwd", "hag_embedding_bwd_workspace_bytes", "hag_embedding_bwd",
     "hag_layer_norm_fwd", "hag_layer_norm_bwd_workspace_bytes", "hag_layer_norm_bwd",
     "hag_clip_grad_norm_workspace_bytes", "hag_clip_grad_norm",
+    "hag_rms_norm_fwd", "hag_rms_norm_quant_fwd", "hag_rms_norm_bwd_workspace_bytes", "hag_rms_norm_bwd",
+    "hag_adamw_state_blocks", "hag_adamw_step",
 ]
 
 
@@ -78,6 +86,11 @@ class HagArrays(ctypes.Structure):
                                        "trace", "csr_t_ptr", "csr_t_idx")] + [
         ("fwd_cut", ctypes.c_int32), ("bwd_cut", ctypes.c_int32)] + [
         (k, ctypes.c_void_p) for k in ("ftail_ptr", "ftail_idx", "btail_ptr", "btail_idx")]
+
+
+class HagAdamwOptions(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_double) for k in ("lr", "beta1", "beta2", "eps", "max_norm")] + [("step", ctypes.c_int64)] + [
+        (k, ctypes.c_void_p) for k in ("lr_device", "step_device", "total_norm")]
 
 
 _lib = None
@@ -178,6 +191,18 @@ def load_library():
     lib.hag_clip_grad_norm_workspace_bytes.restype = size
     lib.hag_clip_grad_norm.argtypes = [i32, vp, vp, vp, vp, f32, vp, vp, vp]
     lib.hag_clip_grad_norm.restype = code
+    lib.hag_rms_norm_fwd.argtypes = [i64, i32, vp, code, i64, vp, code, i64, vp, code, f32, vp, code, i64, vp, i64, vp, vp]
+    lib.hag_rms_norm_fwd.restype = code
+    lib.hag_rms_norm_quant_fwd.argtypes = [i64, i32, vp, code, i64, vp, code, i64, vp, code, f32, code, i32, vp, i64, vp, vp, i64, vp, vp]
+    lib.hag_rms_norm_quant_fwd.restype = code
+    lib.hag_rms_norm_bwd_workspace_bytes.argtypes = [i64, i32]
+    lib.hag_rms_norm_bwd_workspace_bytes.restype = size
+    lib.hag_rms_norm_bwd.argtypes = [i64, i32, vp, code, i64, vp, code, i64, vp, vp, code, vp, i64, vp, i64, vp, i64, vp, vp, vp]
+    lib.hag_rms_norm_bwd.restype = code
+    lib.hag_adamw_state_blocks.argtypes = [i32, vp]
+    lib.hag_adamw_state_blocks.restype = i64
+    lib.hag_adamw_step.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, code, vp, vp, vp, ctypes.POINTER(HagAdamwOptions), vp]
+    lib.hag_adamw_step.restype = code
     lib.hag_status_str.argtypes = [ctypes.c_int]
     lib.hag_status_str.restype = ctypes.c_char_p
     _lib = lib
@@ -754,7 +779,7 @@ def layer_norm_bwd(grad_out, x, mean, rstd, weight=None, out=None, param_grads=T
     return out, gw, gb
 
 
-def _tensor_list(tensors, index):
+def _tensor_list(tensors, index, what="gradients"):
     """Addresses, lengths and types of a list of contiguous device tensors."""
     import torch
     T = torch.Tensor                                            # a loop inside map costs half of one in Python
@@ -762,7 +787,7 @@ def _tensor_list(tensors, index):
     for k in set(kinds):
         _code(k)
     if not all(map(T.is_contiguous, tensors)) or set(map(T.get_device, tensors)) != {index}:
-        raise ValueError(f"gradients must be contiguous tensors on cuda:{index}")
+        raise ValueError(f"{what} must be contiguous tensors on cuda:{index}")
     return list(map(T.data_ptr, tensors)), list(map(T.numel, tensors)), kinds
 
 
@@ -805,3 +830,218 @@ def _clip(grads, max_norm, out, workspace):
     _call("hag_clip_grad_norm", index, count, addresses.buffer_info()[0], None if out is None else to.buffer_info()[0],
           lengths.buffer_info()[0], codes.buffer_info()[0], max_norm, norm.data_ptr(), ws.data_ptr())
     return out, norm
+
+
+# -- a residual stack and its optimiser: root-mean-square norm, AdamW -------------------------------------------------- #
+def _rms_inputs(x, weight, residual, total_out, eps):
+    """What the forward calls share: (device index, rows, columns, x's and the weight's arguments, the stream's type, its
+    matrix for the sum (x where there is no residual), the sum's arguments)."""
+    ld = _rows(x, "x")
+    index, shape, dtype = x.get_device(), x.shape, x.dtype
+    n, d = shape
+    if weight is None:
+        w, wcode = None, HAG_F32
+    else:
+        w, wcode = _vector(weight, "weight", d, index), _code(weight.dtype)
+    if residual is None:
+        if total_out is not None:
+            raise ValueError("total_out is the sum of x and a residual, which is missing")
+        return index, n, d, (x.data_ptr(), _code(dtype), ld, None, _code(dtype), 0, w, wcode, eps), x, (None, 0)
+    ld_res, stream = _rows(residual, "residual", shape, index), residual.dtype
+    if total_out is None:
+        total_out = residual.new_empty((n, d))
+        ld_total = d
+    else:
+        ld_total = _rows(total_out, "total_out", shape, index, stream)
+    return (index, n, d, (x.data_ptr(), _code(dtype), ld, residual.data_ptr(), _code(stream), ld_res, w, wcode, eps), total_out,
+            (total_out.data_ptr(), ld_total))
+
+
+def rms_norm_fwd(x, weight=None, residual=None, eps=1e-5, out=None, total_out=None, dtype=None, stats=True):
+    """``hag_rms_norm_fwd`` over the columns of total = x + residual.  Returns (y, total, rstd): y is of ``dtype`` (default:
+    x's type; bfloat16 is possible for float32), total of the residual's type, and x itself without a residual; rstd is
+    None where ``stats`` is false (no gradient wanted).  ``out`` and ``total_out`` may be x or the residual."""
+    import torch
+    index, n, d, args, total, total_args = _rms_inputs(x, weight, residual, total_out, eps)
+    if out is None:
+        out = x.new_empty((n, d), dtype=dtype or x.dtype)
+        ld_out = d
+    else:
+        ld_out = _rows(out, "out", (n, d), index, dtype)
+    rstd = x.new_empty(n, dtype=torch.float32) if stats else None
+    _call("hag_rms_norm_fwd", index, n, d, *args, out.data_ptr(), _code(out.dtype), ld_out, *total_args,
+          None if rstd is None else rstd.data_ptr())
+    return out, total, rstd
+
+
+_quant_codes = {}
+
+
+def _quant_code(dtype):
+    import torch
+    if not _quant_codes:
+        _quant_codes.update({torch.float8_e4m3fn: HAG_E4M3, torch.int8: HAG_I8})
+    code = _quant_codes.get(dtype)
+    if code is None:
+        raise TypeError(f"8-bit outputs are float8_e4m3fn or int8, got {dtype}")
+    return code
+
+
+def rms_norm_quant_fwd(x, weight=None, residual=None, eps=1e-5, block=0, dtype=None, out=None, scales=None, total_out=None, stats=True):
+    """``hag_rms_norm_quant_fwd``: as ``rms_norm_fwd``, with y in 8 bits (``dtype``: torch.float8_e4m3fn, the default, or
+    torch.int8) and a float32 scale per row (``block`` 0) or per ``block`` columns (32, 64 or 128).  Returns
+    (q, scales, total, rstd); y is q * scales, whose shape is n x ceil(columns / block)."""
+    import torch
+    index, n, d, args, total, total_args = _rms_inputs(x, weight, residual, total_out, eps)
+    if block not in (0, 32, 64, 128):
+        raise ValueError(f"block must be 0, 32, 64 or 128, got {block!r}")
+    if out is None:
+        out = x.new_empty((n, d), dtype=dtype or torch.float8_e4m3fn)
+        ld_out = d
+    else:
+        ld_out = _rows(out, "out", (n, d), index, dtype)
+    kind = _quant_code(out.dtype)
+    shape = (n, -(-d // block) if block else 1)
+    if scales is None:
+        scales = x.new_empty(shape, dtype=torch.float32)
+    elif scales.shape != shape or scales.dtype is not torch.float32 or not scales.is_contiguous() or scales.get_device() != index:
+        raise ValueError(f"scales must be a contiguous float32 tensor of shape {shape} on cuda:{index}")
+    rstd = x.new_empty(n, dtype=torch.float32) if stats else None
+    _call("hag_rms_norm_quant_fwd", index, n, d, *args, kind, block, out.data_ptr(), ld_out, scales.data_ptr(), *total_args,
+          None if rstd is None else rstd.data_ptr())
+    return out, scales, total, rstd
+
+
+def rms_norm_bwd(grad_out, total, rstd, weight=None, grad_total=None, out=None, x_dtype=None, param_grads=True, param_dtype=None,
+                 workspace=None):
+    """``hag_rms_norm_bwd``: (grad_x, grad_residual, grad_weight) from what ``rms_norm_fwd`` (or ``rms_norm_quant_fwd``)
+    returned and the gradient ``grad_total`` that arrives at the sum along the residual stream.  grad_residual is of total's
+    type; grad_x is the same tensor, or a second one in bfloat16 where ``x_dtype`` says that x was narrower than a float32
+    stream.  grad_weight is of the weight's type (without a weight: ``param_dtype``, default float32), and None where
+    ``param_grads`` is false.  ``out`` receives grad_residual; it may be grad_total, total or grad_out."""
+    import torch
+    ld = _rows(total, "total")
+    index, stream, shape = total.get_device(), total.dtype, total.shape
+    n, d = shape
+    ld_g = _rows(grad_out, "grad_out", shape, index)
+    along, ld_along = (None, 0) if grad_total is None else (grad_total.data_ptr(), _rows(grad_total, "grad_total", shape, index, stream))
+    w = None if weight is None else _vector(weight, "weight", d, index, param_dtype)
+    wdt = weight.dtype if weight is not None else param_dtype or torch.float32
+    r = _vector(rstd, "rstd", n, index, torch.float32)
+    if out is None:
+        out = total.new_empty((n, d))
+        ld_out = d
+    else:
+        ld_out = _rows(out, "out", shape, index, stream)
+    grad_x, gx = out, None
+    if x_dtype is not None and x_dtype is not stream:
+        if x_dtype is not torch.bfloat16:
+            raise TypeError(f"x must have been {stream} or bfloat16, got {x_dtype}")
+        grad_x = total.new_empty((n, d), dtype=x_dtype)
+        gx = grad_x.data_ptr()
+    gw = ws = None
+    if param_grads:
+        gw = total.new_empty(d, dtype=wdt)
+        ws = _scratch_for(workspace, load_library().hag_rms_norm_bwd_workspace_bytes(n, d), total)
+    _call("hag_rms_norm_bwd", index, n, d, grad_out.data_ptr(), _code(grad_out.dtype), ld_g, total.data_ptr(), _code(stream), ld, r,
+          w, _code(wdt), along, ld_along, out.data_ptr(), ld_out, gx, d, None if gw is None else gw.data_ptr(),
+          None if ws is None else ws.data_ptr())
+    return grad_x, out, gw
+
+
+class AdamWState(NamedTuple):
+    """The optimiser's states of a list of parameters, in blocks of 256 elements: ``mean`` and ``square`` (the root of the
+    mean square for 8 bits), [blocks, 256], and for 8 bits the ``scales`` of both, [blocks, 2].  To save them, save these
+    tensors; to restore them, make new ones or copy into them."""
+    mean: object
+    square: object
+    scales: Optional[object]
+
+
+def adamw_state(params, bits=32) -> AdamWState:
+    """Zero states for ``adamw_step``: float32, or float8_e4m3fn with a float32 scale per block for ``bits`` = 8."""
+    import torch
+    if bits not in (8, 32):
+        raise ValueError(f"bits must be 8 or 32, got {bits!r}")
+    if not params or not params[0].is_cuda:
+        raise ValueError("parameters must be a list of device tensors, not empty")
+    blocks = sum(-(-p.numel() // HAG_ADAMW_BLOCK) for p in params)
+    like = params[0]
+    dtype = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    mean, square = (like.new_zeros((blocks, HAG_ADAMW_BLOCK), dtype=dtype) for _ in range(2))
+    return AdamWState(mean, square, None if bits == 32 else like.new_zeros((blocks, 2), dtype=torch.float32))
+
+
+def _one_value(t, what, index, dtype):
+    if t.numel() != 1 or t.dtype is not dtype or t.get_device() != index:
+        raise ValueError(f"{what} must be a {dtype} tensor of one value on cuda:{index}")
+    return t.data_ptr()
+
+
+def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, total_norm=None, max_norm=None,
+               copies=None):
+    """``hag_adamw_step``: one AdamW step over all ``params``, which it changes in place with their ``state``
+    (``adamw_state``).  An entry of ``grads`` may be None: that parameter stays as it is.
+
+    ``step`` counts from 1, ``lr`` is the rate; either may be a device tensor of one value (int64, float32), which a
+    captured call reads anew each time.  ``weight_decay`` is a number or a list of one per parameter.  With ``total_norm``
+    (what ``grad_norm`` returned) the gradients are scaled as ``clip_grad_norm`` does for ``max_norm``, on the way.
+    ``copies``: a list of bfloat16 tensors (or None entries) that receive the new values.  Returns ``params``."""
+    import torch
+    if not params or not params[0].is_cuda:
+        raise ValueError("parameters must be a list of device tensors, not empty")
+    index, count = params[0].get_device(), len(params)
+    ptrs, lens, kinds = _tensor_list(params, index, "parameters")
+    if len(grads) != count:
+        raise ValueError(f"{len(grads)} gradients for {count} parameters")
+    missing = any(g is None for g in grads)
+    some = [p if g is None else g for g, p in zip(grads, params)] if missing else grads
+    gptrs, glens, gkinds = _tensor_list(some, index)
+    if glens != lens:
+        raise ValueError("gradients must have the lengths of the parameters")
+    if missing:
+        gptrs = [0 if g is None else at for g, at in zip(grads, gptrs)]
+    written = [at for at, m in zip(ptrs, lens) if m]
+    cptrs = None
+    if copies is not None:
+        if len(copies) != count:
+            raise ValueError(f"{len(copies)} copies for {count} parameters")
+        here = [c for c in copies if c is not None]
+        _, clens, ckinds = _tensor_list(here, index, "copies") if here else ([], [], [])
+        if clens != [m for m, c in zip(lens, copies) if c is not None] or any(k is not torch.bfloat16 for k in ckinds):
+            raise ValueError("copies must be bfloat16 tensors with the lengths of the parameters")
+        cptrs = array("Q", [0 if c is None else c.data_ptr() for c in copies])
+        written += [c.data_ptr() for c, m in zip(copies, lens) if c is not None and m]
+    if len(set(written)) != len(written) or not set(written).isdisjoint([at for at, m in zip(gptrs, lens) if m]):
+        raise ValueError("a tensor is named twice, or a gradient is written as a parameter or copy")
+    mean, square, scales = state
+    blocks = sum(-(-m // HAG_ADAMW_BLOCK) for m in lens)
+    bits8 = scales is not None
+    sdt = torch.float8_e4m3fn if bits8 else torch.float32
+    for t, what in ((mean, "mean"), (square, "square")):
+        if t.shape != (blocks, HAG_ADAMW_BLOCK) or t.dtype is not sdt or not t.is_contiguous() or t.get_device() != index:
+            raise ValueError(f"state.{what} must be a contiguous {sdt} tensor of shape ({blocks}, {HAG_ADAMW_BLOCK}) on cuda:{index}")
+    if bits8 and (scales.shape != (blocks, 2) or scales.dtype is not torch.float32 or not scales.is_contiguous() or scales.get_device() != index):
+        raise ValueError(f"state.scales must be a contiguous float32 tensor of shape ({blocks}, 2) on cuda:{index}")
+    decays = array("d", [weight_decay] * count if isinstance(weight_decay, (int, float)) else weight_decay)
+    if len(decays) != count:
+        raise ValueError(f"{len(decays)} weight decays for {count} parameters")
+    o = HagAdamwOptions(beta1=betas[0], beta2=betas[1], eps=eps)
+    if isinstance(lr, torch.Tensor):
+        o.lr_device = _one_value(lr, "lr", index, torch.float32)
+    else:
+        o.lr = lr
+    if isinstance(step, torch.Tensor):
+        o.step_device = _one_value(step, "step", index, torch.int64)
+    else:
+        o.step = step
+    if (total_norm is None) != (max_norm is None):
+        raise ValueError("total_norm and max_norm go together")
+    if total_norm is not None:
+        o.total_norm, o.max_norm = _one_value(total_norm, "total_norm", index, torch.float32), max_norm
+    addresses, gaddresses, lengths = array("Q", ptrs), array("Q", gptrs), array("q", lens)
+    codes, gcodes = array("i", [_codes[k] for k in kinds]), array("i", [_codes[k] for k in gkinds])
+    _call("hag_adamw_step", index, count, addresses.buffer_info()[0], codes.buffer_info()[0], gaddresses.buffer_info()[0],
+          gcodes.buffer_info()[0], None if cptrs is None else cptrs.buffer_info()[0], lengths.buffer_info()[0], decays.buffer_info()[0],
+          HAG_STATE8 if bits8 else HAG_STATE32, mean.data_ptr(), square.data_ptr(), scales.data_ptr() if bits8 else None, ctypes.byref(o))
+    return params
