@@ -588,7 +588,7 @@ hag_status hag_rms_norm_bwd(int64_t n, int32_t D, const void *grad_y, hag_dtype 
  * ones: lr_device in the place of lr, step_device in the place of step (read by the call; who counts it up is the caller;
  * a step below 1 counts as 1).
  * Errors: NULL, ARG (count < 0, a negative length or decay, lr or max_norm negative or no number, a beta outside [0, 1), eps
- * negative or no number, step < 1), DTYPE, ALIGN (pointer not on its element; states not on 16 bytes, scales not on 8),
+ * negative or no number, step < 1), DTYPE, ALIGN (pointer not on its element; states or scales not on 16 bytes),
  * TOO_LARGE (a tensor of more than 2^39 - 256 elements), CUDA. */
 #define HAG_ADAMW_BLOCK 256
 typedef enum { HAG_STATE32 = 0, HAG_STATE8 = 1 } hag_state_type;

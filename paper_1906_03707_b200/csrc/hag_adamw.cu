@@ -14,6 +14,7 @@
 #include <cfloat>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "hag.h"
 #include "hag_kernels.cuh"
@@ -34,10 +35,10 @@ constexpr float kLowest = 0.001953125f;         // 2^-9, the smallest positive v
 
 struct AdamArgs {
     int32_t tensors;
-    uint32_t blocks;                            // of this launch's tensors
     void *mean, *square;                        // of all tensors
     float2 *scales;
-    float lr, b1, rest1, b2, rest2, eps;        // rest = 1 - b
+    float lr, b1, rest1, b2, eps;               // rest = 1 - b
+    float root2, root_rest2;                    // sqrt(b2), sqrt(1 - b2)
     float rate, root;                           // lr / (1 - b1^t), 1 / sqrt(1 - b2^t): where the step is the host's
     double beta1, beta2;
     const float *lr_at, *norm;
@@ -48,15 +49,24 @@ struct AdamArgs {
     void *copy[kAdamList];
     int64_t len[kAdamList], state[kAdamList];   // elements; first block of the states
     float decay[kAdamList];
-    uint32_t first[kAdamList];                  // first block among this launch's
+    uint32_t units;                             // of this launch's tensors
+    uint32_t first[kAdamList];                  // units before those of each
+    uint32_t blocks[kAdamList], whole[kAdamList];      // how many, and how many of them are read by vectors
     uint8_t p_bf16[kAdamList], g_bf16[kAdamList];
-    uint8_t vec[kAdamList];                     // whether four elements can be read at once
 };
 static_assert(sizeof(AdamArgs) <= 4096, "the list must fit in the parameters of a launch");
 
 struct Coefficients {
-    float lr, rate, root, factor;
+    float lr, rate, root;
+    float norm;                                 // as it was read: it arrives while the first blocks do
 };
+// What the gradient is multiplied with for m, and, before its square, for v.
+__device__ __forceinline__ float2 of_gradient(const AdamArgs &p, float norm) {
+    if (!p.norm) return make_float2(p.rest1, p.root_rest2);
+    const float ratio = __fdividef(p.max_norm, norm + 1e-6f);
+    const float factor = ratio >= 1.0f ? 1.0f : ratio;         // a norm that is no number gives a factor that is none
+    return make_float2(p.rest1 * factor, p.root_rest2 * factor);
+}
 
 __device__ double power(double base, int64_t n) {          // base^n by squaring
     double r = 1.0;
@@ -65,208 +75,312 @@ __device__ double power(double base, int64_t n) {          // base^n by squaring
     return r;
 }
 
-// What the step, the rate and the norm on the device make of the coefficients; one thread's work.
+// What the step and the rate on the device make of the coefficients; one thread's work.
 __device__ __forceinline__ Coefficients coefficients(const AdamArgs &p) {
-    Coefficients c{p.lr, p.rate, p.root, 1.0f};
+    Coefficients c{p.lr, p.rate, p.root, 0.0f};
     if (p.lr_at) c.lr = __ldcg(p.lr_at);
     if (p.step_at) {
         const int64_t t = max(int64_t(1), int64_t(__ldcg(reinterpret_cast<const long long *>(p.step_at))));
         c.rate = float(1.0 / (1.0 - power(p.beta1, t)));
         c.root = float(1.0 / sqrt(1.0 - power(p.beta2, t)));
     }
-    if (p.lr_at || p.step_at) c.rate = float(double(c.lr) * double(c.rate));
-    if (p.norm) {
-        const float ratio = p.max_norm / (__ldcg(p.norm) + 1e-6f);
-        c.factor = ratio >= 1.0f ? 1.0f : ratio;               // a norm that is no number gives a factor that is none
-    }
+    c.rate = float(double(c.lr) * double(c.rate));
     return c;
 }
 
-// The elements of a block that a lane holds: two groups of four, 128 apart, so that a warp's accesses are contiguous;
-// or, where the addresses do not allow that, eight single ones, 32 apart.
-template <bool VEC>
-__device__ __forceinline__ int place(int lane, int j) {
-    return VEC ? (j / 4) * 128 + lane * 4 + j % 4 : j * 32 + lane;
-}
+// The elements of a block that a lane holds, as pairs: two groups of four, 128 apart, so that a warp's accesses are
+// contiguous; or, where the addresses do not allow that, eight single ones, 32 apart.
+constexpr int kPairs = kPerLane / 2;
+// Eight elements of a lane as they are in memory.
+template <typename T, bool VEC>
+struct Eight {
+    hagr::Vec<T, VEC ? 4 : 1> v[VEC ? 2 : kPerLane];
+    __device__ __forceinline__ void load(const T *at, int lane, int count) {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) v[h].template load<hagr::kKeep>(at + h * 128, lane);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPerLane; ++j) {
+                v[j].zero();
+                if (j * 32 + lane < count) v[j].template load<hagr::kKeep>(at, j * 32 + lane);
+            }
+        }
+    }
+    __device__ __forceinline__ float2 pair(int j) const {
+        if constexpr (VEC) return make_float2(v[j / 2].get(j % 2 * 2), v[j / 2].get(j % 2 * 2 + 1));
+        else return make_float2(v[2 * j].get(0), v[2 * j + 1].get(0));
+    }
+};
 
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(float (&v)[kPerLane], const void *at, int64_t first, int lane, int count) {
+__device__ __forceinline__ void store8(const float2 (&v)[kPairs], T *at, int lane, int count) {
     if constexpr (VEC) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
+            const float four[4] = {v[2 * h].x, v[2 * h].y, v[2 * h + 1].x, v[2 * h + 1].y};
             hagr::Vec<T, 4> q;
-            q.template load<hagr::kKeep>(static_cast<const T *>(at) + first + h * 128, lane);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[h * 4 + j] = q.get(j);
+            q.set(four);
+            q.store(at + h * 128, lane);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < kPerLane; ++j) {
-            hagr::Vec<T, 1> q;
-            q.zero();
-            if (j * 32 + lane < count) q.template load<hagr::kKeep>(at, first + j * 32 + lane);
-            v[j] = q.get(0);
+        for (int j = 0; j < kPairs; ++j) {
+            hagr::Vec<T, 1> a, b;
+            a.set(&v[j].x);
+            b.set(&v[j].y);
+            if (j * 64 + lane < count) a.store(at, j * 64 + lane);
+            if (j * 64 + 32 + lane < count) b.store(at, j * 64 + 32 + lane);
         }
     }
 }
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void store8(const float (&v)[kPerLane], void *at, int64_t first, int lane, int count) {
-    if constexpr (VEC) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            hagr::Vec<T, 4> q;
-            q.set(v + h * 4);
-            q.store(static_cast<T *>(at) + first + h * 128, lane);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < kPerLane; ++j) {
-            hagr::Vec<T, 1> q;
-            q.set(v + j);
-            if (j * 32 + lane < count) q.store(at, first + j * 32 + lane);
-        }
-    }
-}
-
-__device__ __forceinline__ float2 from_e4m3(uint16_t two) {
+__device__ __forceinline__ float2 from_e4m3(uint32_t two) {    // of the lower 16 bits
     uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(two));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(uint16_t(two)));
     return __half22float2(*reinterpret_cast<const __half2 *>(&h));
 }
-__device__ __forceinline__ uint16_t to_e4m3(float lo, float hi) {
+__device__ __forceinline__ uint32_t to_e4m3(float2 v) {
     uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(v.y), "f"(v.x));
     return r;
 }
 
 template <bool VEC>
-__device__ __forceinline__ void load_codes(float (&v)[kPerLane], const uint8_t *block, int lane, int count) {
-#pragma unroll
-    for (int j = 0; j < kPerLane; j += VEC ? 4 : 2) {
+struct EightCodes {
+    uint32_t w[VEC ? 2 : kPairs];                              // four codes, or two
+    __device__ __forceinline__ void load(const uint8_t *block, int lane, int count) {
         if constexpr (VEC) {
-            const uint32_t w = __ldcg(reinterpret_cast<const uint32_t *>(block + place<true>(lane, j)));
-            const float2 a = from_e4m3(uint16_t(w)), b = from_e4m3(uint16_t(w >> 16));
-            v[j] = a.x; v[j + 1] = a.y; v[j + 2] = b.x; v[j + 3] = b.y;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) w[h] = __ldcg(reinterpret_cast<const uint32_t *>(block + h * 128) + lane);
         } else {
-            const uint32_t a = place<false>(lane, j) < count ? __ldcg(block + place<false>(lane, j)) : 0;
-            const uint32_t b = place<false>(lane, j + 1) < count ? __ldcg(block + place<false>(lane, j + 1)) : 0;
-            const float2 t = from_e4m3(uint16_t(a | b << 8));
-            v[j] = t.x; v[j + 1] = t.y;
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                const uint32_t a = j * 64 + lane < count ? __ldcg(block + j * 64 + lane) : 0;
+                w[j] = a | (j * 64 + 32 + lane < count ? __ldcg(block + j * 64 + 32 + lane) : 0) << 8;
+            }
         }
     }
-}
+    __device__ __forceinline__ float2 pair(int j) const { return from_e4m3(VEC ? w[j / 2] >> (j % 2 * 16) : w[j]); }
+};
+
 template <bool VEC>
-__device__ __forceinline__ void store_codes(const float (&v)[kPerLane], uint8_t *block, int lane, int count) {
+__device__ __forceinline__ void store_codes(const float2 (&v)[kPairs], uint8_t *block, int lane, int count) {
+    if constexpr (VEC) {
 #pragma unroll
-    for (int j = 0; j < kPerLane; j += VEC ? 4 : 2) {
-        const uint32_t a = to_e4m3(v[j], v[j + 1]);
-        if constexpr (VEC) {
-            *reinterpret_cast<uint32_t *>(block + place<true>(lane, j)) = a | uint32_t(to_e4m3(v[j + 2], v[j + 3])) << 16;
-        } else {
-            if (place<false>(lane, j) < count) block[place<false>(lane, j)] = uint8_t(a);
-            if (place<false>(lane, j + 1) < count) block[place<false>(lane, j + 1)] = uint8_t(a >> 8);
+        for (int h = 0; h < 2; ++h) reinterpret_cast<uint32_t *>(block + h * 128)[lane] = to_e4m3(v[2 * h]) | to_e4m3(v[2 * h + 1]) << 16;
+    } else {
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+            const uint32_t a = to_e4m3(v[j]);
+            if (j * 64 + lane < count) block[j * 64 + lane] = uint8_t(a);
+            if (j * 64 + 32 + lane < count) block[j * 64 + 32 + lane] = uint8_t(a >> 8);
         }
     }
 }
 
-__device__ __forceinline__ float root_of(float v) {            // to two units in the last place
+// Root and reciprocal to an error of 2^-22 or less; what is below 2^-126 counts as zero.
+__device__ __forceinline__ float root_of(float v) {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
+__device__ __forceinline__ float one_over(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float at_least_lowest(float v) {    // NaN stays NaN
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(kLowest));
+    return r;
+}
+__device__ __forceinline__ float2 both(float f) { return make_float2(f, f); }
 
-// The largest finite magnitude of the block (the bits of positive floats are ordered as the floats are).
-__device__ __forceinline__ float block_largest(const float (&v)[kPerLane]) {
-    uint32_t top = 0;
+// The largest magnitude of a block; NaN does not count.
+__device__ __forceinline__ float block_largest(const float2 (&v)[kPairs]) {
+    float top = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kPerLane; ++j) {
-        const uint32_t b = __float_as_uint(fabsf(v[j]));
-        top = max(top, b < 0x7f800000u ? b : 0u);
-    }
-    return __uint_as_float(__reduce_max_sync(0xffffffffu, top));
+    for (int j = 0; j < kPairs; ++j) top = fmaxf(top, fmaxf(fabsf(v[j].x), fabsf(v[j].y)));
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
 }
 __device__ __forceinline__ float scale_of(float largest) { return fmaxf(largest * (1.0f / kTop), kLeastScale); }
 
-// One block of one tensor.  A value that is not finite is stored as NaN, which e4m3 has; infinity it has not.
-template <typename P, typename G, bool BITS8, bool VEC>
-__device__ __forceinline__ void step_block(const AdamArgs &a, const Coefficients &c, int t, int64_t first, int64_t block, int count) {
-    const int lane = threadIdx.x & 31;
-    float p[kPerLane], g[kPerLane], m[kPerLane], v[kPerLane];
-    load8<P, VEC>(p, a.p[t], first, lane, count);
-    load8<G, VEC>(g, a.g[t], first, lane, count);
-    uint8_t *const codes_m = static_cast<uint8_t *>(a.mean) + block * kAdamBlock, *const codes_r = static_cast<uint8_t *>(a.square) + block * kAdamBlock;
-    if constexpr (BITS8) {
-        load_codes<VEC>(m, codes_m, lane, count);
-        load_codes<VEC>(v, codes_r, lane, count);
-        const float2 s = __ldcg(a.scales + block);
+// For the rare block with an infinity: NaN takes its place, which e4m3 has; infinity it has not.
+__device__ __forceinline__ void drop_infinities(float2 (&v)[kPairs]) {
+    const float none = __uint_as_float(0x7fffffffu);
 #pragma unroll
-        for (int j = 0; j < kPerLane; ++j) {
-            m[j] *= s.x;
-            v[j] *= s.y;
-            v[j] *= v[j];
-        }
-    } else {
-        load8<float, VEC>(m, a.mean, block * kAdamBlock, lane, count);
-        load8<float, VEC>(v, a.square, block * kAdamBlock, lane, count);
-    }
-    const float keep = fmaf(-c.lr, a.decay[t], 1.0f);
-    float r[kPerLane];
-#pragma unroll
-    for (int j = 0; j < kPerLane; ++j) {
-        const float d = g[j] * c.factor;
-        m[j] = fmaf(a.b1, m[j], a.rest1 * d);
-        v[j] = fmaf(a.b2, v[j], a.rest2 * (d * d));
-        r[j] = root_of(v[j]);
-        p[j] = fmaf(p[j], keep, -c.rate * __fdividef(m[j], fmaf(r[j], c.root, a.eps)));
-    }
-    store8<P, VEC>(p, a.p[t], first, lane, count);
-    if (a.copy[t]) store8<__nv_bfloat16, VEC>(p, a.copy[t], first, lane, count);
-    if constexpr (BITS8) {
-        const float sm = scale_of(block_largest(m)), sr = scale_of(block_largest(r));
-        const float im = __fdividef(1.0f, sm), ir = __fdividef(1.0f, sr);
-        const float none = __uint_as_float(0x7fffffffu);
-#pragma unroll
-        for (int j = 0; j < kPerLane; ++j) {
-            m[j] = fabsf(m[j]) <= FLT_MAX ? m[j] * im : none;
-            r[j] = r[j] <= FLT_MAX ? (r[j] > 0.0f ? fmaxf(r[j] * ir, kLowest) : 0.0f) : none;
-        }
-        store_codes<VEC>(m, codes_m, lane, count);
-        store_codes<VEC>(r, codes_r, lane, count);
-        if (lane == 0) a.scales[block] = make_float2(sm, sr);
-    } else {
-        store8<float, VEC>(m, a.mean, block * kAdamBlock, lane, count);
-        store8<float, VEC>(v, a.square, block * kAdamBlock, lane, count);
+    for (int j = 0; j < kPairs; ++j) {
+        if (!(fabsf(v[j].x) <= FLT_MAX)) v[j].x = none;
+        if (!(fabsf(v[j].y) <= FLT_MAX)) v[j].y = none;
     }
 }
 
-template <bool BITS8>
-__global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_constant__ AdamArgs a) {
+// m and the root of v in 8 bits.  A block seldom has an infinity or a root of zero: a test for the whole warp decides
+// whether its elements are looked at one by one.
+template <bool VEC>
+__device__ __forceinline__ void store_8_bits(float2 (&m)[kPairs], float2 (&r)[kPairs], uint8_t *to_m, uint8_t *to_r, float2 *scale, int lane, int count) {
+    float top_m = block_largest(m), top_r = block_largest(r);
+    if (fmaxf(top_m, top_r) > FLT_MAX) {
+        drop_infinities(m);
+        drop_infinities(r);
+        top_m = block_largest(m);
+        top_r = block_largest(r);
+    }
+    const float sm = scale_of(top_m), sr = scale_of(top_r);
+    const float2 im = both(one_over(sm)), ir = both(one_over(sr));
+    float least = r[0].x;
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) {
+        least = fminf(least, fminf(r[j].x, r[j].y));
+        m[j] = __fmul2_rn(m[j], im);
+        r[j] = __fmul2_rn(r[j], ir);
+    }
+    if (__any_sync(0xffffffffu, least == 0.0f)) {
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+            if (r[j].x > 0.0f && r[j].x < kLowest) r[j].x = kLowest;
+            if (r[j].y > 0.0f && r[j].y < kLowest) r[j].y = kLowest;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) r[j] = make_float2(at_least_lowest(r[j].x), at_least_lowest(r[j].y));
+    }
+    store_codes<VEC>(m, to_m, lane, count);
+    store_codes<VEC>(r, to_r, lane, count);
+    if (lane == 0) *scale = make_float2(sm, sr);
+}
+
+// Where the arrays of a tensor's blocks lie, from one of them on.
+template <typename P, typename G, bool BITS8>
+struct Arrays {
+    using State = std::conditional_t<BITS8, uint8_t, float>;
+    P *p;
+    const G *g;
+    __nv_bfloat16 *copy;
+    State *m, *v;
+    float2 *scales;
+    __device__ __forceinline__ Arrays(const AdamArgs &a, int t, int64_t within) {
+        const int64_t first = within * kAdamBlock, block = a.state[t] + within;
+        p = static_cast<P *>(a.p[t]) + first;
+        g = static_cast<const G *>(a.g[t]) + first;
+        copy = a.copy[t] ? static_cast<__nv_bfloat16 *>(a.copy[t]) + first : nullptr;
+        m = static_cast<State *>(a.mean) + block * kAdamBlock;
+        v = static_cast<State *>(a.square) + block * kAdamBlock;
+        scales = a.scales + block;
+    }
+};
+
+// What a lane reads of one block.
+template <typename P, typename G, bool BITS8, bool VEC>
+struct Piece {
+    Eight<P, VEC> p;
+    Eight<G, VEC> g;
+    std::conditional_t<BITS8, EightCodes<VEC>, Eight<float, VEC>> m, v;
+    float2 scale;
+    __device__ __forceinline__ void load(const Arrays<P, G, BITS8> &at, int block, int lane, int count) {
+        p.load(at.p + block * kAdamBlock, lane, count);
+        g.load(at.g + block * kAdamBlock, lane, count);
+        m.load(at.m + block * kAdamBlock, lane, count);
+        v.load(at.v + block * kAdamBlock, lane, count);
+        if (BITS8) scale = __ldcg(at.scales + block);
+    }
+};
+
+template <typename P, typename G, bool BITS8, bool VEC>
+__device__ __forceinline__ void step_block(const AdamArgs &a, const Coefficients &c, float keep_, const Piece<P, G, BITS8, VEC> &in,
+                                           const Arrays<P, G, BITS8> &to, int block, int lane, int count) {
+    const float2 of_g = of_gradient(a, c.norm);
+    const float2 keep = both(keep_), of_m = both(of_g.x), of_v = both(of_g.y);
+    const float2 of_old_m = both(BITS8 ? in.scale.x * a.b1 : a.b1), of_old_v = both(BITS8 ? in.scale.y * a.root2 : a.b2);
+    float2 p[kPairs], m[kPairs], v[kPairs], r[kPairs];
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) {
+        const float2 g = in.g.pair(j);
+        m[j] = __ffma2_rn(g, of_m, __fmul2_rn(in.m.pair(j), of_old_m));
+        const float2 e = __fmul2_rn(g, of_v);
+        v[j] = __fmul2_rn(in.v.pair(j), of_old_v);
+        if (BITS8) v[j] = __fmul2_rn(v[j], v[j]);
+        v[j] = __ffma2_rn(e, e, v[j]);
+        r[j] = make_float2(root_of(v[j].x), root_of(v[j].y));
+        const float2 d = __ffma2_rn(r[j], both(c.root), both(a.eps));
+        const float2 x = __fmul2_rn(m[j], make_float2(one_over(d.x), one_over(d.y)));
+        p[j] = __ffma2_rn(x, both(-c.rate), __fmul2_rn(in.p.pair(j), keep));
+    }
+    store8<P, VEC>(p, to.p + block * kAdamBlock, lane, count);
+    if (to.copy) store8<__nv_bfloat16, VEC>(p, to.copy + block * kAdamBlock, lane, count);
+    if constexpr (BITS8) {
+        store_8_bits<VEC>(m, r, to.m + block * kAdamBlock, to.v + block * kAdamBlock, to.scales + block, lane, count);
+    } else {
+        store8<float, VEC>(m, to.m + block * kAdamBlock, lane, count);
+        store8<float, VEC>(v, to.v + block * kAdamBlock, lane, count);
+    }
+}
+
+// T blocks of a tensor from block `within` on; of the whole ones as many as the registers hold are read at once.
+template <typename P, typename G, bool BITS8, int T>
+__device__ __forceinline__ void step_unit(const AdamArgs &a, const Coefficients &c, int t, uint32_t within) {
+    constexpr int kWords = 2 * int(sizeof(P) + sizeof(G)) + (BITS8 ? 4 : 16);          // per lane and block
+    constexpr int B = kWords * T <= 48 ? T : kWords * 2 <= 64 && T > 1 ? 2 : 1;
+    const int lane = threadIdx.x & 31;
+    const float keep = fmaf(-c.lr, a.decay[t], 1.0f);
+    const Arrays<P, G, BITS8> at(a, t, within);
+    if (within + T <= a.whole[t]) {
+#pragma unroll 1
+        for (int i = 0; i < T; i += B) {
+            Piece<P, G, BITS8, true> in[B];
+#pragma unroll
+            for (int k = 0; k < B; ++k) in[k].load(at, i + k, lane, kAdamBlock);
+#pragma unroll
+            for (int k = 0; k < B; ++k) step_block<P, G, BITS8, true>(a, c, keep, in[k], at, i + k, lane, kAdamBlock);
+        }
+    } else {
+        const int n = int(min(uint32_t(T), a.blocks[t] - within));
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            if (T > 1 && within + i < a.whole[t]) {
+                Piece<P, G, BITS8, true> in;
+                in.load(at, i, lane, kAdamBlock);
+                step_block<P, G, BITS8, true>(a, c, keep, in, at, i, lane, kAdamBlock);
+            } else {
+                const int count = int(min(int64_t(kAdamBlock), a.len[t] - int64_t(within + i) * kAdamBlock));
+                Piece<P, G, BITS8, false> in;
+                in.load(at, i, lane, count);
+                step_block<P, G, BITS8, false>(a, c, keep, in, at, i, lane, count);
+            }
+        }
+    }
+}
+
+// T: blocks that a warp takes at a time.
+template <bool BITS8, int T>
+__global__ void __launch_bounds__(kAdamThreads, T > 1 ? 2 : 4) adamw_kernel(const __grid_constant__ AdamArgs a) {
     hagk::pdl_launch_dependents();
     __shared__ Coefficients shared;
+    __shared__ uint32_t first[kAdamList];                              // units before each tensor's
+    if (threadIdx.x < kAdamList) first[threadIdx.x] = int(threadIdx.x) < a.tensors ? a.first[threadIdx.x] : 0xffffffffu;
     hagk::pdl_wait();
-    if (threadIdx.x == 0) shared = coefficients(a);
-    __syncthreads();
-    const Coefficients c = shared;
-    int t = 0;
+    Coefficients c{a.lr, a.rate, a.root};
+    if (a.step_at || a.lr_at) {
+        if (threadIdx.x == 0) shared = coefficients(a);
+        __syncthreads();
+        c = shared;
+    } else {
+        __syncthreads();
+    }
+    c.norm = a.norm ? __ldcg(a.norm) : 0.0f;
+    const int lane = threadIdx.x & 31;
     const uint32_t step = gridDim.x * kAdamWarps;
-    for (uint64_t k = blockIdx.x * kAdamWarps + (threadIdx.x >> 5); k < a.blocks; k += step) {
-        while (t + 1 < a.tensors && a.first[t + 1] <= k) ++t;
-        const int64_t within = int64_t(k - a.first[t]), first = within * kAdamBlock, block = a.state[t] + within;
-        const int count = int(min(int64_t(kAdamBlock), a.len[t] - first));
-        const bool vec = a.vec[t] && count == kAdamBlock;
-        auto run = [&](auto p, auto g) {
-            using P = decltype(p);
-            using G = decltype(g);
-            if (vec) step_block<P, G, BITS8, true>(a, c, t, first, block, count);
-            else step_block<P, G, BITS8, false>(a, c, t, first, block, count);
-        };
+    for (uint32_t k = blockIdx.x * kAdamWarps + (threadIdx.x >> 5); k < a.units; k += step) {
+        static_assert(kAdamList == 64, "two per lane");
+        const int t = __popc(__ballot_sync(0xffffffffu, first[lane] <= k)) + __popc(__ballot_sync(0xffffffffu, first[lane + 32] <= k)) - 1;
+        const uint32_t within = (k - first[t]) * T;
         if (a.p_bf16[t]) {
-            if (a.g_bf16[t]) run(__nv_bfloat16(), __nv_bfloat16());
-            else run(__nv_bfloat16(), float());
+            if (a.g_bf16[t]) step_unit<__nv_bfloat16, __nv_bfloat16, BITS8, T>(a, c, t, within);
+            else step_unit<__nv_bfloat16, float, BITS8, T>(a, c, t, within);
         } else {
-            if (a.g_bf16[t]) run(float(), __nv_bfloat16());
-            else run(float(), float());
+            if (a.g_bf16[t]) step_unit<float, __nv_bfloat16, BITS8, T>(a, c, t, within);
+            else step_unit<float, float, BITS8, T>(a, c, t, within);
         }
     }
 }
@@ -276,8 +390,9 @@ bool dtype_ok(hag_dtype d) { return d == HAG_F32 || d == HAG_BF16; }
 int size_of(hag_dtype d) { return d == HAG_F32 ? 4 : 2; }
 bool on(const void *p, int bytes) { return reinterpret_cast<uintptr_t>(p) % uintptr_t(bytes) == 0; }
 
+constexpr int kUnit = 4;                        // blocks that a warp takes at a time, and of how many on in a launch
+constexpr int64_t kFewBlocks = kSms * 4 * kAdamWarps * 2;
 constexpr int64_t kMostBlocks = 0x7fffffffLL;   // of a tensor and of a launch
-
 }  // namespace
 
 extern "C" int64_t hag_adamw_state_blocks(int32_t count, const int64_t *lengths) {
@@ -316,7 +431,7 @@ extern "C" hag_status hag_adamw_step(int32_t count, void *const *params, const h
     }
     if (total == 0) return HAG_OK;
     if (!mean || !square || (state == HAG_STATE8 && !scales)) return HAG_ERR_NULL;
-    if (!hagl::aligned16(mean) || !hagl::aligned16(square) || !on(scales, 8)) return HAG_ERR_ALIGN;
+    if (!hagl::aligned16(mean) || !hagl::aligned16(square) || !hagl::aligned16(scales)) return HAG_ERR_ALIGN;
     AdamArgs a{};
     a.mean = mean;
     a.square = square;
@@ -325,7 +440,8 @@ extern "C" hag_status hag_adamw_step(int32_t count, void *const *params, const h
     a.b1 = float(o.beta1);
     a.rest1 = float(1.0 - o.beta1);
     a.b2 = float(o.beta2);
-    a.rest2 = float(1.0 - o.beta2);
+    a.root2 = float(std::sqrt(o.beta2));
+    a.root_rest2 = float(std::sqrt(1.0 - o.beta2));
     a.eps = float(o.eps);
     a.beta1 = o.beta1;
     a.beta2 = o.beta2;
@@ -339,13 +455,22 @@ extern "C" hag_status hag_adamw_step(int32_t count, void *const *params, const h
         a.root = float(1.0 / std::sqrt(1.0 - std::pow(o.beta2, double(o.step))));
     }
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    void (*const kernel)(AdamArgs) = state == HAG_STATE8 ? adamw_kernel<true> : adamw_kernel<false>;
+    const bool bits8 = state == HAG_STATE8;
     cudaError_t err = cudaSuccess;
     int64_t at = 0, blocks = 0;
     auto launch = [&]() {
-        a.blocks = uint32_t(blocks);
-        const unsigned grid = unsigned(std::min<int64_t>((blocks + kAdamWarps - 1) / kAdamWarps, kSms * 4));
-        if (a.tensors > 0) err = hagl::launch_pdl<AdamArgs>(kernel, grid, unsigned(kAdamThreads), a, s);
+        if (a.tensors > 0) {
+            const bool many = blocks > kFewBlocks;
+            a.units = 0;
+            for (int i = 0; i < a.tensors; ++i) {
+                a.first[i] = a.units;
+                a.units += many ? (a.blocks[i] + kUnit - 1) / kUnit : a.blocks[i];
+            }
+            const unsigned grid = unsigned(std::min<int64_t>((int64_t(a.units) + kAdamWarps - 1) / kAdamWarps, kSms * (many ? 2 : 4)));
+            void (*const kernel)(AdamArgs) = bits8 ? many ? adamw_kernel<true, kUnit> : adamw_kernel<true, 1>
+                                                   : many ? adamw_kernel<false, kUnit> : adamw_kernel<false, 1>;
+            err = hagl::launch_pdl<AdamArgs>(kernel, grid, unsigned(kAdamThreads), a, s);
+        }
         a.tensors = 0;
         blocks = 0;
     };
@@ -355,17 +480,17 @@ extern "C" hag_status hag_adamw_step(int32_t count, void *const *params, const h
         if (grads[t]) {
             if (a.tensors == kAdamList || blocks + here > kMostBlocks) launch();
             if (err != cudaSuccess) break;
-            const int i = a.tensors++;
+            const int i = a.tensors++, ps = size_of(param_dtypes[t]), gs = size_of(grad_dtypes[t]);
             a.p[i] = params[t];
             a.g[i] = grads[t];
             a.copy[i] = copies ? copies[t] : nullptr;
             a.len[i] = lengths[t];
             a.state[i] = at;
             a.decay[i] = float(decays[t]);
-            a.first[i] = uint32_t(blocks);
-            a.p_bf16[i] = param_dtypes[t] == HAG_BF16;
-            a.g_bf16[i] = grad_dtypes[t] == HAG_BF16;
-            a.vec[i] = on(params[t], 4 * size_of(param_dtypes[t])) && on(grads[t], 4 * size_of(grad_dtypes[t])) && on(a.copy[i], 8);
+            a.p_bf16[i] = ps == 2;
+            a.g_bf16[i] = gs == 2;
+            a.blocks[i] = uint32_t(here);
+            a.whole[i] = on(params[t], 4 * ps) && on(grads[t], 4 * gs) && on(a.copy[i], 8) ? uint32_t(lengths[t] / kAdamBlock) : 0;
             blocks += here;
         }
         at += here;
