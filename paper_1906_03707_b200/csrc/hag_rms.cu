@@ -24,6 +24,7 @@ struct RmsArgs {
     float *scales;
     int32_t block, n_scales;            // columns per scale (0: all), scales per row
     int32_t int8;
+    int32_t stages;                     // of the ring
     float top;
 };
 
@@ -60,30 +61,31 @@ __device__ __forceinline__ void store_codes(const float (&v)[V], void *row, int6
     else hagr::store_words<hagr::kKeep, V>(static_cast<char *>(row) + i * V, pack<V>(v, int8));
 }
 
-// The largest of magnitudes; NaN is larger than anything (the bits of positive floats are ordered as the floats are).
-template <int L>
-__device__ __forceinline__ float lanes_largest(float v) {
+// The larger magnitude; NaN is larger than anything.
+__device__ __forceinline__ float larger(float top, float v) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(top), "f"(fabsf(v)));
+    return r;
+}
+// The largest over the first `lanes` (a power of two) lanes of each such group: the bits of positive floats are ordered as
+// the floats are, and NaN is above them.
+__device__ __forceinline__ float lanes_largest(float v, int lanes) {
     uint32_t b = __float_as_uint(v);
+    if (lanes == 32) return __uint_as_float(__reduce_max_sync(0xffffffffu, b));
 #pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) b = max(b, __shfl_xor_sync(0xffffffffu, b, o));
+    for (int o = 8; o > 0; o >>= 1)
+        if (lanes > o) b = max(b, __shfl_xor_sync(0xffffffffu, b, o));
     return __uint_as_float(b);
 }
-__device__ __forceinline__ float larger(float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }
 template <int L>
 __device__ __forceinline__ float group_largest(float v, float *slot) {
-    v = lanes_largest<L ? L : 32>(v);
+    v = lanes_largest(v, L ? L : 32);
     if constexpr (L == 0) {
         if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
         __syncthreads();
-        v = lanes_largest<32>((threadIdx.x & 31) < (blockDim.x >> 5) ? slot[threadIdx.x & 31] : 0.0f);
+        v = lanes_largest((threadIdx.x & 31) < (blockDim.x >> 5) ? slot[threadIdx.x & 31] : 0.0f, 32);
     }
     return v;
-}
-// the same over the first `lanes` (a power of two) only
-__device__ __forceinline__ float some_largest(float v, int lanes) {
-    uint32_t b = __float_as_uint(v);
-    for (int o = lanes / 2; o > 0; o >>= 1) b = max(b, __shfl_xor_sync(0xffffffffu, b, o));
-    return __uint_as_float(b);
 }
 // top is 448 or 127; a largest value that is not finite gives a scale that is none
 __device__ __forceinline__ float scale_of(float largest, const RmsArgs &p) {
@@ -91,17 +93,10 @@ __device__ __forceinline__ float scale_of(float largest, const RmsArgs &p) {
     return s < FLT_MIN ? FLT_MIN : s;
 }
 
-template <typename X, typename S, int V>
-__device__ __forceinline__ void add_rows(float (&h)[V], const Wide<X, V> &x, const Wide<S, V> &r, bool res) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = res ? x.v.get(j) + r.v.get(j) : x.v.get(j);
-}
-
-// Scales and codes of K vectors of a thread, which lie kStep = 32 apart (or are a row's all, of fewer lanes): `y` are the
-// values, first their number in the row.  A scale's columns lie within a warp: they are block / V lanes of one vector, or,
-// for V = 1, block / 32 vectors of all lanes.
-template <int V, int K, int STEP>
-__device__ __forceinline__ void quant_blocks(float (&y)[K][V], const RmsArgs &p, int64_t r, int first, int n_vec, bool live) {
+// Scales and codes of K vectors of a thread: `y` are the values.  A scale's columns lie within a warp: they are block / V
+// lanes of one vector, or, for V = 1, block / 32 vectors of all lanes.
+template <int V, int K, typename At>
+__device__ __forceinline__ void quant_blocks(hagr::Pairs<V> (&y)[K], const RmsArgs &p, int64_t r, const At &at, int n_vec, bool live) {
     char *q = static_cast<char *>(p.y) + r * p.ld_y;
     const int lanes = V == 1 ? 32 : p.block / V, together = V == 1 ? p.block / 32 : 1;
     float top[K];
@@ -109,130 +104,184 @@ __device__ __forceinline__ void quant_blocks(float (&y)[K][V], const RmsArgs &p,
     for (int k = 0; k < K; ++k) {
         top[k] = 0.0f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) top[k] = larger(top[k], fabsf(y[k][j]));
-        top[k] = some_largest(top[k], lanes);
+        for (int j = 0; j < V; ++j) top[k] = larger(top[k], y[k].v[j]);
+        top[k] = lanes_largest(top[k], lanes);
     }
     if constexpr (V == 1 && K > 1) {
 #pragma unroll
-        for (int k = 0; k < K; k += 2)
+        for (int k = 0; k + 1 < K; k += 2)
             if (together > 1) top[k] = top[k + 1] = larger(top[k], top[k + 1]);
-        if constexpr (K % 4 == 0) {
 #pragma unroll
-            for (int k = 0; k < K; k += 4)
-                if (together > 2) top[k] = top[k + 1] = top[k + 2] = top[k + 3] = larger(top[k], top[k + 2]);
-        }
+        for (int k = 0; k + 2 < K; k += 4)
+            if (together > 2) {
+                top[k] = top[k + 1] = larger(top[k], top[k + 2]);
+                top[k + 2] = top[k];
+                if (k + 3 < K) top[k + 3] = top[k];
+            }
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int vec = first + k * STEP;
-        const float scale = scale_of(top[k], p), inverse = __fdividef(1.0f, scale);
-        float t[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) t[j] = y[k][j] * inverse;
+        const int vec = at.vec(k);
+        const float scale = scale_of(top[k], p);
+        y[k].mul_all(__fdividef(1.0f, scale));
         if (!live || vec >= n_vec) continue;
-        store_codes<V>(t, q, vec, p.int8);
+        store_codes<V>(y[k].v, q, vec, p.int8);
         const int c = vec * V;
         if (c % p.block == 0) p.scales[r * p.n_scales + c / p.block] = scale;
     }
 }
 
-template <int PER_LANE> constexpr int kTurnRows = PER_LANE >= 32 ? 1 : 32 / PER_LANE < 4 ? 32 / PER_LANE : 4;
+// Rows whose vectors fill 16 bytes are copied into a ring in shared memory some turns ahead, so that what is in flight does
+// not take registers; others are read when their turn comes, all of them before the first is used.
+template <typename X, typename S, int V> constexpr bool kRing = V * int(sizeof(X) < sizeof(S) ? sizeof(X) : sizeof(S)) >= 16;
+// Rows per turn: 32 bytes per lane of the ring, or 16 columns.
+constexpr int kTurnBytes = 32;
+template <typename X, typename S, int V, int K, bool RES> constexpr int kRowBytes = K * V * int(sizeof(X) + (RES ? sizeof(S) : 0));     // per lane
+template <typename X, typename S, int V, int L, int K, bool RES> constexpr int kTurnRows =
+    L == 0 ? 1 : kRing<X, S, V> ? (kRowBytes<X, S, V, K, RES> >= kTurnBytes ? 1 : kTurnBytes / kRowBytes<X, S, V, K, RES>)
+                                : V * K >= 16 ? 1 : 16 / (V * K) < 4 ? 16 / (V * K) : 4;
 
-template <typename X, typename S, typename Y, int V, int L, int K, bool QUANT>
+template <typename X, typename S, typename Y, int V, int L, int K, bool QUANT, bool RES>
 __global__ void __launch_bounds__(L ? kWarpRowThreads : kRowThreads, L ? 2 : 1) rms_fwd_kernel(const __grid_constant__ RmsArgs p) {
     hagk::pdl_launch_dependents();
-    constexpr int R = L ? kTurnRows<V * K> : 1;
-    using P = Place<L, K>;
+    constexpr int R = kTurnRows<X, S, V, L, K, RES>;
+    constexpr bool RING = kRing<X, S, V>;
+    using P = Place<L, K, QUANT && V == 1>;
+    using CX = ChunkCopy<X, V, P, K>;
+    using CS = ChunkCopy<S, V, P, K>;
+    extern __shared__ __align__(16) char raw[];
     __shared__ float slots[4][32];
     const P at;
     const int n_vec = p.D / V;
     const float inverse = 1.0f / float(p.D);
-    const bool res = p.res != nullptr;
-    bool mine[K];
-    float w[K][V];
-    hagk::pdl_wait();
+    const int64_t ld_x = p.ld_x * int64_t(sizeof(X)), ld_res = p.ld_res * int64_t(sizeof(S));
+    const int row_bytes = CX::bytes() + (RES ? CS::bytes() : 0), stage = R * row_bytes, end = p.stages * stage;
+    int64_t next = at.group * R;
+    int write = 0, read = 0;
+    auto issue = [&]() {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        mine[k] = at.first + k * P::kStep < n_vec;
-        if (mine[k]) load_weights<V>(w[k], p.w, p.w_bf16, p.w_vectors, int64_t(at.first + k * P::kStep) * V);
+        for (int i = 0; i < R; ++i) {
+            const int64_t r = next + i;
+            char *const to = raw + write + i * row_bytes;
+            CX::issue(to, static_cast<const char *>(p.x) + r * ld_x, at, n_vec, r < p.n);
+            if (RES) CS::issue(to + CX::bytes(), static_cast<const char *>(p.res) + r * ld_res, at, n_vec, r < p.n);
+        }
+        hagr::commit_copies();
+        next += at.groups * R;
+        write = write + stage == end ? 0 : write + stage;
+    };
+    hagk::pdl_wait();
+    if constexpr (RING) {
+        for (int s = 0; s < p.stages; ++s) issue();
     }
+    hagr::Pairs<V> w[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) w[k].fill(0.0f);
+    load_all_weights<V, K>(w, p.w, p.w_bf16, p.w_vectors, at, n_vec);
     int turn = 0;
     for (int64_t lead = at.leader() * R, r0 = at.group * R; lead < p.n; lead += at.groups * R, r0 += at.groups * R, turn ^= 1) {
-        float h[R][K][V], s[R];
-        {
-            Wide<X, V> x[R][K];
-            Wide<S, V> q[R][K];
+        hagr::Pairs<V> h[R][K];
+        float s[R];
+        if constexpr (RING) {
+            hagr::wait_oldest(p.stages);
+            if (CX::kCrosses || (RES && CS::kCrosses)) __syncwarp();
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const char *from = raw + read + i * row_bytes;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    h[i][k] = CX::get(from, at, k);
+                    if (RES) h[i][k].add(CS::get(from + CX::bytes(), at, k));
+                }
+            }
+            if (CX::kCrosses || (RES && CS::kCrosses)) __syncwarp();
+            issue();
+            read = read + stage == end ? 0 : read + stage;
+        } else {
+            hagr::Vec<X, V> x[R][K];
+            hagr::Vec<S, V> q[R][K];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const bool live = r0 + i < p.n;
+                const char *xr = static_cast<const char *>(p.x) + (r0 + i) * ld_x, *qr = static_cast<const char *>(p.res) + (r0 + i) * ld_res;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    x[i][k].zero();
+                    if (live && at.mine(k, n_vec)) x[i][k].template load<hagr::kKeep>(xr, at.vec(k));
+                }
+                if (RES) {
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        q[i][k].zero();
+                        if (live && at.mine(k, n_vec)) q[i][k].template load<hagr::kKeep>(qr, at.vec(k));
+                    }
+                }
+            }
 #pragma unroll
             for (int i = 0; i < R; ++i)
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    x[i][k].v.zero();
-                    q[i][k].v.zero();
-                    if (mine[k] && r0 + i < p.n) {
-                        x[i][k].load(static_cast<const X *>(p.x) + (r0 + i) * p.ld_x, at.first + k * P::kStep);
-                        if (res) q[i][k].load(static_cast<const S *>(p.res) + (r0 + i) * p.ld_res, at.first + k * P::kStep);
-                    }
+                    h[i][k] = hagr::widen(x[i][k]);
+                    if (RES) h[i][k].add(hagr::widen(q[i][k]));
                 }
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                s[i] = 0.0f;
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    add_rows<X, S, V>(h[i][k], x[i][k], q[i][k], res);
-                    float t = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < V; ++j) t = fmaf(h[i][k][j], h[i][k][j], t);
-                    s[i] += t;
-                }
-            }
         }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            s[i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) s[i] += h[i][k].dot(h[i][k]);
+        }
+        const Sums<L, R> rstds(s, slots[turn], [&](float q) { return rsqrtf(q * inverse + p.eps); });
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int64_t r = r0 + i;
             const bool live = r < p.n;
-            const float rstd = rsqrtf(group_sum<L>(s[i], slots[turn]) * inverse + p.eps);
-            if (p.rstd && live && at.first == 0) p.rstd[r] = rstd;
+            const float rstd = rstds.get(i);
+            if (p.rstd && live && at.first()) p.rstd[r] = rstd;
             if (p.total && live) {
+                char *const to = static_cast<char *>(p.total) + r * p.ld_total * int64_t(sizeof(S));
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
                     Wide<S, V> o;
-                    o.v.set(h[i][k]);
-                    if (mine[k]) o.store(static_cast<S *>(p.total) + r * p.ld_total, at.first + k * P::kStep);
+                    o.v.set(h[i][k].v);
+                    if (at.mine(k, n_vec)) o.store(to, at.vec(k));
                 }
             }
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j) h[i][k][j] = mine[k] ? h[i][k][j] * rstd * w[k][j] : 0.0f;
+            for (int k = 0; k < K; ++k) {
+                h[i][k].mul_all(rstd);
+                h[i][k].mul(w[k]);
+            }
+            char *const to = static_cast<char *>(p.y) + r * p.ld_y * int64_t(sizeof(Y));
             if constexpr (!QUANT) {
                 if (live) {
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
                         Wide<Y, V> o;
-                        o.v.set(h[i][k]);
-                        if (mine[k]) o.store(static_cast<Y *>(p.y) + r * p.ld_y, at.first + k * P::kStep);
+                        o.v.set(h[i][k].v);
+                        if (at.mine(k, n_vec)) o.store(to, at.vec(k));
                     }
                 }
             } else if (p.block) {
-                quant_blocks<V, K, P::kStep>(h[i], p, r, at.first, n_vec, live);
+                quant_blocks<V, K>(h[i], p, r, at, n_vec, live);
             } else {
                 float top = 0.0f;
 #pragma unroll
                 for (int k = 0; k < K; ++k)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) top = larger(top, fabsf(h[i][k][j]));
+                    for (int j = 0; j < V; ++j) top = larger(top, h[i][k].v[j]);
                 const float scale = scale_of(group_largest<L>(top, slots[2 + turn]), p), inv = __fdividef(1.0f, scale);
                 if (!live) continue;
-                if (at.first == 0) p.scales[r] = scale;
+                if (at.first()) p.scales[r] = scale;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) h[i][k][j] *= inv;
-                    if (mine[k]) store_codes<V>(h[i][k], static_cast<char *>(p.y) + r * p.ld_y, at.first + k * P::kStep, p.int8);
+                    h[i][k].mul_all(inv);
+                    if (at.mine(k, n_vec)) store_codes<V>(h[i][k].v, to, at.vec(k), p.int8);
                 }
             }
         }
     }
+    if constexpr (RING) hagr::wait_copies<0>();
 }
 
 // Rows of more columns: a block walks its row, a warp 32 K vectors at a time, once for the squares, once more for the
@@ -240,50 +289,55 @@ __global__ void __launch_bounds__(L ? kWarpRowThreads : kRowThreads, L ? 2 : 1) 
 template <typename X, typename S, typename Y, int V, bool QUANT>
 __global__ void __launch_bounds__(kRowThreads, 1) rms_fwd_long_kernel(const __grid_constant__ RmsArgs p) {
     hagk::pdl_launch_dependents();
-    constexpr int K = 4;
+    constexpr int K = V == 8 ? 2 : 4;
     __shared__ float slots[2][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n_vec = p.D / V, stride = (kRowThreads / 32) * 32 * K;
     const bool res = p.res != nullptr;
+    struct Walk {                                                      // K chunks side by side
+        int base;
+        __device__ __forceinline__ int vec(int k) const { return base + k * 32; }
+        __device__ __forceinline__ bool mine(int k, int n) const { return base + k * 32 < n; }
+    };
     hagk::pdl_wait();
     for (int64_t r = blockIdx.x; r < p.n; r += gridDim.x) {
         const X *xr = static_cast<const X *>(p.x) + r * p.ld_x;
         const S *qr = static_cast<const S *>(p.res) + (res ? r * p.ld_res : 0);
-        auto rows = [&](int base, float (&h)[K][V]) {                  // the sums of 32 K vectors from `base` on
+        auto rows = [&](const Walk &at, hagr::Pairs<V> (&h)[K]) {      // the sums of K vectors
             Wide<X, V> x[K];
             Wide<S, V> q[K];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 x[k].v.zero();
                 q[k].v.zero();
-                if (base + k * 32 + lane < n_vec) {
-                    x[k].load(xr, base + k * 32 + lane);
-                    if (res) q[k].load(qr, base + k * 32 + lane);
+                if (at.mine(k, n_vec)) {
+                    x[k].load(xr, at.vec(k));
+                    if (res) q[k].load(qr, at.vec(k));
                 }
             }
 #pragma unroll
-            for (int k = 0; k < K; ++k) add_rows<X, S, V>(h[k], x[k], q[k], res);
-        };
-        auto scaled = [&](int base, float rstd, float (&h)[K][V]) {
-#pragma unroll
             for (int k = 0; k < K; ++k) {
-                float w[V];
-                const int vec = base + k * 32 + lane;
-                if (vec < n_vec) load_weights<V>(w, p.w, p.w_bf16, p.w_vectors, int64_t(vec) * V);
-#pragma unroll
-                for (int j = 0; j < V; ++j) h[k][j] = vec < n_vec ? h[k][j] * rstd * w[j] : 0.0f;
+                h[k] = hagr::widen(x[k].v);
+                if (res) h[k].add(hagr::widen(q[k].v));
             }
         };
-        float s = 0.0f, h[K][V];
-        for (int base = warp * 32 * K; base < n_vec; base += stride) {
-            rows(base, h);
+        auto scaled = [&](const Walk &at, float rstd, hagr::Pairs<V> (&h)[K]) {
+            hagr::Pairs<V> w[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k) w[k].fill(0.0f);
+            load_all_weights<V, K>(w, p.w, p.w_bf16, p.w_vectors, at, n_vec);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                float t = 0.0f;
-#pragma unroll
-                for (int j = 0; j < V; ++j) t = fmaf(h[k][j], h[k][j], t);
-                s += t;
+                h[k].mul_all(rstd);
+                h[k].mul(w[k]);
             }
+        };
+        float s = 0.0f;
+        hagr::Pairs<V> h[K];
+        for (Walk at{warp * 32 * K + lane}; at.base - lane < n_vec; at.base += stride) {
+            rows(at, h);
+#pragma unroll
+            for (int k = 0; k < K; ++k) s += h[k].dot(h[k]);
         }
         const float rstd = rsqrtf(group_sum<0>(s, slots[0]) / float(p.D) + p.eps);
         if (p.rstd && threadIdx.x == 0) p.rstd[r] = rstd;
@@ -291,45 +345,44 @@ __global__ void __launch_bounds__(kRowThreads, 1) rms_fwd_long_kernel(const __gr
         if constexpr (QUANT) {
             if (!p.block) {
                 float top = 0.0f;
-                for (int base = warp * 32 * K; base < n_vec; base += stride) {
-                    rows(base, h);
-                    scaled(base, rstd, h);
+                for (Walk at{warp * 32 * K + lane}; at.base - lane < n_vec; at.base += stride) {
+                    rows(at, h);
+                    scaled(at, rstd, h);
 #pragma unroll
                     for (int k = 0; k < K; ++k)
 #pragma unroll
-                        for (int j = 0; j < V; ++j) top = larger(top, fabsf(h[k][j]));
+                        for (int j = 0; j < V; ++j) top = larger(top, h[k].v[j]);
                 }
                 const float scale = scale_of(group_largest<0>(top, slots[1]), p);
                 if (threadIdx.x == 0) p.scales[r] = scale;
                 inv = __fdividef(1.0f, scale);
             }
         }
-        for (int base = warp * 32 * K; base < n_vec; base += stride) {
-            rows(base, h);
+        for (Walk at{warp * 32 * K + lane}; at.base - lane < n_vec; at.base += stride) {
+            rows(at, h);
             if (p.total) {
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
                     Wide<S, V> o;
-                    o.v.set(h[k]);
-                    if (base + k * 32 + lane < n_vec) o.store(static_cast<S *>(p.total) + r * p.ld_total, base + k * 32 + lane);
+                    o.v.set(h[k].v);
+                    if (at.mine(k, n_vec)) o.store(static_cast<S *>(p.total) + r * p.ld_total, at.vec(k));
                 }
             }
-            scaled(base, rstd, h);
+            scaled(at, rstd, h);
             if constexpr (!QUANT) {
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
                     Wide<Y, V> o;
-                    o.v.set(h[k]);
-                    if (base + k * 32 + lane < n_vec) o.store(static_cast<Y *>(p.y) + r * p.ld_y, base + k * 32 + lane);
+                    o.v.set(h[k].v);
+                    if (at.mine(k, n_vec)) o.store(static_cast<Y *>(p.y) + r * p.ld_y, at.vec(k));
                 }
             } else if (p.block) {
-                quant_blocks<V, K, 32>(h, p, r, base + lane, n_vec, true);
+                quant_blocks<V, K>(h, p, r, at, n_vec, true);
             } else {
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) h[k][j] *= inv;
-                    if (base + k * 32 + lane < n_vec) store_codes<V>(h[k], static_cast<char *>(p.y) + r * p.ld_y, base + k * 32 + lane, p.int8);
+                    h[k].mul_all(inv);
+                    if (at.mine(k, n_vec)) store_codes<V>(h[k].v, static_cast<char *>(p.y) + r * p.ld_y, at.vec(k), p.int8);
                 }
             }
         }
@@ -337,52 +390,94 @@ __global__ void __launch_bounds__(kRowThreads, 1) rms_fwd_long_kernel(const __gr
     }
 }
 
-template <typename X, typename S, typename Y, int V, int L, int K, bool QUANT>
-cudaError_t launch_rows(const RmsArgs &p, cudaStream_t s) {
-    constexpr auto kernel = rms_fwd_kernel<X, S, Y, V, L, K, QUANT>;
-    constexpr int R = L ? kTurnRows<V * K> : 1;
-    const unsigned threads = L ? kWarpRowThreads : unsigned((p.D / V + 32 * K - 1) / (32 * K)) * 32;
-    const int64_t rows = L ? int64_t(kWarpRowThreads / 32) * (32 / (L ? L : 32)) * R : 1;
-    const int64_t grid = std::min<int64_t>((p.n + rows - 1) / rows, int64_t(kSms) * blocks_per_sm<kernel>(threads, 0));
-    return launch(kernel, dim3(unsigned(grid)), threads, 0, p, s);
+// Threads per SM of the kernels with a ring: what is on its way at a time decides how near they come to the memory's rate.
+// Rows of up to 32 bytes per lane and turn: two stages of 512 threads (10^6 x 256 bf16 320 us, with three stages 365, with
+// twice the threads 333, with one stage of them 419).  More bytes per lane: one stage of 1536 threads (500 000 x 512 bf16
+// 313 us, with two stages of 512 threads 335; 10^6 x 256 bf16 around an fp32 stream 478 and 542).
+constexpr int kShortThreads = 512, kLongThreads = 1536;
+
+template <typename X, typename S, typename Y, int V, int L, int K, bool QUANT, bool RES>
+cudaError_t launch_rows(RmsArgs &p, int warps, cudaStream_t s) {
+    constexpr auto kernel = rms_fwd_kernel<X, S, Y, V, L, K, QUANT, RES>;
+    constexpr int R = kTurnRows<X, S, V, L, K, RES>, kGroup = L ? L : 32;
+    const unsigned threads = L ? kWarpRowThreads : unsigned(warps) * 32;
+    const cudaError_t err = allow_shared<kernel>();
+    if (err != cudaSuccess) return err;
+    const int64_t rows = L ? int64_t(kWarpRowThreads / kGroup) * R : 1;
+    size_t shared = 0;
+    int most = kSms;
+    if constexpr (kRing<X, S, V>) {
+        constexpr int kLane = R * kRowBytes<X, S, V, K, RES>;
+        constexpr bool kShort = kLane <= kTurnBytes || (L == 0 && QUANT);
+        p.stages = kShort ? 2 : 1;
+        shared = size_t(kLane) * threads * p.stages;
+        most = std::max(2, (kShort ? kShortThreads : kLongThreads) / int(threads));
+    }
+    most = std::min(most, blocks_per_sm<kernel>(threads, shared));
+    const int64_t grid = std::min<int64_t>((p.n + rows - 1) / rows, int64_t(kSms) * most);
+    return launch(kernel, dim3(unsigned(grid)), threads, shared, p, s);
 }
 
-// Rows of up to 32 columns per lane go to a warp or a part of one, wider ones to a block.
-template <typename X, typename S, typename Y, int V, bool QUANT>
-cudaError_t launch_width(const RmsArgs &p, cudaStream_t s) {
-    const int32_t n_vec = p.D / V;
+// Rows of up to 1024 columns (narrow vectors: 512) go to a warp or a part of one, wider ones to a block: the fewest warps
+// with 16 columns per thread, and then as few chunks per warp as they need.
+template <typename X, typename S, typename Y, int V, bool QUANT, bool RES>
+cudaError_t launch_width(RmsArgs &p, cudaStream_t s) {
+    const int32_t n_vec = p.D / V, chunks = (n_vec + 31) / 32;
     if (p.D > kMostInRegisters) {
         constexpr auto kernel = rms_fwd_long_kernel<X, S, Y, V, QUANT>;
         return launch(kernel, dim3(unsigned(std::min<int64_t>(p.n, int64_t(kSms) * blocks_per_sm<kernel>(kRowThreads, 0)))), kRowThreads, 0, p, s);
     }
-    if (n_vec <= 4) return launch_rows<X, S, Y, V, 4, 1, QUANT>(p, s);
-    if (n_vec <= 8) return launch_rows<X, S, Y, V, 8, 1, QUANT>(p, s);
-    if (n_vec <= 16) return launch_rows<X, S, Y, V, 16, 1, QUANT>(p, s);
-    if (n_vec <= 32) return launch_rows<X, S, Y, V, 32, 1, QUANT>(p, s);
-    if (n_vec <= 64) return launch_rows<X, S, Y, V, 32, 2, QUANT>(p, s);
-    if (n_vec <= 128) return launch_rows<X, S, Y, V, 32, 4, QUANT>(p, s);
-    if constexpr (V == 1) {
-        if (n_vec <= 256) return launch_rows<X, S, Y, V, 32, 8, QUANT>(p, s);
-        if (n_vec <= 512) return launch_rows<X, S, Y, V, 32, 16, QUANT>(p, s);
+    if constexpr (V > 1) {
+        if (n_vec == 1) return launch_rows<X, S, Y, V, 1, 1, QUANT, RES>(p, 1, s);
+        if (n_vec == 2) return launch_rows<X, S, Y, V, 2, 1, QUANT, RES>(p, 1, s);
     }
-    return launch_rows<X, S, Y, V, 0, kPerThread / V, QUANT>(p, s);
+    if (n_vec <= 4) return launch_rows<X, S, Y, V, 4, 1, QUANT, RES>(p, 1, s);
+    if (n_vec <= 8) return launch_rows<X, S, Y, V, 8, 1, QUANT, RES>(p, 1, s);
+    if (n_vec <= 16) return launch_rows<X, S, Y, V, 16, 1, QUANT, RES>(p, 1, s);
+    if (chunks == 1) return launch_rows<X, S, Y, V, 32, 1, QUANT, RES>(p, 1, s);
+    if (chunks == 2) return launch_rows<X, S, Y, V, 32, 2, QUANT, RES>(p, 1, s);
+    if (chunks <= 4) return launch_rows<X, S, Y, V, 32, 4, QUANT, RES>(p, 1, s);
+    if constexpr (V > 1) {
+        return launch_rows<X, S, Y, V, 0, kPerThread / V, QUANT, RES>(p, (chunks * V + kPerThread - 1) / kPerThread, s);
+    } else {
+        if (chunks <= 6) return launch_rows<X, S, Y, V, 32, 6, QUANT, RES>(p, 1, s);
+        if (chunks <= 8) return launch_rows<X, S, Y, V, 32, 8, QUANT, RES>(p, 1, s);
+        if (chunks <= 10) return launch_rows<X, S, Y, V, 32, 10, QUANT, RES>(p, 1, s);
+        if (chunks <= 12) return launch_rows<X, S, Y, V, 32, 12, QUANT, RES>(p, 1, s);
+        if (chunks <= 14) return launch_rows<X, S, Y, V, 32, 14, QUANT, RES>(p, 1, s);
+        if (chunks <= 16) return launch_rows<X, S, Y, V, 32, 16, QUANT, RES>(p, 1, s);
+        const int each = QUANT ? 4 : 2, units = (chunks + each - 1) / each;             // chunks that stay together
+        const int warps = (units * each + kPerThread - 1) / kPerThread, k = (units + warps - 1) / warps * each;
+        if constexpr (!QUANT) {
+            if (k <= 10) return launch_rows<X, S, Y, V, 0, 10, QUANT, RES>(p, warps, s);
+            if (k == 14) return launch_rows<X, S, Y, V, 0, 14, QUANT, RES>(p, warps, s);
+        }
+        if (k <= 12) return launch_rows<X, S, Y, V, 0, 12, QUANT, RES>(p, warps, s);
+        return launch_rows<X, S, Y, V, 0, 16, QUANT, RES>(p, warps, s);
+    }
 }
 
-template <typename X, typename S, typename Y, bool QUANT, int N>
-cudaError_t launch_typed(RmsArgs &p, const Matrix (&m)[N], cudaStream_t s) {
+template <typename X, typename S, typename Y, bool QUANT, bool RES, int N>
+cudaError_t launch_vectors(RmsArgs &p, const Matrix (&m)[N], cudaStream_t s) {
     constexpr int kMost = sizeof(X) == 2 || sizeof(Y) == 2 ? 8 : 4;       // the narrowest type fills 16 bytes
     const int we = p.w_bf16 ? 2 : 4;
     if (vectors_fit(kMost, p.D, m)) {
         p.w_vectors = on(p.w, std::min(16, kMost * we));
-        return launch_width<X, S, Y, kMost, QUANT>(p, s);
+        return launch_width<X, S, Y, kMost, QUANT, RES>(p, s);
     }
     if constexpr (kMost == 8)
         if (vectors_fit(4, p.D, m)) {
             p.w_vectors = on(p.w, 4 * we);
-            return launch_width<X, S, Y, 4, QUANT>(p, s);
+            return launch_width<X, S, Y, 4, QUANT, RES>(p, s);
         }
     p.w_vectors = 0;
-    return launch_width<X, S, Y, 1, QUANT>(p, s);
+    return launch_width<X, S, Y, 1, QUANT, RES>(p, s);
+}
+template <typename X, typename S, typename Y, bool QUANT, int N>
+cudaError_t launch_typed(RmsArgs &p, const Matrix (&m)[N], cudaStream_t s) {
+    if constexpr (std::is_same<X, S>::value)                              // an fp32 stream around bf16 is there
+        if (!p.res) return launch_vectors<X, S, Y, QUANT, false>(p, m, s);
+    return launch_vectors<X, S, Y, QUANT, true>(p, m, s);
 }
 
 bool types_ok(hag_dtype x, hag_dtype stream, hag_dtype y, bool res) {

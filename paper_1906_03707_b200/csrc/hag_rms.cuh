@@ -64,24 +64,35 @@ __device__ __forceinline__ void store_weight(void *p, int bf16, int64_t i, float
         static_cast<float *>(p)[i] = f;
     }
 }
-// V weights from column c on; `vectors`: whether they can be read as one
-template <int V>
-__device__ __forceinline__ void load_weights(float (&w)[V], const void *p, int bf16, bool vectors, int64_t c) {
-    if (vectors && p) {
-        if (bf16) {
-            hagr::Vec<__nv_bfloat16, V> q;
-            q.template load<hagr::kNear>(p, size_t(c) / V);
+// The weights of a thread's K vectors; `vectors`: whether they can be read as such.  Without weights they are ones.  One
+// test of the type for all of them: loads behind a test of their own would wait for one another.
+template <int V, int K, typename At>
+__device__ __forceinline__ void load_all_weights(hagr::Pairs<V> (&w)[K], const void *p, int bf16, bool vectors, const At &at, int n_vec) {
+    auto load = [&](auto type, auto width) {
+        using T = decltype(type);
+        constexpr int N = decltype(width)::value;
+        hagr::Vec<T, N> q[K][V / N];
 #pragma unroll
-            for (int j = 0; j < V; ++j) w[j] = q.get(j);
-        } else {
-            hagr::Vec<float, V> q;
-            q.template load<hagr::kNear>(p, size_t(c) / V);
+        for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int j = 0; j < V; ++j) w[j] = q.get(j);
-        }
+            for (int j = 0; j < V / N; ++j)
+                if (at.mine(k, n_vec)) q[k][j].template load<hagr::kNear>(p, size_t(at.vec(k)) * (V / N) + j);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (at.mine(k, n_vec)) w[k].v[j] = q[k][j / N].get(j % N);
+    };
+    if (!p) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (at.mine(k, n_vec)) w[k].fill(1.0f);
+    } else if (vectors) {
+        if (bf16) load(__nv_bfloat16(), std::integral_constant<int, V>());
+        else load(float(), std::integral_constant<int, V>());
     } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) w[j] = load_weight(p, bf16, c + j);
+        if (bf16) load(__nv_bfloat16(), std::integral_constant<int, 1>());
+        else load(float(), std::integral_constant<int, 1>());
     }
 }
 
@@ -100,28 +111,99 @@ __device__ __forceinline__ float group_sum(float v, float *slot) {
 }
 
 // The place of a thread in its row, and of its row among the others.
-//   L > 0: L lanes of a warp per row, 32 / L rows per warp; L = 0: a block per row, 32 K vectors per warp.
-// Vector k of the thread is number first + k * kStep of the row.
-template <int L, int K>
+//   L > 0: L lanes of a warp per row, 32 / L rows per warp; L = 0: a block per row.
+// A thread has K vectors of the row.  Neighbouring lanes have neighbouring vectors, 32 (or L) of them are a chunk, and the
+// warps of a block take chunks in turn; GROUPED: four chunks in turn, so that 128 columns of V = 1 lie in one warp.  Of the
+// widths that a kernel is launched with, all chunks but the last kPartial of a thread lie within the row.
+template <int L, int K, bool GROUPED>
 struct Place {
-    static constexpr int kStep = L ? L : 32;
-    int first;
-    int64_t group, groups;         // of this thread, and of the launch
+    static constexpr int kLanes = L ? L : 32;
+    static constexpr bool kWarpRows = L > 0;
+    static constexpr int kPartial = GROUPED && L == 0 ? 4 : K >= 4 ? 2 : 1;
+    int lane, warp, warps;                     // lane of the group that shares a row; warp of the row's
+    int64_t group, groups;                     // of this thread, and of the launch
     __device__ __forceinline__ Place() {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         if constexpr (L) {
-            constexpr int G = 32 / (L ? L : 32);
-            first = lane % (L ? L : 32);
-            group = (int64_t(blockIdx.x) * (kWarpRowThreads / 32) + warp) * G + lane / (L ? L : 32);
+            constexpr int G = 32 / kLanes;
+            lane = threadIdx.x % kLanes;
+            warp = 0;
+            warps = 1;
+            group = (int64_t(blockIdx.x) * (kWarpRowThreads / 32) + (threadIdx.x >> 5)) * G + (threadIdx.x & 31) / kLanes;
             groups = int64_t(gridDim.x) * (kWarpRowThreads / 32) * G;
         } else {
-            first = warp * 32 * K + lane;
+            lane = threadIdx.x & 31;
+            warp = threadIdx.x >> 5;
+            warps = blockDim.x >> 5;
             group = blockIdx.x;
             groups = gridDim.x;
         }
     }
+    __device__ __forceinline__ int chunk(int k) const {        // first vector of chunk k
+        if constexpr (L) return k * kLanes;
+        else if constexpr (GROUPED) return ((k / 4 * warps + warp) * 4 + k % 4) * 32;
+        else return (k * warps + warp) * 32;
+    }
+    __device__ __forceinline__ int vec(int k) const { return chunk(k) + lane; }
+    __device__ __forceinline__ bool mine(int k, int n_vec) const { return k < K - kPartial || vec(k) < n_vec; }
+    __device__ __forceinline__ bool first() const { return lane == 0 && warp == 0; }
     // the group whose rows decide how many turns the warp takes
-    __device__ __forceinline__ int64_t leader() const { return L ? group - (threadIdx.x & 31) / (L ? L : 32) : group; }
+    __device__ __forceinline__ int64_t leader() const { return L ? group - (threadIdx.x & 31) / kLanes : group; }
+};
+
+// Sums of R values over the lanes (or the block) that share a row; get(i) is the i-th in every lane, after f was applied to
+// it.  Where there are more lanes than rows the sums are spread over the lanes, and f is computed once.
+template <int L, int R>
+struct Sums {
+    static constexpr bool kSpread = L >= 2 * R && R > 1;
+    float v[kSpread ? 1 : R];
+    template <typename F>
+    __device__ __forceinline__ Sums(const float (&s)[R], float *slot, F f) {
+        if constexpr (kSpread) {
+            v[0] = f(hagr::spread_sums<L, R>(s, threadIdx.x % L));
+        } else {
+            static_assert(L > 0 || R == 1, "");
+#pragma unroll
+            for (int i = 0; i < R; ++i) v[i] = f(group_sum<L>(s[i], slot));
+        }
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (kSpread) return hagr::spread_get<L, R>(v[0], i, threadIdx.x & 31);
+        else return v[i];
+    }
+};
+
+// Rows on their way into shared memory: chunk k of all groups (or warps) of the block side by side, then chunk k + 1.  A
+// chunk is copied 16 bytes per lane at a time; where a vector has 32 bytes, a lane reads what its neighbours copied.
+template <typename T, int V, typename P, int K>
+struct ChunkCopy {
+    static constexpr int kVector = V * int(sizeof(T)), kChunk = P::kLanes * kVector;
+    static constexpr bool kCrosses = kVector > 16;             // lanes read each other's copies
+    // a row that does not exist, and vectors beyond it, are zeros
+    static __device__ __forceinline__ int threads() { return P::kLanes < 32 || P::kWarpRows ? kWarpRowThreads : int(blockDim.x); }
+    static __device__ __forceinline__ int group() { return int(threadIdx.x) / P::kLanes * kChunk; }
+    static __device__ __forceinline__ int bytes() { return K * threads() * kVector; }          // of a row of each group
+    static __device__ __forceinline__ void issue(char *to, const char *row, const P &at, int n_vec, bool live) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < kVector / 16; ++j) {
+                const int piece = (j * P::kLanes + at.lane) * 16;
+                const int64_t from = int64_t(at.chunk(k)) * kVector + piece;
+                char *const slot = to + k * threads() * kVector + group() + piece;
+                if (live && (k < K - P::kPartial || from < int64_t(n_vec) * kVector)) hagr::copy_async<16>(slot, row + from);
+                else *reinterpret_cast<uint4 *>(slot) = make_uint4(0, 0, 0, 0);
+            }
+    }
+    static __device__ __forceinline__ hagr::Pairs<V> get(const char *from, const P &at, int k) {
+        hagr::Vec<T, V> v;
+        const char *slot = from + k * threads() * kVector + group() + at.lane * kVector;
+#pragma unroll
+        for (int j = 0; j < kVector / 16; ++j) {
+            const uint4 q = reinterpret_cast<const uint4 *>(slot)[j];
+            v.raw.w[4 * j] = q.x; v.raw.w[4 * j + 1] = q.y; v.raw.w[4 * j + 2] = q.z; v.raw.w[4 * j + 3] = q.w;
+        }
+        return hagr::widen(v);
+    }
 };
 
 template <typename Args>
@@ -137,6 +219,20 @@ cudaError_t launch(void (*kernel)(Args), dim3 grid, unsigned threads, size_t sha
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+constexpr int kSmShared = 227 * 1024;      // shared memory that the blocks of an SM can use, and one block
+// Lets a kernel use the shared memory of the current device's SMs (once per kernel and device).
+template <auto KERNEL>
+cudaError_t allow_shared() {
+    static std::atomic<uint64_t> ready{0};
+    int device = 0;
+    cudaError_t err = cudaGetDevice(&device);
+    const uint64_t bit = uint64_t(1) << (device & 63);
+    if (err != cudaSuccess || (ready.load(std::memory_order_relaxed) & bit)) return err;
+    err = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmShared - 2048);
+    if (err == cudaSuccess) ready.fetch_or(bit, std::memory_order_relaxed);
+    return err;
 }
 
 // How many blocks of the kernel an SM runs at once (asked once per kernel and number of warps).

@@ -19,6 +19,7 @@ struct RmsBwdArgs {
     void *out, *x;                          // x: the gradient in bf16 besides
     float *partial;                         // [parts][D]; NULL: gw is not wanted
     void *gw;
+    int32_t stages;                         // of the ring
     int32_t parts;                          // blocks that leave a sum of their own
     bool joined;                            // the only block leaves gw itself
 };
@@ -30,114 +31,189 @@ __device__ __forceinline__ void leave(const RmsBwdArgs &p, int64_t c, float v) {
 }
 
 template <typename S, int V>
-__device__ __forceinline__ void store_gradient(const RmsBwdArgs &p, int64_t r, int64_t vec, const float (&o)[V]) {
+__device__ __forceinline__ void store_gradient(const RmsBwdArgs &p, int64_t r, int64_t vec, const hagr::Pairs<V> &o) {
     Wide<S, V> a;
-    a.v.set(o);
+    a.v.set(o.v);
     a.store(static_cast<S *>(p.out) + r * p.ld_out, vec);
     if constexpr (sizeof(S) == 4) {
         if (p.x) {
             Wide<__nv_bfloat16, V> b;
-            b.v.set(o);
+            b.v.set(o.v);
             b.store(static_cast<__nv_bfloat16 *>(p.x) + r * p.ld_x, vec);
         }
     }
 }
 
-template <int PER_LANE> constexpr int kTurnRows = PER_LANE <= 8 ? 2 : 1;
+// Rows whose vectors fill 16 bytes are copied into a ring in shared memory some turns ahead; others are read when their turn
+// comes, all of them before the first is used.
+template <typename Y, int V> constexpr bool kRing = V * int(sizeof(Y)) >= 16;
+// Rows per turn: two where they are 96 bytes per lane of the ring (10^6 x 256 bf16 295 us, with one 323; of one or two
+// lanes one: 2 000 000 x 8 bf16 27 us, with two 36), or 8 columns.  Two stages of as much, one of more or where lanes read
+// what others copied (100 000 x 1024 fp32 237 us, with two 256; 10^6 x 256 bf16 around an fp32 stream 623 and 665;
+// 500 000 x 512 bf16 304, with two 293).
+constexpr int kTurnBytes = 96;
+template <typename S, typename Y, int V, int K, bool ALONG> constexpr int kRowBytes = K * V * int(sizeof(Y) + (ALONG ? 2 : 1) * sizeof(S));    // per lane
+template <typename S, typename Y, int V, int L, int K, bool ALONG> constexpr int kTurnRows =
+    L == 0 ? 1 : kRing<Y, V> ? (kRowBytes<S, Y, V, K, ALONG> * 2 <= kTurnBytes && L > 2 ? 2 : 1) : V * K <= 4 ? 4 : V * K <= 8 ? 2 : 1;
 
-template <typename S, typename Y, int V, int L, int K>
+template <typename S, typename Y, int V, int L, int K, bool ALONG>
 __global__ void __launch_bounds__(L ? kWarpRowThreads : kRowThreads, L ? 2 : 1) rms_bwd_kernel(const __grid_constant__ RmsBwdArgs p) {
     hagk::pdl_launch_dependents();
-    constexpr int R = L ? kTurnRows<V * K> : 1;
-    using P = Place<L, K>;
+    constexpr int R = kTurnRows<S, Y, V, L, K, ALONG>;
+    constexpr bool RING = kRing<Y, V>;
+    using P = Place<L, K, false>;
+    using CY = ChunkCopy<Y, V, P, K>;
+    using CS = ChunkCopy<S, V, P, K>;
+    using Values = hagr::Pairs<V>;
+    extern __shared__ __align__(16) char raw[];
     __shared__ float slots[2][32];
     const P at;
     const int n_vec = p.D / V;
     const float inverse = 1.0f / float(p.D);
-    bool mine[K];
-    float w[K][V], sum[K][V];
-    hagk::pdl_wait();
+    const int64_t ld_g = p.ld_g * int64_t(sizeof(Y)), ld_total = p.ld_total * int64_t(sizeof(S)), ld_along = p.ld_along * int64_t(sizeof(S));
+    const int row_bytes = CY::bytes() + (ALONG ? 2 : 1) * CS::bytes(), stage = R * row_bytes, end = p.stages * stage;
+    int64_t next = at.group * R;
+    int write = 0, read = 0;
+    float rstd_next[R];
+    auto statistics = [&](int64_t r) {                         // of a turn ahead
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        mine[k] = at.first + k * P::kStep < n_vec;
-#pragma unroll
-        for (int j = 0; j < V; ++j) w[k][j] = sum[k][j] = 0.0f;
-        if (mine[k]) load_weights<V>(w[k], p.w, p.w_bf16, p.w_vectors, int64_t(at.first + k * P::kStep) * V);
-    }
-    int turn = 0;
-    for (int64_t lead = at.leader() * R, r0 = at.group * R; lead < p.n; lead += at.groups * R, r0 += at.groups * R, turn ^= 1) {
-        Wide<Y, V> g[R][K];
-        Wide<S, V> t[R][K], a[R][K];
-        float rstd[R];
+        for (int i = 0; i < R; ++i) rstd_next[i] = r + i < p.n ? __ldcg(p.rstd + r + i) : 0.0f;
+    };
+    auto issue = [&]() {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            rstd[i] = r0 + i < p.n ? __ldcg(p.rstd + r0 + i) : 0.0f;
+            const int64_t r = next + i;
+            char *const to = raw + write + i * row_bytes;
+            CY::issue(to, static_cast<const char *>(p.g) + r * ld_g, at, n_vec, r < p.n);
+            CS::issue(to + CY::bytes(), static_cast<const char *>(p.total) + r * ld_total, at, n_vec, r < p.n);
+            if (ALONG) CS::issue(to + CY::bytes() + CS::bytes(), static_cast<const char *>(p.along) + r * ld_along, at, n_vec, r < p.n);
+        }
+        hagr::commit_copies();
+        next += at.groups * R;
+        write = write + stage == end ? 0 : write + stage;
+    };
+    hagk::pdl_wait();
+    if constexpr (RING) {
+        for (int s = 0; s < p.stages; ++s) issue();
+    }
+    statistics(at.group * R);
+    Values w[K], sum[K];
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                g[i][k].v.zero();
-                t[i][k].v.zero();
-                a[i][k].v.zero();
-                if (mine[k] && r0 + i < p.n) {
-                    const int vec = at.first + k * P::kStep;
-                    g[i][k].load(static_cast<const Y *>(p.g) + (r0 + i) * p.ld_g, vec);
-                    t[i][k].load(static_cast<const S *>(p.total) + (r0 + i) * p.ld_total, vec);
-                    if (p.along) a[i][k].load(static_cast<const S *>(p.along) + (r0 + i) * p.ld_along, vec);
+    for (int k = 0; k < K; ++k) {
+        w[k].fill(0.0f);
+        sum[k].fill(0.0f);
+    }
+    load_all_weights<V, K>(w, p.w, p.w_bf16, p.w_vectors, at, n_vec);
+    int turn = 0;
+    for (int64_t lead = at.leader() * R, r0 = at.group * R; lead < p.n; lead += at.groups * R, r0 += at.groups * R, turn ^= 1) {
+        Values hh[R][K], q[R][K], a[R][K];
+        float rstd[R], s[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) rstd[i] = rstd_next[i];
+        statistics(r0 + at.groups * R);
+        if constexpr (RING) {
+            hagr::wait_oldest(p.stages);
+            if (CY::kCrosses || CS::kCrosses) __syncwarp();
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const char *from = raw + read + i * row_bytes;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    q[i][k] = CY::get(from, at, k);
+                    hh[i][k] = CS::get(from + CY::bytes(), at, k);
+                    if (ALONG) a[i][k] = CS::get(from + CY::bytes() + CS::bytes(), at, k);
+                    else a[i][k].fill(0.0f);
                 }
             }
+            if (CY::kCrosses || CS::kCrosses) __syncwarp();
+            issue();
+            read = read + stage == end ? 0 : read + stage;
+        } else {
+            hagr::Vec<Y, V> g[R][K];
+            hagr::Vec<S, V> t[R][K], b[R][K];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const bool live = r0 + i < p.n;
+                const char *gr = static_cast<const char *>(p.g) + (r0 + i) * ld_g, *tr = static_cast<const char *>(p.total) + (r0 + i) * ld_total;
+                const char *br = static_cast<const char *>(p.along) + (r0 + i) * ld_along;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    g[i][k].zero();
+                    t[i][k].zero();
+                    if (live && at.mine(k, n_vec)) {
+                        g[i][k].template load<hagr::kKeep>(gr, at.vec(k));
+                        t[i][k].template load<hagr::kKeep>(tr, at.vec(k));
+                    }
+                }
+                if (ALONG) {
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        b[i][k].zero();
+                        if (live && at.mine(k, n_vec)) b[i][k].template load<hagr::kKeep>(br, at.vec(k));
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    q[i][k] = hagr::widen(g[i][k]);
+                    hh[i][k] = hagr::widen(t[i][k]);
+                    if (ALONG) a[i][k] = hagr::widen(b[i][k]);
+                    else a[i][k].fill(0.0f);
+                }
         }
-        float s[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             s[i] = 0.0f;
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float d = g[i][k].v.get(j) * (t[i][k].v.get(j) * rstd[i]);
-                    sum[k][j] += d;
-                    s[i] = fmaf(d, w[k][j], s[i]);
-                }
+            for (int k = 0; k < K; ++k) {
+                hh[i][k].mul_all(rstd[i]);
+                sum[k].fma(q[i][k], hh[i][k]);
+                q[i][k].mul(w[k]);
+                s[i] += q[i][k].dot(hh[i][k]);
+            }
         }
+        const Sums<L, R> means(s, slots[turn], [&](float v) { return -v * inverse; });
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const float m = group_sum<L>(s[i], slots[turn]) * inverse;
+            const float m = means.get(i);
             if (r0 + i >= p.n) continue;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                float o[V];
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float hh = t[i][k].v.get(j) * rstd[i];
-                    o[j] = fmaf(rstd[i], fmaf(-hh, m, g[i][k].v.get(j) * w[k][j]), a[i][k].v.get(j));
-                }
-                if (mine[k]) store_gradient<S, V>(p, r0 + i, at.first + k * P::kStep, o);
+                hh[i][k].affine(m, q[i][k]);
+                a[i][k].add_scaled(hh[i][k], rstd[i]);
+                if (at.mine(k, n_vec)) store_gradient<S, V>(p, r0 + i, at.vec(k), a[i][k]);
             }
         }
     }
+    if constexpr (RING) hagr::wait_copies<0>();
     if (!p.partial) return;
     if constexpr (L == 0) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (mine[k]) leave(p, int64_t(at.first + k * 32) * V + j, sum[k][j]);
+                if (at.mine(k, n_vec)) leave(p, int64_t(at.vec(k)) * V + j, sum[k].v[j]);
     } else {
         // groups of the warp, then warps of the block, in a fixed order
         constexpr int C = L * K * V, kWarps = kWarpRowThreads / 32;
-        __shared__ float joined[kWarps][C];
+        float *const joined = reinterpret_cast<float *>(raw);              // [warps][C], over the ring
+        __syncthreads();
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
+                float v = sum[k].v[j];
 #pragma unroll
-                for (int o = L; o < 32; o <<= 1) sum[k][j] += __shfl_xor_sync(0xffffffffu, sum[k][j], o);
-                if ((threadIdx.x & 31) < L) joined[threadIdx.x >> 5][(at.first + k * L) * V + j] = sum[k][j];
+                for (int o = L; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                if ((threadIdx.x & 31) < L) joined[(threadIdx.x >> 5) * C + at.vec(k) * V + j] = v;
             }
         __syncthreads();
         for (int c = threadIdx.x; c < p.D; c += kWarpRowThreads) {
             float v = 0.0f;
 #pragma unroll
-            for (int q = 0; q < kWarps; ++q) v += joined[q][c];
+            for (int o = 0; o < kWarps; ++o) v += joined[o * C + c];
             leave(p, c, v);
         }
     }
@@ -146,84 +222,100 @@ __global__ void __launch_bounds__(L ? kWarpRowThreads : kRowThreads, L ? 2 : 1) 
 template <typename S, typename Y, int V>
 __global__ void __launch_bounds__(kRowThreads, 1) rms_bwd_long_kernel(const __grid_constant__ RmsBwdArgs p) {
     hagk::pdl_launch_dependents();
-    constexpr int K = 2;
-    extern __shared__ __align__(16) float sums[];            // [D] where gw is wanted from this kernel
+    constexpr int K = V == 8 ? 1 : V == 4 ? 2 : 4;
+    using Values = hagr::Pairs<V>;
+    extern __shared__ __align__(16) char raw[];               // gw where it is wanted from this kernel, in planes of a vector's elements
+    float *const sums = reinterpret_cast<float *>(raw);
     __shared__ float slots[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n_vec = p.D / V, stride = (kRowThreads / 32) * 32 * K;
+    struct Walk {                                             // K chunks side by side
+        int base;
+        __device__ __forceinline__ int vec(int k) const { return base + k * 32; }
+        __device__ __forceinline__ bool mine(int k, int n) const { return base + k * 32 < n; }
+    };
+    auto walk = [&](auto f) {
+        for (Walk at{warp * 32 * K + lane}; at.base - lane < n_vec; at.base += stride) f(at);
+    };
     if (p.partial)                                            // a thread's own columns: no barrier is needed
-        for (int base = warp * 32 * K; base < n_vec; base += stride)
+        walk([&](const Walk &at) {
 #pragma unroll
             for (int k = 0; k < K; ++k)
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    if (base + k * 32 + lane < n_vec) sums[(base + k * 32 + lane) * V + j] = 0.0f;
+                    if (at.mine(k, n_vec)) sums[j * n_vec + at.vec(k)] = 0.0f;
+        });
     hagk::pdl_wait();
     for (int64_t r = blockIdx.x; r < p.n; r += gridDim.x) {
         const Y *gr = static_cast<const Y *>(p.g) + r * p.ld_g;
         const S *tr = static_cast<const S *>(p.total) + r * p.ld_total;
         const S *ar = static_cast<const S *>(p.along) + (p.along ? r * p.ld_along : 0);
         const float rstd = __ldcg(p.rstd + r);
-        float s = 0.0f;
-        for (int base = warp * 32 * K; base < n_vec; base += stride) {
-            Wide<Y, V> g[K];
+        // hh and g of the vectors, and the weights
+        auto rows = [&](const Walk &at, Values (&hh)[K], Values (&g)[K], Values (&w)[K]) {
+            Wide<Y, V> x[K];
             Wide<S, V> t[K];
-            float w[K][V];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const int vec = base + k * 32 + lane;
-                if (vec >= n_vec) continue;
-                g[k].load(gr, vec);
-                t[k].load(tr, vec);
-                load_weights<V>(w[k], p.w, p.w_bf16, p.w_vectors, int64_t(vec) * V);
-            }
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int vec = base + k * 32 + lane;
-                if (vec >= n_vec) continue;
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float d = g[k].v.get(j) * (t[k].v.get(j) * rstd);
-                    if (p.partial) sums[vec * V + j] += d;
-                    s = fmaf(d, w[k][j], s);
+                x[k].v.zero();
+                t[k].v.zero();
+                w[k].fill(0.0f);
+                if (at.mine(k, n_vec)) {
+                    x[k].load(gr, at.vec(k));
+                    t[k].load(tr, at.vec(k));
                 }
             }
-        }
-        const float m = group_sum<0>(s, slots) / float(p.D);
-        for (int base = warp * 32 * K; base < n_vec; base += stride) {
-            Wide<Y, V> g[K];
-            Wide<S, V> t[K], a[K];
-            float w[K][V];
+            load_all_weights<V, K>(w, p.w, p.w_bf16, p.w_vectors, at, n_vec);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const int vec = base + k * 32 + lane;
+                g[k] = hagr::widen(x[k].v);
+                hh[k] = hagr::widen(t[k].v);
+                hh[k].mul_all(rstd);
+            }
+        };
+        float s = 0.0f;
+        walk([&](const Walk &at) {
+            Values hh[K], g[K], w[K];
+            rows(at, hh, g, w);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                g[k].mul(hh[k]);
+                if (p.partial && at.mine(k, n_vec)) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) sums[j * n_vec + at.vec(k)] += g[k].v[j];
+                }
+                s += g[k].dot(w[k]);
+            }
+        });
+        const float m = -group_sum<0>(s, slots) / float(p.D);
+        walk([&](const Walk &at) {
+            Values hh[K], g[K], w[K];
+            Wide<S, V> a[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
                 a[k].v.zero();
-                if (vec >= n_vec) continue;
-                g[k].load(gr, vec);
-                t[k].load(tr, vec);
-                if (p.along) a[k].load(ar, vec);
-                load_weights<V>(w[k], p.w, p.w_bf16, p.w_vectors, int64_t(vec) * V);
+                if (p.along && at.mine(k, n_vec)) a[k].load(ar, at.vec(k));
             }
+            rows(at, hh, g, w);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const int vec = base + k * 32 + lane;
-                if (vec >= n_vec) continue;
-                float o[V];
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    o[j] = fmaf(rstd, fmaf(-(t[k].v.get(j) * rstd), m, g[k].v.get(j) * w[k][j]), a[k].v.get(j));
-                store_gradient<S, V>(p, r, vec, o);
+                g[k].mul(w[k]);
+                hh[k].affine(m, g[k]);
+                Values o = hagr::widen(a[k].v);
+                o.add_scaled(hh[k], rstd);
+                if (at.mine(k, n_vec)) store_gradient<S, V>(p, r, at.vec(k), o);
             }
-        }
+        });
         __syncthreads();                                      // the slots are written again
     }
     if (!p.partial) return;
-    for (int base = warp * 32 * K; base < n_vec; base += stride)
+    walk([&](const Walk &at) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (base + k * 32 + lane < n_vec) leave(p, int64_t(base + k * 32 + lane) * V + j, sums[(base + k * 32 + lane) * V + j]);
+                if (at.mine(k, n_vec)) leave(p, int64_t(at.vec(k)) * V + j, sums[j * n_vec + at.vec(k)]);
+    });
 }
 
 // gw of one strip of 32 columns and one part of the rows, for rows whose gw does not fit in shared memory.
@@ -276,36 +368,31 @@ int most_parts(int32_t D) { return kSms * std::max(1, std::min(8, 16384 / D)); }
 // Values of a gradient that one block takes alone, without a second launch.
 constexpr int64_t kFewValues = 16384;
 
-// Lets a kernel use the shared memory of the current device's SMs (once per kernel and device).
-template <auto KERNEL>
-cudaError_t allow_shared() {
-    static std::atomic<uint64_t> ready{0};
-    int device = 0;
-    cudaError_t err = cudaGetDevice(&device);
-    const uint64_t bit = uint64_t(1) << (device & 63);
-    if (err != cudaSuccess || (ready.load(std::memory_order_relaxed) & bit)) return err;
-    err = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostInShared * 4);
-    if (err == cudaSuccess) ready.fetch_or(bit, std::memory_order_relaxed);
-    return err;
-}
-
-template <typename S, typename Y, int V, int L, int K>
-cudaError_t launch_rows(RmsBwdArgs &p, cudaStream_t s) {
-    constexpr auto kernel = rms_bwd_kernel<S, Y, V, L, K>;
-    constexpr int R = L ? kTurnRows<V * K> : 1;
-    const unsigned threads = L ? kWarpRowThreads : unsigned((p.D / V + 32 * K - 1) / (32 * K)) * 32;
-    const int64_t rows = L ? int64_t(kWarpRowThreads / 32) * (32 / (L ? L : 32)) * R : 1;
-    const int64_t most = std::min(kSms * blocks_per_sm<kernel>(threads, 0), most_parts(p.D));
-    int64_t grid = std::min<int64_t>((p.n + rows - 1) / rows, most);
+template <typename S, typename Y, int V, int L, int K, bool ALONG>
+cudaError_t launch_rows(RmsBwdArgs &p, int warps, cudaStream_t s) {
+    constexpr auto kernel = rms_bwd_kernel<S, Y, V, L, K, ALONG>;
+    constexpr int R = kTurnRows<S, Y, V, L, K, ALONG>, kGroup = L ? L : 32;
+    const unsigned threads = L ? kWarpRowThreads : unsigned(warps) * 32;
+    const cudaError_t err = allow_shared<kernel>();
+    if (err != cudaSuccess) return err;
+    size_t shared = size_t(threads / 32) * L * K * V * 4;
+    if constexpr (kRing<Y, V>) {
+        constexpr int kLane = R * kRowBytes<S, Y, V, K, ALONG>;
+        p.stages = kLane <= kTurnBytes && V * sizeof(S) == 16 ? 2 : 1;
+        shared = std::max(shared, size_t(kLane) * threads * p.stages);
+    }
+    const int most = blocks_per_sm<kernel>(threads, shared);
+    const int64_t rows = L ? int64_t(kWarpRowThreads / kGroup) * R : 1;
+    int64_t grid = std::min<int64_t>((p.n + rows - 1) / rows, std::min(kSms * most, most_parts(p.D)));
     if (L && p.partial && p.n * p.D <= kFewValues) grid = 1;
     p.parts = int32_t(grid);
     p.joined = grid == 1;
-    return launch(kernel, dim3(unsigned(grid)), threads, 0, p, s);
+    return launch(kernel, dim3(unsigned(grid)), threads, shared, p, s);
 }
 
-template <typename S, typename Y, int V>
+template <typename S, typename Y, int V, bool ALONG>
 cudaError_t launch_width(RmsBwdArgs &p, cudaStream_t s) {
-    const int32_t n_vec = p.D / V;
+    const int32_t n_vec = p.D / V, chunks = (n_vec + 31) / 32;
     if (p.D > kMostInRegisters) {
         constexpr auto kernel = rms_bwd_long_kernel<S, Y, V>;
         const cudaError_t err = allow_shared<kernel>();
@@ -323,35 +410,53 @@ cudaError_t launch_width(RmsBwdArgs &p, cudaStream_t s) {
         p.joined = grid == 1;
         return launch(kernel, dim3(grid), kRowThreads, p.partial ? size_t(p.D) * 4 : 0, p, s);
     }
-    if (n_vec <= 4) return launch_rows<S, Y, V, 4, 1>(p, s);
-    if (n_vec <= 8) return launch_rows<S, Y, V, 8, 1>(p, s);
-    if (n_vec <= 16) return launch_rows<S, Y, V, 16, 1>(p, s);
-    if (n_vec <= 32) return launch_rows<S, Y, V, 32, 1>(p, s);
-    if (n_vec <= 64) return launch_rows<S, Y, V, 32, 2>(p, s);
-    if constexpr (V < 8)
-        if (n_vec <= 128) return launch_rows<S, Y, V, 32, 4>(p, s);
-    if constexpr (V == 1) {
-        if (n_vec <= 256) return launch_rows<S, Y, V, 32, 8>(p, s);
-        if (n_vec <= 512) return launch_rows<S, Y, V, 32, 16>(p, s);
+    if constexpr (V > 1) {
+        if (n_vec == 1) return launch_rows<S, Y, V, 1, 1, ALONG>(p, 1, s);
+        if (n_vec == 2) return launch_rows<S, Y, V, 2, 1, ALONG>(p, 1, s);
     }
-    return launch_rows<S, Y, V, 0, kPerThread / V>(p, s);
+    if (n_vec <= 4) return launch_rows<S, Y, V, 4, 1, ALONG>(p, 1, s);
+    if (n_vec <= 8) return launch_rows<S, Y, V, 8, 1, ALONG>(p, 1, s);
+    if (n_vec <= 16) return launch_rows<S, Y, V, 16, 1, ALONG>(p, 1, s);
+    if (chunks == 1) return launch_rows<S, Y, V, 32, 1, ALONG>(p, 1, s);
+    if (chunks == 2) return launch_rows<S, Y, V, 32, 2, ALONG>(p, 1, s);
+    if constexpr (V < 8)
+        if (chunks <= 4) return launch_rows<S, Y, V, 32, 4, ALONG>(p, 1, s);
+    if constexpr (V > 1) {
+        return launch_rows<S, Y, V, 0, kPerThread / V, ALONG>(p, (chunks * V + kPerThread - 1) / kPerThread, s);
+    } else {
+        if (chunks <= 6) return launch_rows<S, Y, V, 32, 6, ALONG>(p, 1, s);
+        if (chunks <= 8) return launch_rows<S, Y, V, 32, 8, ALONG>(p, 1, s);
+        if (chunks <= 10) return launch_rows<S, Y, V, 32, 10, ALONG>(p, 1, s);
+        if (chunks <= 12) return launch_rows<S, Y, V, 32, 12, ALONG>(p, 1, s);
+        if (chunks <= 14) return launch_rows<S, Y, V, 32, 14, ALONG>(p, 1, s);
+        if (chunks <= 16) return launch_rows<S, Y, V, 32, 16, ALONG>(p, 1, s);
+        const int pairs = (chunks + 1) / 2, warps = (2 * pairs + kPerThread - 1) / kPerThread, k = (pairs + warps - 1) / warps * 2;
+        if (k <= 10) return launch_rows<S, Y, V, 0, 10, ALONG>(p, warps, s);
+        if (k <= 12) return launch_rows<S, Y, V, 0, 12, ALONG>(p, warps, s);
+        if (k <= 14) return launch_rows<S, Y, V, 0, 14, ALONG>(p, warps, s);
+        return launch_rows<S, Y, V, 0, 16, ALONG>(p, warps, s);
+    }
 }
 
-template <typename S, typename Y, int N>
-cudaError_t launch_typed(RmsBwdArgs &p, const Matrix (&m)[N], cudaStream_t s) {
+template <typename S, typename Y, bool ALONG, int N>
+cudaError_t launch_vectors(RmsBwdArgs &p, const Matrix (&m)[N], cudaStream_t s) {
     constexpr int kMost = sizeof(Y) == 2 ? 8 : 4;             // the narrowest type fills 16 bytes
     const int we = p.w_bf16 ? 2 : 4;
     if (vectors_fit(kMost, p.D, m)) {
         p.w_vectors = on(p.w, std::min(16, kMost * we));
-        return launch_width<S, Y, kMost>(p, s);
+        return launch_width<S, Y, kMost, ALONG>(p, s);
     }
     if constexpr (kMost == 8)
         if (vectors_fit(4, p.D, m)) {
             p.w_vectors = on(p.w, 4 * we);
-            return launch_width<S, Y, 4>(p, s);
+            return launch_width<S, Y, 4, ALONG>(p, s);
         }
     p.w_vectors = 0;
-    return launch_width<S, Y, 1>(p, s);
+    return launch_width<S, Y, 1, ALONG>(p, s);
+}
+template <typename S, typename Y, int N>
+cudaError_t launch_typed(RmsBwdArgs &p, const Matrix (&m)[N], cudaStream_t s) {
+    return p.along ? launch_vectors<S, Y, true>(p, m, s) : launch_vectors<S, Y, false>(p, m, s);
 }
 
 }  // namespace

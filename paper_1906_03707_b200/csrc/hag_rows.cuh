@@ -179,4 +179,107 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
+// Sums of R values per lane over the L lanes of a group: lanes trade halves of the list while it has more than one
+// value (4 sums over 32 lanes take 6 shuffles, not 20), and each lane ends with ONE of the sums: number (gl * R / L).
+// What follows a sum (a division, a root) is then done once, not once per value.
+template <int L, int R>
+__device__ __forceinline__ float spread_sums(const float (&in)[R], int gl) {
+    float v[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) v[i] = in[i];
+    int o = L / 2;
+#pragma unroll
+    for (int h = R / 2; h >= 1; h /= 2, o /= 2) {
+        const bool upper = gl & o;
+#pragma unroll
+        for (int i = 0; i < h; ++i) {
+            const float keep = upper ? v[i + h] : v[i], give = upper ? v[i] : v[i + h];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+    }
+#pragma unroll
+    for (; o > 0; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    return v[0];
+}
+// Value number i of a list spread that way, in every lane of the group.
+template <int L, int R>
+__device__ __forceinline__ float spread_get(float v, int i, int lane) {
+    return __shfl_sync(0xffffffffu, v, (lane & ~(L - 1)) + i * (L / R));
+}
+
+// Two fp32 operations per instruction; N is even or 1.
+template <int N>
+struct Pairs {
+    float v[N];
+    template <typename F2, typename F1>
+    static __device__ __forceinline__ void each(F2 f2, F1 f1) {
+#pragma unroll
+        for (int j = 0; j + 1 < N; j += 2) f2(j);
+        if constexpr (N % 2) f1(N - 1);
+    }
+    __device__ __forceinline__ float2 two(int j) const { return make_float2(v[j], v[j + 1]); }
+    __device__ __forceinline__ void put(int j, float2 t) { v[j] = t.x; v[j + 1] = t.y; }
+    __device__ __forceinline__ void fill(float f) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = f;
+    }
+    __device__ __forceinline__ void add(const Pairs &a) {                                     // v += a
+        each([&](int j) { put(j, __fadd2_rn(two(j), a.two(j))); }, [&](int j) { v[j] += a.v[j]; });
+    }
+    __device__ __forceinline__ void fma(const Pairs &a, const Pairs &b) {                     // v += a * b
+        each([&](int j) { put(j, __ffma2_rn(a.two(j), b.two(j), two(j))); }, [&](int j) { v[j] = fmaf(a.v[j], b.v[j], v[j]); });
+    }
+    __device__ __forceinline__ void mul(const Pairs &a) {
+        each([&](int j) { put(j, __fmul2_rn(two(j), a.two(j))); }, [&](int j) { v[j] *= a.v[j]; });
+    }
+    __device__ __forceinline__ void shift_scale(float s, float m) {                           // v = (v + s) * m
+        each([&](int j) { put(j, __fmul2_rn(__fadd2_rn(two(j), make_float2(s, s)), make_float2(m, m))); },
+             [&](int j) { v[j] = (v[j] + s) * m; });
+    }
+    __device__ __forceinline__ void mul_all(float m) {
+        each([&](int j) { put(j, __fmul2_rn(two(j), make_float2(m, m))); }, [&](int j) { v[j] *= m; });
+    }
+    __device__ __forceinline__ void shift(float s) {                                          // v += s
+        each([&](int j) { put(j, __fadd2_rn(two(j), make_float2(s, s))); }, [&](int j) { v[j] += s; });
+    }
+    __device__ __forceinline__ void affine(float m, float s) {                                // v = v * m + s
+        each([&](int j) { put(j, __ffma2_rn(two(j), make_float2(m, m), make_float2(s, s))); }, [&](int j) { v[j] = fmaf(v[j], m, s); });
+    }
+    __device__ __forceinline__ void affine(float m, const Pairs &s) {                         // v = v * m + s
+        each([&](int j) { put(j, __ffma2_rn(two(j), make_float2(m, m), s.two(j))); }, [&](int j) { v[j] = fmaf(v[j], m, s.v[j]); });
+    }
+    __device__ __forceinline__ void add_scaled(const Pairs &a, float m) {                     // v += a * m
+        each([&](int j) { put(j, __ffma2_rn(a.two(j), make_float2(m, m), two(j))); }, [&](int j) { v[j] = fmaf(a.v[j], m, v[j]); });
+    }
+    __device__ __forceinline__ float sum() const {
+        float2 s = make_float2(v[0], N > 1 ? v[N > 1] : 0.0f);
+#pragma unroll
+        for (int j = 2; j + 1 < N; j += 2) s = __fadd2_rn(s, two(j));
+        return s.x + s.y;
+    }
+    __device__ __forceinline__ float dot(const Pairs &a) const {
+        if constexpr (N == 1) return v[0] * a.v[0];
+        float2 s = __fmul2_rn(two(0), a.two(0));
+#pragma unroll
+        for (int j = 2; j + 1 < N; j += 2) s = __ffma2_rn(two(j), a.two(j), s);
+        return s.x + s.y;
+    }
+};
+
+template <typename T, int V>
+__device__ __forceinline__ Pairs<V> widen(const Vec<T, V> &a) {
+    Pairs<V> f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) f.v[j] = a.get(j);
+    return f;
+}
+
+// Waits until the oldest of the stages has arrived (a launch has fewer stages where a row fills the shared memory).
+__device__ __forceinline__ void wait_oldest(int stages) {
+    if (stages == 4) wait_copies<3>();
+    else if (stages == 3) wait_copies<2>();
+    else if (stages == 2) wait_copies<1>();
+    else wait_copies<0>();
+}
+
 }  // namespace hagr
