@@ -79,8 +79,8 @@ __device__ __forceinline__ float lanes_largest(float v, int lanes) {
 }
 template <int L>
 __device__ __forceinline__ float group_largest(float v, float *slot) {
-    v = lanes_largest(v, L ? L : 32);
-    if constexpr (L == 0) {
+    v = lanes_largest(v, L > 0 ? L : 32);
+    if constexpr (L <= 0) {
         if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
         __syncthreads();
         v = lanes_largest((threadIdx.x & 31) < (blockDim.x >> 5) ? slot[threadIdx.x & 31] : 0.0f, 32);
@@ -94,40 +94,36 @@ __device__ __forceinline__ float scale_of(float largest, const RmsArgs &p) {
 }
 
 // Scales and codes of K vectors of a thread: `y` are the values.  A scale's columns lie within a warp: they are block / V
-// lanes of one vector, or, for V = 1, block / 32 vectors of all lanes.
+// lanes of one vector, or, for V = 1, T = block / 32 vectors of all lanes.
+template <int T, int V, int K, typename At>
+__device__ __forceinline__ void quant_groups(hagr::Pairs<V> (&y)[K], const RmsArgs &p, int64_t r, const At &at, int n_vec, bool live, int lanes) {
+    char *q = static_cast<char *>(p.y) + r * p.ld_y;
+#pragma unroll
+    for (int k0 = 0; k0 < K; k0 += T) {
+        float top = 0.0f;
+#pragma unroll
+        for (int k = k0; k < k0 + T && k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) top = larger(top, y[k].v[j]);
+        const float scale = scale_of(lanes_largest(top, lanes), p), inverse = __fdividef(1.0f, scale);
+        if (!live) continue;
+#pragma unroll
+        for (int k = k0; k < k0 + T && k < K; ++k) {
+            y[k].mul_all(inverse);
+            if (at.mine(k, n_vec)) store_codes<V>(y[k].v, q, at.vec(k), p.int8);
+        }
+        const int c = at.vec(k0) * V;
+        if (c % p.block == 0 && at.mine(k0, n_vec)) p.scales[r * p.n_scales + c / p.block] = scale;
+    }
+}
 template <int V, int K, typename At>
 __device__ __forceinline__ void quant_blocks(hagr::Pairs<V> (&y)[K], const RmsArgs &p, int64_t r, const At &at, int n_vec, bool live) {
-    char *q = static_cast<char *>(p.y) + r * p.ld_y;
-    const int lanes = V == 1 ? 32 : p.block / V, together = V == 1 ? p.block / 32 : 1;
-    float top[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        top[k] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) top[k] = larger(top[k], y[k].v[j]);
-        top[k] = lanes_largest(top[k], lanes);
-    }
-    if constexpr (V == 1 && K > 1) {
-#pragma unroll
-        for (int k = 0; k + 1 < K; k += 2)
-            if (together > 1) top[k] = top[k + 1] = larger(top[k], top[k + 1]);
-#pragma unroll
-        for (int k = 0; k + 2 < K; k += 4)
-            if (together > 2) {
-                top[k] = top[k + 1] = larger(top[k], top[k + 2]);
-                top[k + 2] = top[k];
-                if (k + 3 < K) top[k + 3] = top[k];
-            }
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int vec = at.vec(k);
-        const float scale = scale_of(top[k], p);
-        y[k].mul_all(__fdividef(1.0f, scale));
-        if (!live || vec >= n_vec) continue;
-        store_codes<V>(y[k].v, q, vec, p.int8);
-        const int c = vec * V;
-        if (c % p.block == 0) p.scales[r * p.n_scales + c / p.block] = scale;
+    if constexpr (V > 1) {
+        quant_groups<1, V, K>(y, p, r, at, n_vec, live, p.block / V);
+    } else {
+        if (p.block == 128) quant_groups<4, V, K>(y, p, r, at, n_vec, live, 32);
+        else if (p.block == 64) quant_groups<2, V, K>(y, p, r, at, n_vec, live, 32);
+        else quant_groups<1, V, K>(y, p, r, at, n_vec, live, 32);
     }
 }
 
@@ -138,11 +134,11 @@ template <typename X, typename S, int V> constexpr bool kRing = V * int(sizeof(X
 constexpr int kTurnBytes = 32;
 template <typename X, typename S, int V, int K, bool RES> constexpr int kRowBytes = K * V * int(sizeof(X) + (RES ? sizeof(S) : 0));     // per lane
 template <typename X, typename S, int V, int L, int K, bool RES> constexpr int kTurnRows =
-    L == 0 ? 1 : kRing<X, S, V> ? (kRowBytes<X, S, V, K, RES> >= kTurnBytes ? 1 : kTurnBytes / kRowBytes<X, S, V, K, RES>)
+    L <= 0 ? 1 : kRing<X, S, V> ? (kRowBytes<X, S, V, K, RES> >= kTurnBytes ? 1 : kTurnBytes / kRowBytes<X, S, V, K, RES>)
                                 : V * K >= 16 ? 1 : 16 / (V * K) < 4 ? 16 / (V * K) : 4;
 
 template <typename X, typename S, typename Y, int V, int L, int K, bool QUANT, bool RES>
-__global__ void __launch_bounds__(L ? kWarpRowThreads : kRowThreads, L ? 2 : 1) rms_fwd_kernel(const __grid_constant__ RmsArgs p) {
+__global__ void __launch_bounds__(kThreadsOf<L>, L > 0 ? 2 : 1) rms_fwd_kernel(const __grid_constant__ RmsArgs p) {
     hagk::pdl_launch_dependents();
     constexpr int R = kTurnRows<X, S, V, L, K, RES>;
     constexpr bool RING = kRing<X, S, V>;
@@ -174,10 +170,8 @@ __global__ void __launch_bounds__(L ? kWarpRowThreads : kRowThreads, L ? 2 : 1) 
     if constexpr (RING) {
         for (int s = 0; s < p.stages; ++s) issue();
     }
-    hagr::Pairs<V> w[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) w[k].fill(0.0f);
-    load_all_weights<V, K>(w, p.w, p.w_bf16, p.w_vectors, at, n_vec);
+    hagr::Pairs<V> w[kKeepWeights<L> ? K : 1];
+    if constexpr (kKeepWeights<L>) load_all_weights<V, K>(w, p.w, p.w_bf16, p.w_vectors, at, n_vec);
     int turn = 0;
     for (int64_t lead = at.leader() * R, r0 = at.group * R; lead < p.n; lead += at.groups * R, r0 += at.groups * R, turn ^= 1) {
         hagr::Pairs<V> h[R][K];
@@ -248,9 +242,19 @@ __global__ void __launch_bounds__(L ? kWarpRowThreads : kRowThreads, L ? 2 : 1) 
                 }
             }
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                h[i][k].mul_all(rstd);
-                h[i][k].mul(w[k]);
+            for (int k = 0; k < K; ++k) h[i][k].mul_all(rstd);
+            if constexpr (kKeepWeights<L>) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) h[i][k].mul(w[k]);
+            } else {
+                constexpr int U = V > 1 ? 1 : 4;
+#pragma unroll
+                for (int k = 0; k < K; k += U) {
+                    hagr::Pairs<V> some[U];
+                    load_all_weights<V, U>(some, p.w, p.w_bf16, p.w_vectors, From<P>{at, k}, n_vec);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) h[i][k + u].mul(some[u]);
+                }
             }
             char *const to = static_cast<char *>(p.y) + r * p.ld_y * int64_t(sizeof(Y));
             if constexpr (!QUANT) {
@@ -323,8 +327,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) rms_fwd_long_kernel(const __gr
         };
         auto scaled = [&](const Walk &at, float rstd, hagr::Pairs<V> (&h)[K]) {
             hagr::Pairs<V> w[K];
-#pragma unroll
-            for (int k = 0; k < K; ++k) w[k].fill(0.0f);
             load_all_weights<V, K>(w, p.w, p.w_bf16, p.w_vectors, at, n_vec);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -399,19 +401,19 @@ constexpr int kShortThreads = 512, kLongThreads = 1536;
 template <typename X, typename S, typename Y, int V, int L, int K, bool QUANT, bool RES>
 cudaError_t launch_rows(RmsArgs &p, int warps, cudaStream_t s) {
     constexpr auto kernel = rms_fwd_kernel<X, S, Y, V, L, K, QUANT, RES>;
-    constexpr int R = kTurnRows<X, S, V, L, K, RES>, kGroup = L ? L : 32;
-    const unsigned threads = L ? kWarpRowThreads : unsigned(warps) * 32;
+    constexpr int R = kTurnRows<X, S, V, L, K, RES>, kGroup = L > 0 ? L : 32;
+    const unsigned threads = L > 0 ? kWarpRowThreads : unsigned(warps) * 32;
     const cudaError_t err = allow_shared<kernel>();
     if (err != cudaSuccess) return err;
-    const int64_t rows = L ? int64_t(kWarpRowThreads / kGroup) * R : 1;
+    const int64_t rows = L > 0 ? int64_t(kWarpRowThreads / kGroup) * R : 1;
     size_t shared = 0;
     int most = kSms;
     if constexpr (kRing<X, S, V>) {
         constexpr int kLane = R * kRowBytes<X, S, V, K, RES>;
-        constexpr bool kShort = kLane <= kTurnBytes || (L == 0 && QUANT);
-        p.stages = kShort ? 2 : 1;
+        constexpr bool kShort = kLane <= kTurnBytes || (L <= 0 && QUANT);
+        p.stages = kShort && size_t(kLane) * threads * 2 <= size_t(kMostShared) ? 2 : 1;
         shared = size_t(kLane) * threads * p.stages;
-        most = std::max(2, (kShort ? kShortThreads : kLongThreads) / int(threads));
+        most = std::max(L < 0 ? 1 : 2, (kShort ? kShortThreads : kLongThreads) / int(threads));
     }
     most = std::min(most, blocks_per_sm<kernel>(threads, shared));
     const int64_t grid = std::min<int64_t>((p.n + rows - 1) / rows, int64_t(kSms) * most);
@@ -432,13 +434,25 @@ cudaError_t launch_width(RmsArgs &p, cudaStream_t s) {
         if (n_vec == 2) return launch_rows<X, S, Y, V, 2, 1, QUANT, RES>(p, 1, s);
     }
     if (n_vec <= 4) return launch_rows<X, S, Y, V, 4, 1, QUANT, RES>(p, 1, s);
-    if (n_vec <= 8) return launch_rows<X, S, Y, V, 8, 1, QUANT, RES>(p, 1, s);
-    if (n_vec <= 16) return launch_rows<X, S, Y, V, 16, 1, QUANT, RES>(p, 1, s);
-    if (chunks == 1) return launch_rows<X, S, Y, V, 32, 1, QUANT, RES>(p, 1, s);
-    if (chunks == 2) return launch_rows<X, S, Y, V, 32, 2, QUANT, RES>(p, 1, s);
-    if (chunks <= 4) return launch_rows<X, S, Y, V, 32, 4, QUANT, RES>(p, 1, s);
     if constexpr (V > 1) {
-        return launch_rows<X, S, Y, V, 0, kPerThread / V, QUANT, RES>(p, (chunks * V + kPerThread - 1) / kPerThread, s);
+        if (n_vec <= 8) return launch_rows<X, S, Y, V, 8, 1, QUANT, RES>(p, 1, s);
+        if (n_vec <= 16) return launch_rows<X, S, Y, V, 16, 1, QUANT, RES>(p, 1, s);
+        if (chunks == 1) return launch_rows<X, S, Y, V, 32, 1, QUANT, RES>(p, 1, s);
+    } else {
+        if (n_vec <= 8) return launch_rows<X, S, Y, V, 4, 2, QUANT, RES>(p, 1, s);
+        if (n_vec <= 16) return launch_rows<X, S, Y, V, 8, 2, QUANT, RES>(p, 1, s);
+        if (n_vec <= 32) return launch_rows<X, S, Y, V, 8, 4, QUANT, RES>(p, 1, s);
+        if constexpr (!QUANT)              // 32 columns of a scale lie in one vector of a warp
+            if (n_vec <= 64) return launch_rows<X, S, Y, V, 16, 4, QUANT, RES>(p, 1, s);
+    }
+    if constexpr (V > 1 || QUANT)
+        if (chunks == 2) return launch_rows<X, S, Y, V, 32, 2, QUANT, RES>(p, 1, s);
+    if (chunks <= 4) return launch_rows<X, S, Y, V, 32, 4, QUANT, RES>(p, 1, s);
+    const bool wide = p.D > kRowThreads * kPerThread;
+    if constexpr (V > 1) {
+        const int warps = (chunks * V + kPerThread - 1) / kPerThread;
+        if (wide) return launch_rows<X, S, Y, V, -1, kPerThread / V, QUANT, RES>(p, warps, s);
+        return launch_rows<X, S, Y, V, 0, kPerThread / V, QUANT, RES>(p, warps, s);
     } else {
         if (chunks <= 6) return launch_rows<X, S, Y, V, 32, 6, QUANT, RES>(p, 1, s);
         if (chunks <= 8) return launch_rows<X, S, Y, V, 32, 8, QUANT, RES>(p, 1, s);
@@ -448,6 +462,15 @@ cudaError_t launch_width(RmsArgs &p, cudaStream_t s) {
         if (chunks <= 16) return launch_rows<X, S, Y, V, 32, 16, QUANT, RES>(p, 1, s);
         const int each = QUANT ? 4 : 2, units = (chunks + each - 1) / each;             // chunks that stay together
         const int warps = (units * each + kPerThread - 1) / kPerThread, k = (units + warps - 1) / warps * each;
+        if (wide) {                        // as many warps as a block may have: their columns' loads are all that hides latency
+            const int most = kWideThreads / 32, few = (units + most - 1) / most, many = (units + few - 1) / few;
+            if constexpr (!QUANT) {
+                if (few * each <= 10) return launch_rows<X, S, Y, V, -1, 10, QUANT, RES>(p, many, s);
+                if (few * each == 14) return launch_rows<X, S, Y, V, -1, 14, QUANT, RES>(p, many, s);
+            }
+            if (few * each <= 12) return launch_rows<X, S, Y, V, -1, 12, QUANT, RES>(p, many, s);
+            return launch_rows<X, S, Y, V, -1, 16, QUANT, RES>(p, many, s);
+        }
         if constexpr (!QUANT) {
             if (k <= 10) return launch_rows<X, S, Y, V, 0, 10, QUANT, RES>(p, warps, s);
             if (k == 14) return launch_rows<X, S, Y, V, 0, 14, QUANT, RES>(p, warps, s);

@@ -17,8 +17,9 @@ namespace hagn {
 constexpr int kSms = 148;
 constexpr int kWarpRowThreads = 256;      // of a block whose warps take rows of their own
 constexpr int kRowThreads = 512;          // at most, of a block that takes a row
-constexpr int kPerThread = 16;            // columns of a row per thread of such a block
-constexpr int kMostInRegisters = kRowThreads * kPerThread;     // columns
+constexpr int kWideThreads = 1024;        // of one that takes a row of more than 8192 columns
+constexpr int kPerThread = 16;            // columns of a row per thread of such blocks
+constexpr int kMostInRegisters = kWideThreads * kPerThread;        // columns
 
 // A vector of V elements, by one access of up to 32 bytes.
 template <typename T, int V>
@@ -64,7 +65,7 @@ __device__ __forceinline__ void store_weight(void *p, int bf16, int64_t i, float
         static_cast<float *>(p)[i] = f;
     }
 }
-// The weights of a thread's K vectors; `vectors`: whether they can be read as such.  Without weights they are ones.  One
+// The weights of a thread's K vectors, zeros beyond the row; `vectors`: whether they can be read as such.  Without weights they are ones.  One
 // test of the type for all of them: loads behind a test of their own would wait for one another.
 template <int V, int K, typename At>
 __device__ __forceinline__ void load_all_weights(hagr::Pairs<V> (&w)[K], const void *p, int bf16, bool vectors, const At &at, int n_vec) {
@@ -72,6 +73,8 @@ __device__ __forceinline__ void load_all_weights(hagr::Pairs<V> (&w)[K], const v
         using T = decltype(type);
         constexpr int N = decltype(width)::value;
         hagr::Vec<T, N> q[K][V / N];
+#pragma unroll
+        for (int k = 0; k < K; ++k) w[k].fill(0.0f);
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
@@ -85,8 +88,7 @@ __device__ __forceinline__ void load_all_weights(hagr::Pairs<V> (&w)[K], const v
     };
     if (!p) {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (at.mine(k, n_vec)) w[k].fill(1.0f);
+        for (int k = 0; k < K; ++k) w[k].fill(at.mine(k, n_vec) ? 1.0f : 0.0f);
     } else if (vectors) {
         if (bf16) load(__nv_bfloat16(), std::integral_constant<int, V>());
         else load(float(), std::integral_constant<int, V>());
@@ -96,13 +98,24 @@ __device__ __forceinline__ void load_all_weights(hagr::Pairs<V> (&w)[K], const v
     }
 }
 
-// Sums over the L lanes that share a row, or (L = 0) over the block; every thread receives the sum.  `slot`: of the block's
+// Vectors k0, k0 + 1, ... of a thread, for kernels that read the weights of a few at a time, row by row.
+template <typename At>
+struct From {
+    const At &at;
+    int k0;
+    __device__ __forceinline__ int vec(int k) const { return at.vec(k0 + k); }
+    __device__ __forceinline__ bool mine(int k, int n_vec) const { return at.mine(k0 + k, n_vec); }
+};
+template <int L> constexpr bool kKeepWeights = L >= 0;         // blocks of many threads have no registers for them
+template <int L> constexpr int kThreadsOf = L > 0 ? kWarpRowThreads : L == 0 ? kRowThreads : kWideThreads;
+
+// Sums over the L lanes that share a row, or (L <= 0) over the block; every thread receives the sum.  `slot`: of the block's
 // sums, another one than that of the sum before, so that one barrier is enough.
 template <int L>
 __device__ __forceinline__ float group_sum(float v, float *slot) {
 #pragma unroll
-    for (int o = (L ? L : 32) / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if constexpr (L == 0) {
+    for (int o = (L > 0 ? L : 32) / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (L <= 0) {
         if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
         __syncthreads();
         v = hagr::warp_sum((threadIdx.x & 31) < (blockDim.x >> 5) ? slot[threadIdx.x & 31] : 0.0f);
@@ -111,19 +124,19 @@ __device__ __forceinline__ float group_sum(float v, float *slot) {
 }
 
 // The place of a thread in its row, and of its row among the others.
-//   L > 0: L lanes of a warp per row, 32 / L rows per warp; L = 0: a block per row.
+//   L > 0: L lanes of a warp per row, 32 / L rows per warp; L = 0: a block per row; L = -1: a block of up to kWideThreads.
 // A thread has K vectors of the row.  Neighbouring lanes have neighbouring vectors, 32 (or L) of them are a chunk, and the
 // warps of a block take chunks in turn; GROUPED: four chunks in turn, so that 128 columns of V = 1 lie in one warp.  Of the
 // widths that a kernel is launched with, all chunks but the last kPartial of a thread lie within the row.
 template <int L, int K, bool GROUPED>
 struct Place {
-    static constexpr int kLanes = L ? L : 32;
+    static constexpr int kLanes = L > 0 ? L : 32;
     static constexpr bool kWarpRows = L > 0;
-    static constexpr int kPartial = GROUPED && L == 0 ? 4 : K >= 4 ? 2 : 1;
+    static constexpr int kPartial = GROUPED && L <= 0 ? 4 : K >= 4 ? 2 : 1;
     int lane, warp, warps;                     // lane of the group that shares a row; warp of the row's
     int64_t group, groups;                     // of this thread, and of the launch
     __device__ __forceinline__ Place() {
-        if constexpr (L) {
+        if constexpr (kWarpRows) {
             constexpr int G = 32 / kLanes;
             lane = threadIdx.x % kLanes;
             warp = 0;
@@ -139,7 +152,7 @@ struct Place {
         }
     }
     __device__ __forceinline__ int chunk(int k) const {        // first vector of chunk k
-        if constexpr (L) return k * kLanes;
+        if constexpr (kWarpRows) return k * kLanes;
         else if constexpr (GROUPED) return ((k / 4 * warps + warp) * 4 + k % 4) * 32;
         else return (k * warps + warp) * 32;
     }
@@ -147,7 +160,7 @@ struct Place {
     __device__ __forceinline__ bool mine(int k, int n_vec) const { return k < K - kPartial || vec(k) < n_vec; }
     __device__ __forceinline__ bool first() const { return lane == 0 && warp == 0; }
     // the group whose rows decide how many turns the warp takes
-    __device__ __forceinline__ int64_t leader() const { return L ? group - (threadIdx.x & 31) / kLanes : group; }
+    __device__ __forceinline__ int64_t leader() const { return kWarpRows ? group - (threadIdx.x & 31) / kLanes : group; }
 };
 
 // Sums of R values over the lanes (or the block) that share a row; get(i) is the i-th in every lane, after f was applied to
@@ -221,7 +234,8 @@ cudaError_t launch(void (*kernel)(Args), dim3 grid, unsigned threads, size_t sha
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-constexpr int kSmShared = 227 * 1024;      // shared memory that the blocks of an SM can use, and one block
+constexpr int kSmShared = 227 * 1024;      // shared memory that the blocks of an SM can use
+constexpr int kMostShared = kSmShared - 2048;      // and the dynamic part of one block's
 // Lets a kernel use the shared memory of the current device's SMs (once per kernel and device).
 template <auto KERNEL>
 cudaError_t allow_shared() {
@@ -230,7 +244,7 @@ cudaError_t allow_shared() {
     cudaError_t err = cudaGetDevice(&device);
     const uint64_t bit = uint64_t(1) << (device & 63);
     if (err != cudaSuccess || (ready.load(std::memory_order_relaxed) & bit)) return err;
-    err = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmShared - 2048);
+    err = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     if (err == cudaSuccess) ready.fetch_or(bit, std::memory_order_relaxed);
     return err;
 }

@@ -1,8 +1,7 @@
 // The gradient of the root-mean-square norm with the residual's addition.  With hh = h * rstd and q = g * w:
 //   grad = rstd * (q - hh * mean(q * hh)) + what arrives along the residual stream,  gw = sum over rows of g * hh
 // A row is read once and its gradient written once; gw stays with the threads over all their rows, is joined per block
-// and then over the blocks, in a fixed order.  Rows of more columns than a block's registers hold are read twice, the
-// second time out of the caches, and gw is kept in shared memory.
+// and then over the blocks, in a fixed order.
 #include "hag_rms.cuh"
 
 namespace {
@@ -54,10 +53,10 @@ template <typename Y, int V> constexpr bool kRing = V * int(sizeof(Y)) >= 16;
 constexpr int kTurnBytes = 96;
 template <typename S, typename Y, int V, int K, bool ALONG> constexpr int kRowBytes = K * V * int(sizeof(Y) + (ALONG ? 2 : 1) * sizeof(S));    // per lane
 template <typename S, typename Y, int V, int L, int K, bool ALONG> constexpr int kTurnRows =
-    L == 0 ? 1 : kRing<Y, V> ? (kRowBytes<S, Y, V, K, ALONG> * 2 <= kTurnBytes && L > 2 ? 2 : 1) : V * K <= 4 ? 4 : V * K <= 8 ? 2 : 1;
+    L <= 0 ? 1 : kRing<Y, V> ? (kRowBytes<S, Y, V, K, ALONG> * 2 <= kTurnBytes && L > 2 ? 2 : 1) : V * K <= 8 ? 2 : 1;
 
 template <typename S, typename Y, int V, int L, int K, bool ALONG>
-__global__ void __launch_bounds__(L ? kWarpRowThreads : kRowThreads, L ? 2 : 1) rms_bwd_kernel(const __grid_constant__ RmsBwdArgs p) {
+__global__ void __launch_bounds__(kThreadsOf<L>, L > 0 ? 2 : 1) rms_bwd_kernel(const __grid_constant__ RmsBwdArgs p) {
     hagk::pdl_launch_dependents();
     constexpr int R = kTurnRows<S, Y, V, L, K, ALONG>;
     constexpr bool RING = kRing<Y, V>;
@@ -97,16 +96,20 @@ __global__ void __launch_bounds__(L ? kWarpRowThreads : kRowThreads, L ? 2 : 1) 
         for (int s = 0; s < p.stages; ++s) issue();
     }
     statistics(at.group * R);
-    Values w[K], sum[K];
+    // Blocks of many threads keep the sums of gw in registers and read everything else twice, out of the ring (or the
+    // caches); the ring's stage is given back at the end of the row.
+    constexpr bool kHold = kKeepWeights<L>;
+    Values w[kHold ? K : 1], sum[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        w[k].fill(0.0f);
-        sum[k].fill(0.0f);
-    }
-    load_all_weights<V, K>(w, p.w, p.w_bf16, p.w_vectors, at, n_vec);
+    for (int k = 0; k < K; ++k) sum[k].fill(0.0f);
+    if constexpr (kHold) load_all_weights<V, K>(w, p.w, p.w_bf16, p.w_vectors, at, n_vec);
+    auto give_back = [&]() {
+        if (CY::kCrosses || CS::kCrosses) __syncwarp();
+        issue();
+        read = read + stage == end ? 0 : read + stage;
+    };
     int turn = 0;
     for (int64_t lead = at.leader() * R, r0 = at.group * R; lead < p.n; lead += at.groups * R, r0 += at.groups * R, turn ^= 1) {
-        Values hh[R][K], q[R][K], a[R][K];
         float rstd[R], s[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) rstd[i] = rstd_next[i];
@@ -114,82 +117,152 @@ __global__ void __launch_bounds__(L ? kWarpRowThreads : kRowThreads, L ? 2 : 1) 
         if constexpr (RING) {
             hagr::wait_oldest(p.stages);
             if (CY::kCrosses || CS::kCrosses) __syncwarp();
+        }
+        if constexpr (kHold) {
+            Values hh[R][K], q[R][K], a[R][K];
+            if constexpr (RING) {
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const char *from = raw + read + i * row_bytes;
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    q[i][k] = CY::get(from, at, k);
-                    hh[i][k] = CS::get(from + CY::bytes(), at, k);
-                    if (ALONG) a[i][k] = CS::get(from + CY::bytes() + CS::bytes(), at, k);
-                    else a[i][k].fill(0.0f);
-                }
-            }
-            if (CY::kCrosses || CS::kCrosses) __syncwarp();
-            issue();
-            read = read + stage == end ? 0 : read + stage;
-        } else {
-            hagr::Vec<Y, V> g[R][K];
-            hagr::Vec<S, V> t[R][K], b[R][K];
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const bool live = r0 + i < p.n;
-                const char *gr = static_cast<const char *>(p.g) + (r0 + i) * ld_g, *tr = static_cast<const char *>(p.total) + (r0 + i) * ld_total;
-                const char *br = static_cast<const char *>(p.along) + (r0 + i) * ld_along;
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    g[i][k].zero();
-                    t[i][k].zero();
-                    if (live && at.mine(k, n_vec)) {
-                        g[i][k].template load<hagr::kKeep>(gr, at.vec(k));
-                        t[i][k].template load<hagr::kKeep>(tr, at.vec(k));
-                    }
-                }
-                if (ALONG) {
+                for (int i = 0; i < R; ++i) {
+                    const char *from = raw + read + i * row_bytes;
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
-                        b[i][k].zero();
-                        if (live && at.mine(k, n_vec)) b[i][k].template load<hagr::kKeep>(br, at.vec(k));
+                        q[i][k] = CY::get(from, at, k);
+                        hh[i][k] = CS::get(from + CY::bytes(), at, k);
+                        if (ALONG) a[i][k] = CS::get(from + CY::bytes() + CS::bytes(), at, k);
+                        else a[i][k].fill(0.0f);
                     }
                 }
+                give_back();
+            } else {
+                hagr::Vec<Y, V> g[R][K];
+                hagr::Vec<S, V> t[R][K], b[R][K];
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    const bool live = r0 + i < p.n;
+                    const char *gr = static_cast<const char *>(p.g) + (r0 + i) * ld_g, *tr = static_cast<const char *>(p.total) + (r0 + i) * ld_total;
+                    const char *br = static_cast<const char *>(p.along) + (r0 + i) * ld_along;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        g[i][k].zero();
+                        t[i][k].zero();
+                        if (live && at.mine(k, n_vec)) {
+                            g[i][k].template load<hagr::kKeep>(gr, at.vec(k));
+                            t[i][k].template load<hagr::kKeep>(tr, at.vec(k));
+                        }
+                    }
+                    if (ALONG) {
+#pragma unroll
+                        for (int k = 0; k < K; ++k) {
+                            b[i][k].zero();
+                            if (live && at.mine(k, n_vec)) b[i][k].template load<hagr::kKeep>(br, at.vec(k));
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        q[i][k] = hagr::widen(g[i][k]);
+                        hh[i][k] = hagr::widen(t[i][k]);
+                        if (ALONG) a[i][k] = hagr::widen(b[i][k]);
+                        else a[i][k].fill(0.0f);
+                    }
             }
 #pragma unroll
-            for (int i = 0; i < R; ++i)
+            for (int i = 0; i < R; ++i) {
+                s[i] = 0.0f;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    q[i][k] = hagr::widen(g[i][k]);
-                    hh[i][k] = hagr::widen(t[i][k]);
-                    if (ALONG) a[i][k] = hagr::widen(b[i][k]);
-                    else a[i][k].fill(0.0f);
+                    hh[i][k].mul_all(rstd[i]);
+                    sum[k].fma(q[i][k], hh[i][k]);
+                    q[i][k].mul(w[k]);
+                    s[i] += q[i][k].dot(hh[i][k]);
                 }
-        }
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            s[i] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                hh[i][k].mul_all(rstd[i]);
-                sum[k].fma(q[i][k], hh[i][k]);
-                q[i][k].mul(w[k]);
-                s[i] += q[i][k].dot(hh[i][k]);
             }
-        }
-        const Sums<L, R> means(s, slots[turn], [&](float v) { return -v * inverse; });
+            const Sums<L, R> means(s, slots[turn], [&](float v) { return -v * inverse; });
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const float m = means.get(i);
-            if (r0 + i >= p.n) continue;
+            for (int i = 0; i < R; ++i) {
+                const float m = means.get(i);
+                if (r0 + i >= p.n) continue;
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                hh[i][k].affine(m, q[i][k]);
-                a[i][k].add_scaled(hh[i][k], rstd[i]);
-                if (at.mine(k, n_vec)) store_gradient<S, V>(p, r0 + i, at.vec(k), a[i][k]);
+                for (int k = 0; k < K; ++k) {
+                    hh[i][k].affine(m, q[i][k]);
+                    a[i][k].add_scaled(hh[i][k], rstd[i]);
+                    if (at.mine(k, n_vec)) store_gradient<S, V>(p, r0 + i, at.vec(k), a[i][k]);
+                }
             }
+        } else {
+            static_assert(kHold || R == 1, "");
+            const char *gr = static_cast<const char *>(p.g) + r0 * ld_g, *tr = static_cast<const char *>(p.total) + r0 * ld_total;
+            const char *br = static_cast<const char *>(p.along) + r0 * ld_along, *from = raw + read;
+            constexpr int U = V >= 4 ? 1 : 4;                  // vectors at a time
+            auto pass = [&](auto f) {
+#pragma unroll
+                for (int k0 = 0; k0 < K; k0 += U) {
+                    Values g[U], hh[U], w1[U];
+                    if constexpr (RING) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            g[u] = CY::get(from, at, k0 + u);
+                            hh[u] = CS::get(from + CY::bytes(), at, k0 + u);
+                        }
+                    } else {
+                        hagr::Vec<Y, V> x[U];
+                        hagr::Vec<S, V> y[U];
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            x[u].zero();
+                            y[u].zero();
+                            if (at.mine(k0 + u, n_vec)) {
+                                x[u].template load<hagr::kKeep>(gr, at.vec(k0 + u));
+                                y[u].template load<hagr::kKeep>(tr, at.vec(k0 + u));
+                            }
+                        }
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            g[u] = hagr::widen(x[u]);
+                            hh[u] = hagr::widen(y[u]);
+                        }
+                    }
+                    load_all_weights<V, U>(w1, p.w, p.w_bf16, p.w_vectors, From<P>{at, k0}, n_vec);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        hh[u].mul_all(rstd[0]);
+                        f(k0 + u, g[u], hh[u], w1[u]);
+                    }
+                }
+            };
+            s[0] = 0.0f;
+            pass([&](int k, Values &g, const Values &hh, const Values &w1) {
+                sum[k].fma(g, hh);
+                g.mul(w1);
+                s[0] += g.dot(hh);
+            });
+            const float m = -group_sum<L>(s[0], slots[turn]) * inverse;
+            pass([&](int k, Values &g, Values &hh, const Values &w1) {
+                Values o;
+                o.fill(0.0f);
+                if (ALONG) {
+                    if constexpr (RING) {
+                        o = CS::get(from + CY::bytes() + CS::bytes(), at, k);
+                    } else {
+                        hagr::Vec<S, V> b;
+                        b.zero();
+                        if (at.mine(k, n_vec)) b.template load<hagr::kKeep>(br, at.vec(k));
+                        o = hagr::widen(b);
+                    }
+                }
+                g.mul(w1);
+                hh.affine(m, g);
+                o.add_scaled(hh, rstd[0]);
+                if (at.mine(k, n_vec)) store_gradient<S, V>(p, r0, at.vec(k), o);
+            });
+            if constexpr (RING) give_back();
         }
     }
     if constexpr (RING) hagr::wait_copies<0>();
     if (!p.partial) return;
-    if constexpr (L == 0) {
+    if constexpr (L <= 0) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
@@ -219,13 +292,12 @@ __global__ void __launch_bounds__(L ? kWarpRowThreads : kRowThreads, L ? 2 : 1) 
     }
 }
 
+// Rows of more columns: a block walks its row twice, the second time out of the caches; gw has a kernel of its own.
 template <typename S, typename Y, int V>
 __global__ void __launch_bounds__(kRowThreads, 1) rms_bwd_long_kernel(const __grid_constant__ RmsBwdArgs p) {
     hagk::pdl_launch_dependents();
     constexpr int K = V == 8 ? 1 : V == 4 ? 2 : 4;
     using Values = hagr::Pairs<V>;
-    extern __shared__ __align__(16) char raw[];               // gw where it is wanted from this kernel, in planes of a vector's elements
-    float *const sums = reinterpret_cast<float *>(raw);
     __shared__ float slots[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n_vec = p.D / V, stride = (kRowThreads / 32) * 32 * K;
@@ -237,14 +309,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) rms_bwd_long_kernel(const __gr
     auto walk = [&](auto f) {
         for (Walk at{warp * 32 * K + lane}; at.base - lane < n_vec; at.base += stride) f(at);
     };
-    if (p.partial)                                            // a thread's own columns: no barrier is needed
-        walk([&](const Walk &at) {
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (at.mine(k, n_vec)) sums[j * n_vec + at.vec(k)] = 0.0f;
-        });
     hagk::pdl_wait();
     for (int64_t r = blockIdx.x; r < p.n; r += gridDim.x) {
         const Y *gr = static_cast<const Y *>(p.g) + r * p.ld_g;
@@ -259,7 +323,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) rms_bwd_long_kernel(const __gr
             for (int k = 0; k < K; ++k) {
                 x[k].v.zero();
                 t[k].v.zero();
-                w[k].fill(0.0f);
                 if (at.mine(k, n_vec)) {
                     x[k].load(gr, at.vec(k));
                     t[k].load(tr, at.vec(k));
@@ -280,10 +343,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) rms_bwd_long_kernel(const __gr
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 g[k].mul(hh[k]);
-                if (p.partial && at.mine(k, n_vec)) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) sums[j * n_vec + at.vec(k)] += g[k].v[j];
-                }
                 s += g[k].dot(w[k]);
             }
         });
@@ -308,17 +367,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) rms_bwd_long_kernel(const __gr
         });
         __syncthreads();                                      // the slots are written again
     }
-    if (!p.partial) return;
-    walk([&](const Walk &at) {
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (at.mine(k, n_vec)) leave(p, int64_t(at.vec(k)) * V + j, sums[j * n_vec + at.vec(k)]);
-    });
 }
 
-// gw of one strip of 32 columns and one part of the rows, for rows whose gw does not fit in shared memory.
+// gw of one strip of 32 columns and one part of the rows.
 constexpr int kStripRows = 8;
 template <typename S, typename Y>
 __global__ void __launch_bounds__(32 * kStripRows) rms_weight_strips_kernel(const __grid_constant__ RmsBwdArgs p) {
@@ -361,7 +412,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) rms_weight_join_kernel(const 
     if (lane == 0 && k < p.D) store_weight(p.gw, p.w_bf16, k, s);
 }
 
-constexpr int kMostInShared = 48 * 1024;                      // columns
 constexpr int kParts = 64;                                    // of the strips
 // Parts of gw, i.e. blocks of the other kernels, at most: the wider the rows, the fewer blocks fit an SM.
 int most_parts(int32_t D) { return kSms * std::max(1, std::min(8, 16384 / D)); }
@@ -371,20 +421,21 @@ constexpr int64_t kFewValues = 16384;
 template <typename S, typename Y, int V, int L, int K, bool ALONG>
 cudaError_t launch_rows(RmsBwdArgs &p, int warps, cudaStream_t s) {
     constexpr auto kernel = rms_bwd_kernel<S, Y, V, L, K, ALONG>;
-    constexpr int R = kTurnRows<S, Y, V, L, K, ALONG>, kGroup = L ? L : 32;
-    const unsigned threads = L ? kWarpRowThreads : unsigned(warps) * 32;
+    constexpr int R = kTurnRows<S, Y, V, L, K, ALONG>, kGroup = L > 0 ? L : 32;
+    const unsigned threads = L > 0 ? kWarpRowThreads : unsigned(warps) * 32;
     const cudaError_t err = allow_shared<kernel>();
     if (err != cudaSuccess) return err;
-    size_t shared = size_t(threads / 32) * L * K * V * 4;
+    size_t shared = L > 0 ? size_t(threads / 32) * L * K * V * 4 : 0;
     if constexpr (kRing<Y, V>) {
         constexpr int kLane = R * kRowBytes<S, Y, V, K, ALONG>;
-        p.stages = kLane <= kTurnBytes && V * sizeof(S) == 16 ? 2 : 1;
+        p.stages = (kLane <= kTurnBytes && V * sizeof(S) == 16) || L < 0 ? 2 : 1;
+        if (size_t(kLane) * threads * p.stages > size_t(kMostShared)) p.stages = 1;
         shared = std::max(shared, size_t(kLane) * threads * p.stages);
     }
     const int most = blocks_per_sm<kernel>(threads, shared);
-    const int64_t rows = L ? int64_t(kWarpRowThreads / kGroup) * R : 1;
+    const int64_t rows = L > 0 ? int64_t(kWarpRowThreads / kGroup) * R : 1;
     int64_t grid = std::min<int64_t>((p.n + rows - 1) / rows, std::min(kSms * most, most_parts(p.D)));
-    if (L && p.partial && p.n * p.D <= kFewValues) grid = 1;
+    if (L > 0 && p.partial && p.n * p.D <= kFewValues) grid = 1;
     p.parts = int32_t(grid);
     p.joined = grid == 1;
     return launch(kernel, dim3(unsigned(grid)), threads, shared, p, s);
@@ -394,35 +445,36 @@ template <typename S, typename Y, int V, bool ALONG>
 cudaError_t launch_width(RmsBwdArgs &p, cudaStream_t s) {
     const int32_t n_vec = p.D / V, chunks = (n_vec + 31) / 32;
     if (p.D > kMostInRegisters) {
-        constexpr auto kernel = rms_bwd_long_kernel<S, Y, V>;
-        const cudaError_t err = allow_shared<kernel>();
-        if (err != cudaSuccess) return err;
-        const unsigned grid = unsigned(std::min<int64_t>(p.n, kSms));
-        if (p.partial && p.D > kMostInShared) {               // first: the gradient may take the place of what they read
+        if (p.partial) {       // first: the gradient may take the place of what they read
             p.parts = int32_t(std::min<int64_t>((p.n + kStripRows - 1) / kStripRows, kParts));
-            const cudaError_t e = launch(rms_weight_strips_kernel<S, Y>, dim3(unsigned((p.D + 31) / 32), unsigned(p.parts)), 32 * kStripRows, 0, p, s);
-            if (e != cudaSuccess) return e;
-            RmsBwdArgs q = p;
-            q.partial = nullptr;
-            return launch(kernel, dim3(grid), kRowThreads, 0, q, s);
+            const cudaError_t err = launch(rms_weight_strips_kernel<S, Y>, dim3(unsigned((p.D + 31) / 32), unsigned(p.parts)), 32 * kStripRows, 0, p, s);
+            if (err != cudaSuccess) return err;
         }
-        p.parts = int32_t(grid);
-        p.joined = grid == 1;
-        return launch(kernel, dim3(grid), kRowThreads, p.partial ? size_t(p.D) * 4 : 0, p, s);
+        return launch(rms_bwd_long_kernel<S, Y, V>, dim3(unsigned(std::min<int64_t>(p.n, kSms * 2))), kRowThreads, 0, p, s);
     }
     if constexpr (V > 1) {
         if (n_vec == 1) return launch_rows<S, Y, V, 1, 1, ALONG>(p, 1, s);
         if (n_vec == 2) return launch_rows<S, Y, V, 2, 1, ALONG>(p, 1, s);
     }
     if (n_vec <= 4) return launch_rows<S, Y, V, 4, 1, ALONG>(p, 1, s);
-    if (n_vec <= 8) return launch_rows<S, Y, V, 8, 1, ALONG>(p, 1, s);
-    if (n_vec <= 16) return launch_rows<S, Y, V, 16, 1, ALONG>(p, 1, s);
-    if (chunks == 1) return launch_rows<S, Y, V, 32, 1, ALONG>(p, 1, s);
-    if (chunks == 2) return launch_rows<S, Y, V, 32, 2, ALONG>(p, 1, s);
+    if constexpr (V > 1) {
+        if (n_vec <= 8) return launch_rows<S, Y, V, 8, 1, ALONG>(p, 1, s);
+        if (n_vec <= 16) return launch_rows<S, Y, V, 16, 1, ALONG>(p, 1, s);
+        if (chunks == 1) return launch_rows<S, Y, V, 32, 1, ALONG>(p, 1, s);
+        if (chunks == 2) return launch_rows<S, Y, V, 32, 2, ALONG>(p, 1, s);
+    } else {
+        if (n_vec <= 8) return launch_rows<S, Y, V, 4, 2, ALONG>(p, 1, s);
+        if (n_vec <= 16) return launch_rows<S, Y, V, 8, 2, ALONG>(p, 1, s);
+        if (n_vec <= 32) return launch_rows<S, Y, V, 8, 4, ALONG>(p, 1, s);
+        if (n_vec <= 64) return launch_rows<S, Y, V, 16, 4, ALONG>(p, 1, s);
+    }
     if constexpr (V < 8)
         if (chunks <= 4) return launch_rows<S, Y, V, 32, 4, ALONG>(p, 1, s);
+    const bool wide = p.D > kRowThreads * kPerThread;
     if constexpr (V > 1) {
-        return launch_rows<S, Y, V, 0, kPerThread / V, ALONG>(p, (chunks * V + kPerThread - 1) / kPerThread, s);
+        const int warps = (chunks * V + kPerThread - 1) / kPerThread;
+        if (wide) return launch_rows<S, Y, V, -1, kPerThread / V, ALONG>(p, warps, s);
+        return launch_rows<S, Y, V, 0, kPerThread / V, ALONG>(p, warps, s);
     } else {
         if (chunks <= 6) return launch_rows<S, Y, V, 32, 6, ALONG>(p, 1, s);
         if (chunks <= 8) return launch_rows<S, Y, V, 32, 8, ALONG>(p, 1, s);
@@ -431,6 +483,13 @@ cudaError_t launch_width(RmsBwdArgs &p, cudaStream_t s) {
         if (chunks <= 14) return launch_rows<S, Y, V, 32, 14, ALONG>(p, 1, s);
         if (chunks <= 16) return launch_rows<S, Y, V, 32, 16, ALONG>(p, 1, s);
         const int pairs = (chunks + 1) / 2, warps = (2 * pairs + kPerThread - 1) / kPerThread, k = (pairs + warps - 1) / warps * 2;
+        if (wide) {            // as many warps as a block may have: their columns' loads are all that hides latency
+            const int most = kWideThreads / 32, few = (pairs + most - 1) / most, many = (pairs + few - 1) / few;
+            if (few <= 5) return launch_rows<S, Y, V, -1, 10, ALONG>(p, many, s);
+            if (few == 6) return launch_rows<S, Y, V, -1, 12, ALONG>(p, many, s);
+            if (few == 7) return launch_rows<S, Y, V, -1, 14, ALONG>(p, many, s);
+            return launch_rows<S, Y, V, -1, 16, ALONG>(p, many, s);
+        }
         if (k <= 10) return launch_rows<S, Y, V, 0, 10, ALONG>(p, warps, s);
         if (k <= 12) return launch_rows<S, Y, V, 0, 12, ALONG>(p, warps, s);
         if (k <= 14) return launch_rows<S, Y, V, 0, 14, ALONG>(p, warps, s);
