@@ -22,7 +22,7 @@ from __future__ import annotations
 import ctypes
 import os
 from array import array
-from operator import eq
+from operator import attrgetter, eq
 from typing import NamedTuple, Optional
 
 import numpy as np
@@ -779,7 +779,7 @@ def layer_norm_bwd(grad_out, x, mean, rstd, weight=None, out=None, param_grads=T
     return out, gw, gb
 
 
-def _tensor_list(tensors, index, what="gradients"):
+def _tensor_list(tensors, index):
     """Addresses, lengths and types of a list of contiguous device tensors."""
     import torch
     T = torch.Tensor                                            # a loop inside map costs half of one in Python
@@ -787,7 +787,7 @@ def _tensor_list(tensors, index, what="gradients"):
     for k in set(kinds):
         _code(k)
     if not all(map(T.is_contiguous, tensors)) or set(map(T.get_device, tensors)) != {index}:
-        raise ValueError(f"{what} must be contiguous tensors on cuda:{index}")
+        raise ValueError(f"gradients must be contiguous tensors on cuda:{index}")
     return list(map(T.data_ptr, tensors)), list(map(T.numel, tensors)), kinds
 
 
@@ -833,6 +833,14 @@ def _clip(grads, max_norm, out, workspace):
 
 
 # -- a residual stack and its optimiser: root-mean-square norm, AdamW -------------------------------------------------- #
+def _empty_rows(t, n, d, dtype=None):
+    """New rows of t's shape and of t's type, or another; a copy of a contiguous tensor's description is the quicker way."""
+    import torch
+    if t.is_contiguous() and (dtype is None or dtype is t.dtype):
+        return torch.empty_like(t)
+    return t.new_empty((n, d), dtype=dtype or t.dtype)
+
+
 def _rms_inputs(x, weight, residual, total_out, eps):
     """What the forward calls share: (device index, rows, columns, x's and the weight's arguments, the stream's type, its
     matrix for the sum (x where there is no residual), the sum's arguments)."""
@@ -849,7 +857,7 @@ def _rms_inputs(x, weight, residual, total_out, eps):
         return index, n, d, (x.data_ptr(), _code(dtype), ld, None, _code(dtype), 0, w, wcode, eps), x, (None, 0)
     ld_res, stream = _rows(residual, "residual", shape, index), residual.dtype
     if total_out is None:
-        total_out = residual.new_empty((n, d))
+        total_out = _empty_rows(residual, n, d)
         ld_total = d
     else:
         ld_total = _rows(total_out, "total_out", shape, index, stream)
@@ -864,7 +872,7 @@ def rms_norm_fwd(x, weight=None, residual=None, eps=1e-5, out=None, total_out=No
     import torch
     index, n, d, args, total, total_args = _rms_inputs(x, weight, residual, total_out, eps)
     if out is None:
-        out = x.new_empty((n, d), dtype=dtype or x.dtype)
+        out = _empty_rows(x, n, d, dtype)
         ld_out = d
     else:
         ld_out = _rows(out, "out", (n, d), index, dtype)
@@ -929,7 +937,7 @@ def rms_norm_bwd(grad_out, total, rstd, weight=None, grad_total=None, out=None, 
     wdt = weight.dtype if weight is not None else param_dtype or torch.float32
     r = _vector(rstd, "rstd", n, index, torch.float32)
     if out is None:
-        out = total.new_empty((n, d))
+        out = _empty_rows(total, n, d)
         ld_out = d
     else:
         ld_out = _rows(out, "out", shape, index, stream)
@@ -978,6 +986,31 @@ def _one_value(t, what, index, dtype):
     return t.data_ptr()
 
 
+_dtype_of = attrgetter("dtype")
+
+
+def _addresses(tensors, index, what):
+    """Addresses, lengths and type codes of a list of contiguous device tensors; AttributeError where an entry is None."""
+    import torch
+    T = torch.Tensor
+    if not _codes:
+        _runtime()
+    kinds = list(map(_dtype_of, tensors))
+    try:
+        codes = list(map(_codes.__getitem__, kinds))
+    except KeyError as e:
+        raise TypeError(f"{what} must be float32 or bfloat16, got {e.args[0]}") from None
+    if not all(map(T.is_contiguous, tensors)) or set(map(T.get_device, tensors)) != {index}:
+        raise ValueError(f"{what} must be contiguous tensors on cuda:{index}")
+    return list(map(T.data_ptr, tensors)), list(map(T.numel, tensors)), codes
+
+
+def _written_twice(params, copies, grads):
+    """The same without tensors that hold nothing, whose addresses say nothing."""
+    written = [t.data_ptr() for t in (*params, *(copies or ())) if t is not None and t.numel()]
+    return len(set(written)) != len(written) or not set(written).isdisjoint([g.data_ptr() for g in grads if g is not None and g.numel()])
+
+
 def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, total_norm=None, max_norm=None,
                copies=None):
     """``hag_adamw_step``: one AdamW step over all ``params``, which it changes in place with their ``state``
@@ -991,31 +1024,32 @@ def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
     if not params or not params[0].is_cuda:
         raise ValueError("parameters must be a list of device tensors, not empty")
     index, count = params[0].get_device(), len(params)
-    ptrs, lens, kinds = _tensor_list(params, index, "parameters")
     if len(grads) != count:
         raise ValueError(f"{len(grads)} gradients for {count} parameters")
-    missing = any(g is None for g in grads)
-    some = [p if g is None else g for g, p in zip(grads, params)] if missing else grads
-    gptrs, glens, gkinds = _tensor_list(some, index)
+    ptrs, lens, codes = _addresses(params, index, "parameters")
+    try:
+        gptrs, glens, gcodes = _addresses(grads, index, "gradients")
+    except AttributeError:                                      # some are None
+        gptrs, glens, gcodes = _addresses([p if g is None else g for g, p in zip(grads, params)], index, "gradients")
+        gptrs = [0 if g is None else at for g, at in zip(grads, gptrs)]
     if glens != lens:
         raise ValueError("gradients must have the lengths of the parameters")
-    if missing:
-        gptrs = [0 if g is None else at for g, at in zip(grads, gptrs)]
-    written = [at for at, m in zip(ptrs, lens) if m]
-    cptrs = None
+    cptrs, written = None, ptrs
     if copies is not None:
         if len(copies) != count:
             raise ValueError(f"{len(copies)} copies for {count} parameters")
         here = [c for c in copies if c is not None]
-        _, clens, ckinds = _tensor_list(here, index, "copies") if here else ([], [], [])
-        if clens != [m for m, c in zip(lens, copies) if c is not None] or any(k is not torch.bfloat16 for k in ckinds):
+        some, clens, ckinds = _addresses(here, index, "copies") if here else ([], [], [])
+        if clens != [m for m, c in zip(lens, copies) if c is not None] or any(k != HAG_BF16 for k in ckinds):
             raise ValueError("copies must be bfloat16 tensors with the lengths of the parameters")
-        cptrs = array("Q", [0 if c is None else c.data_ptr() for c in copies])
-        written += [c.data_ptr() for c, m in zip(copies, lens) if c is not None and m]
-    if len(set(written)) != len(written) or not set(written).isdisjoint([at for at, m in zip(gptrs, lens) if m]):
-        raise ValueError("a tensor is named twice, or a gradient is written as a parameter or copy")
+        written = ptrs + some
+        cptrs = array("Q", some if len(here) == count else [0 if c is None else c.data_ptr() for c in copies])
+    names = set(written)
+    if len(names) != len(written) or not names.isdisjoint(gptrs):
+        if _written_twice(params, copies, grads):
+            raise ValueError("a tensor is named twice, or a gradient is written as a parameter or copy")
     mean, square, scales = state
-    blocks = sum(-(-m // HAG_ADAMW_BLOCK) for m in lens)
+    blocks = sum([(m + (HAG_ADAMW_BLOCK - 1)) // HAG_ADAMW_BLOCK for m in lens])
     bits8 = scales is not None
     sdt = torch.float8_e4m3fn if bits8 else torch.float32
     for t, what in ((mean, "mean"), (square, "square")):
@@ -1023,7 +1057,7 @@ def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
             raise ValueError(f"state.{what} must be a contiguous {sdt} tensor of shape ({blocks}, {HAG_ADAMW_BLOCK}) on cuda:{index}")
     if bits8 and (scales.shape != (blocks, 2) or scales.dtype is not torch.float32 or not scales.is_contiguous() or scales.get_device() != index):
         raise ValueError(f"state.scales must be a contiguous float32 tensor of shape ({blocks}, 2) on cuda:{index}")
-    decays = array("d", [weight_decay] * count if isinstance(weight_decay, (int, float)) else weight_decay)
+    decays = array("d", [weight_decay]) * count if isinstance(weight_decay, (int, float)) else array("d", weight_decay)
     if len(decays) != count:
         raise ValueError(f"{len(decays)} weight decays for {count} parameters")
     o = HagAdamwOptions(beta1=betas[0], beta2=betas[1], eps=eps)
@@ -1039,9 +1073,7 @@ def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
         raise ValueError("total_norm and max_norm go together")
     if total_norm is not None:
         o.total_norm, o.max_norm = _one_value(total_norm, "total_norm", index, torch.float32), max_norm
-    addresses, gaddresses, lengths = array("Q", ptrs), array("Q", gptrs), array("q", lens)
-    codes, gcodes = array("i", [_codes[k] for k in kinds]), array("i", [_codes[k] for k in gkinds])
-    _call("hag_adamw_step", index, count, addresses.buffer_info()[0], codes.buffer_info()[0], gaddresses.buffer_info()[0],
-          gcodes.buffer_info()[0], None if cptrs is None else cptrs.buffer_info()[0], lengths.buffer_info()[0], decays.buffer_info()[0],
-          HAG_STATE8 if bits8 else HAG_STATE32, mean.data_ptr(), square.data_ptr(), scales.data_ptr() if bits8 else None, ctypes.byref(o))
+    lists = [array("Q", ptrs), array("i", codes), array("Q", gptrs), array("i", gcodes), cptrs, array("q", lens), decays]
+    _call("hag_adamw_step", index, count, *[None if x is None else x.buffer_info()[0] for x in lists], HAG_STATE8 if bits8 else HAG_STATE32,
+          mean.data_ptr(), square.data_ptr(), scales.data_ptr() if bits8 else None, ctypes.byref(o))
     return params
