@@ -7,7 +7,17 @@
 // rather than v: it spans half the binades, and it is what the step divides by.  A positive root is never stored as
 // zero, since m of the same element, which has a scale of its own, might not be: m / eps would be a step of any size.
 //
-// A warp takes a block, eight elements per lane; the largest of a block is two warp-wide maxima.
+// A warp takes a block, eight elements per lane; the largest of a block is a maximum over the warp.  Coefficients are folded
+// so that a pair of elements takes few instructions (m: one product and one fused product of what is read; v: the square of
+// one product plus that of another), two elements per instruction where there is one for that; the root, the reciprocal
+// and the codes are the hardware's.
+//
+// Bound by memory: 10 bytes per bf16 parameter with 8-bit states, 28 per fp32 one with fp32 states.  Measured on B200,
+// 24 to 40 tensors of 200 million parameters together: bf16 with 8-bit states 327 us (6.1 TB/s), fp32 with bf16 gradients and
+// copies and fp32 states 915 us (6.1 TB/s); 12 tensors of 50 000 values together 3.0 and 3.6 us.  A warp that copied its
+// blocks into a ring in shared memory first took 415 us and 998, one that read the next block into registers 458 and 911.
+// Tensors that do not begin on four of their elements are read one element at a time: 7 million fp32 parameters with
+// 8-bit states 34 us, aligned 20.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -390,8 +400,13 @@ bool dtype_ok(hag_dtype d) { return d == HAG_F32 || d == HAG_BF16; }
 int size_of(hag_dtype d) { return d == HAG_F32 ? 4 : 2; }
 bool on(const void *p, int bytes) { return reinterpret_cast<uintptr_t>(p) % uintptr_t(bytes) == 0; }
 
-constexpr int kUnit = 4;                        // blocks that a warp takes at a time, and of how many on in a launch
-constexpr int64_t kFewBlocks = kSms * 4 * kAdamWarps * 2;
+// Blocks that a warp takes at a time where a launch has more than kFewBlocks: four, all of whose data is read before the
+// first is worked on, so that what surrounds a block (its tensor, its addresses) is shared.  200 million bf16 parameters
+// with 8-bit states: four 327 us, two 364, eight 363; one, as a launch of few blocks takes them, 391.  Of few blocks one at
+// a time, for more warps: 5 million fp32 parameters with 8-bit states 16.2 us, four at a time 20.0; 8 million 24.9 and
+// 27.0, with fp32 states 40.7 and 38.7; 16 million bf16 with 8-bit states 36.5 and 30.8.
+constexpr int kUnit = 4;
+constexpr int64_t kFewBlocks = kSms * 4 * kAdamWarps * 5;
 constexpr int64_t kMostBlocks = 0x7fffffffLL;   // of a tensor and of a launch
 }  // namespace
 
