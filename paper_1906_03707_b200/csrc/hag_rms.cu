@@ -403,6 +403,7 @@ cudaError_t launch_rows(RmsArgs &p, int warps, cudaStream_t s) {
     constexpr auto kernel = rms_fwd_kernel<X, S, Y, V, L, K, QUANT, RES>;
     constexpr int R = kTurnRows<X, S, V, L, K, RES>, kGroup = L > 0 ? L : 32;
     const unsigned threads = L > 0 ? kWarpRowThreads : unsigned(warps) * 32;
+    if (!columns_fit<Place<L, K, QUANT && V == 1>, K>(p.D / V, warps)) return cudaErrorInvalidConfiguration;
     const cudaError_t err = allow_shared<kernel>();
     if (err != cudaSuccess) return err;
     const int64_t rows = L > 0 ? int64_t(kWarpRowThreads / kGroup) * R : 1;

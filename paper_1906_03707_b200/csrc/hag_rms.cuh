@@ -163,6 +163,13 @@ struct Place {
     __device__ __forceinline__ int64_t leader() const { return kWarpRows ? group - (threadIdx.x & 31) / kLanes : group; }
 };
 
+// Whether the chunks of a row's warps cover it, and all but the last kPartial of each lie within it.
+template <typename P, int K>
+inline bool columns_fit(int n_vec, int warps) {
+    const int64_t step = P::kWarpRows ? P::kLanes : 32 * int64_t(warps);
+    return K * step >= n_vec && (K - P::kPartial) * step <= n_vec;
+}
+
 // Sums of R values over the lanes (or the block) that share a row; get(i) is the i-th in every lane, after f was applied to
 // it.  Where there are more lanes than rows the sums are spread over the lanes, and f is computed once.
 template <int L, int R>

@@ -103,6 +103,38 @@ __global__ void __launch_bounds__(kThreadsOf<L>, L > 0 ? 2 : 1) rms_bwd_kernel(c
 #pragma unroll
     for (int k = 0; k < K; ++k) sum[k].fill(0.0f);
     if constexpr (kHold) load_all_weights<V, K>(w, p.w, p.w_bf16, p.w_vectors, at, n_vec);
+    // narrow vectors: rows as they are in memory, the next ones on their way while a row of a block is worked on
+    constexpr bool kAhead = !RING && L == 0 && K <= 8;
+    struct Raw {
+        hagr::Vec<Y, V> g[R][K];
+        hagr::Vec<S, V> t[R][K], a[ALONG ? R : 1][ALONG ? K : 1];
+    };
+    auto fetch = [&](Raw &x, int64_t r0) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const bool live = r0 + i < p.n;
+            const char *gr = static_cast<const char *>(p.g) + (r0 + i) * ld_g, *tr = static_cast<const char *>(p.total) + (r0 + i) * ld_total;
+            const char *ar = static_cast<const char *>(p.along) + (r0 + i) * ld_along;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                x.g[i][k].zero();
+                x.t[i][k].zero();
+                if (live && at.mine(k, n_vec)) {
+                    x.g[i][k].template load<hagr::kKeep>(gr, at.vec(k));
+                    x.t[i][k].template load<hagr::kKeep>(tr, at.vec(k));
+                }
+            }
+            if constexpr (ALONG) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    x.a[i][k].zero();
+                    if (live && at.mine(k, n_vec)) x.a[i][k].template load<hagr::kKeep>(ar, at.vec(k));
+                }
+            }
+        }
+    };
+    Raw next_rows;
+    if constexpr (kAhead) fetch(next_rows, at.group * R);
     auto give_back = [&]() {
         if (CY::kCrosses || CS::kCrosses) __syncwarp();
         issue();
@@ -134,37 +166,20 @@ __global__ void __launch_bounds__(kThreadsOf<L>, L > 0 ? 2 : 1) rms_bwd_kernel(c
                 }
                 give_back();
             } else {
-                hagr::Vec<Y, V> g[R][K];
-                hagr::Vec<S, V> t[R][K], b[R][K];
-#pragma unroll
-                for (int i = 0; i < R; ++i) {
-                    const bool live = r0 + i < p.n;
-                    const char *gr = static_cast<const char *>(p.g) + (r0 + i) * ld_g, *tr = static_cast<const char *>(p.total) + (r0 + i) * ld_total;
-                    const char *br = static_cast<const char *>(p.along) + (r0 + i) * ld_along;
-#pragma unroll
-                    for (int k = 0; k < K; ++k) {
-                        g[i][k].zero();
-                        t[i][k].zero();
-                        if (live && at.mine(k, n_vec)) {
-                            g[i][k].template load<hagr::kKeep>(gr, at.vec(k));
-                            t[i][k].template load<hagr::kKeep>(tr, at.vec(k));
-                        }
-                    }
-                    if (ALONG) {
-#pragma unroll
-                        for (int k = 0; k < K; ++k) {
-                            b[i][k].zero();
-                            if (live && at.mine(k, n_vec)) b[i][k].template load<hagr::kKeep>(br, at.vec(k));
-                        }
-                    }
+                Raw now;
+                if constexpr (kAhead) {
+                    now = next_rows;
+                    fetch(next_rows, r0 + at.groups * R);
+                } else {
+                    fetch(now, r0);
                 }
 #pragma unroll
                 for (int i = 0; i < R; ++i)
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
-                        q[i][k] = hagr::widen(g[i][k]);
-                        hh[i][k] = hagr::widen(t[i][k]);
-                        if (ALONG) a[i][k] = hagr::widen(b[i][k]);
+                        q[i][k] = hagr::widen(now.g[i][k]);
+                        hh[i][k] = hagr::widen(now.t[i][k]);
+                        if constexpr (ALONG) a[i][k] = hagr::widen(now.a[i][k]);
                         else a[i][k].fill(0.0f);
                     }
             }
@@ -423,6 +438,7 @@ cudaError_t launch_rows(RmsBwdArgs &p, int warps, cudaStream_t s) {
     constexpr auto kernel = rms_bwd_kernel<S, Y, V, L, K, ALONG>;
     constexpr int R = kTurnRows<S, Y, V, L, K, ALONG>, kGroup = L > 0 ? L : 32;
     const unsigned threads = L > 0 ? kWarpRowThreads : unsigned(warps) * 32;
+    if (!columns_fit<Place<L, K, false>, K>(p.D / V, warps)) return cudaErrorInvalidConfiguration;
     const cudaError_t err = allow_shared<kernel>();
     if (err != cudaSuccess) return err;
     size_t shared = L > 0 ? size_t(threads / 32) * L * K * V * 4 : 0;
@@ -482,6 +498,9 @@ cudaError_t launch_width(RmsBwdArgs &p, cudaStream_t s) {
         if (chunks <= 12) return launch_rows<S, Y, V, 32, 12, ALONG>(p, 1, s);
         if (chunks <= 14) return launch_rows<S, Y, V, 32, 14, ALONG>(p, 1, s);
         if (chunks <= 16) return launch_rows<S, Y, V, 32, 16, ALONG>(p, 1, s);
+        // eight chunks per warp leave registers for the next row: 39 960 x 1001 bf16 76 us, with up to sixteen 87; 5000 x 1001
+        // fp32 17.6 and 22.4 (of 17 and 18 chunks more than the last two of a warp would lie beyond the row)
+        if (chunks > 18 && chunks <= kRowThreads / 32 * 8) return launch_rows<S, Y, V, 0, 8, ALONG>(p, (chunks + 7) / 8, s);
         const int pairs = (chunks + 1) / 2, warps = (2 * pairs + kPerThread - 1) / kPerThread, k = (pairs + warps - 1) / warps * 2;
         if (wide) {            // as many warps as a block may have: their columns' loads are all that hides latency
             const int most = kWideThreads / 32, few = (pairs + most - 1) / most, many = (pairs + few - 1) / few;

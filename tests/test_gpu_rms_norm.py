@@ -153,6 +153,29 @@ def test_backward(n, d, types):
 
 
 @pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("pad", [0, 3])
+def test_every_width(types, pad):
+    """All widths up to 700 and every 31st up to 9000: neighbours of every change of the kernel, each row's end guarded."""
+    for d in [*range(1, 701), *range(701, 9000, 31)]:
+        x, residual, w = _inputs(50, 3, d + pad, types)
+        x, residual, w = x[:, :d], residual[:, :d], w[:d]
+        guard = {t: torch.full((5, d + pad), 3.0, device="cuda", dtype=t) for t in {TYPES[types][1], TYPES[types][2]}}
+        for t, out in guard.items():
+            inside = out[1:4, :d]
+            if t is TYPES[types][2]:
+                _check_forward(x, w, residual, out=inside)
+            if t is TYPES[types][1]:
+                _check_backward(x if types == "mixed" else residual, residual, w, residual, out=inside)
+            inside.fill_(3.0)
+            assert (out == 3).all(), d
+        if d % 3 == 0:
+            codes = torch.full((5, d + pad), 3, device="cuda", dtype=I8)
+            _check_quant(x, w, residual, (32, 64, 128, 0)[d // 3 % 4], I8, out=codes[1:4, :d])
+            codes[1:4, :d] = 3
+            assert (codes == 3).all(), d
+
+
+@pytest.mark.parametrize("types", TYPES)
 def test_strides_offsets_and_in_place(types):
     tx, ts, ty = TYPES[types]
     a, b, c, e = _randn(12, 70, 700).to(tx), _randn(13, 70, 650).to(ts), _randn(14, 70, 670).to(ty), _randn(15, 70, 690).to(ts)
