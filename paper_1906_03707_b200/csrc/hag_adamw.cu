@@ -14,7 +14,7 @@
 //
 // Bound by memory: 10 bytes per bf16 parameter with 8-bit states, 28 per fp32 one with fp32 states.  Measured on B200,
 // 24 to 40 tensors of 200 million parameters together: bf16 with 8-bit states 327 us (6.1 TB/s), fp32 with bf16 gradients and
-// copies and fp32 states 915 us (6.1 TB/s); 12 tensors of 50 000 values together 3.0 and 3.6 us.  A warp that copied its
+// copies and fp32 states 829 us (6.7 TB/s); 12 tensors of 50 000 values together 3.0 and 3.6 us.  A warp that copied its
 // blocks into a ring in shared memory first took 415 us and 998, one that read the next block into registers 458 and 911.
 // Tensors that do not begin on four of their elements are read one element at a time: 7 million fp32 parameters with
 // 8-bit states 34 us, aligned 20.
@@ -404,7 +404,10 @@ bool on(const void *p, int bytes) { return reinterpret_cast<uintptr_t>(p) % uint
 // first is worked on, so that what surrounds a block (its tensor, its addresses) is shared.  200 million bf16 parameters
 // with 8-bit states: four 327 us, two 364, eight 363; one, as a launch of few blocks takes them, 391.  Of few blocks one at
 // a time, for more warps: 5 million fp32 parameters with 8-bit states 16.2 us, four at a time 20.0; 8 million 24.9 and
-// 27.0, with fp32 states 40.7 and 38.7; 16 million bf16 with 8-bit states 36.5 and 30.8.
+// 27.0; 16 million bf16 ones 36.5 and 30.8.
+// The grid: with 8-bit states as many thread blocks as run at once (150 million fp32 parameters 377 us, a hundred per SM
+// 423); with fp32 states up to a hundred per SM, which take their units as others end (150 million fp32 parameters 611 us,
+// as many as run 690; of few blocks up to sixteen: 5 million 23.8 us, four 26.2).
 constexpr int kUnit = 4;
 constexpr int64_t kFewBlocks = kSms * 4 * kAdamWarps * 5;
 constexpr int64_t kMostBlocks = 0x7fffffffLL;   // of a tensor and of a launch
@@ -481,7 +484,7 @@ extern "C" hag_status hag_adamw_step(int32_t count, void *const *params, const h
                 a.first[i] = a.units;
                 a.units += many ? (a.blocks[i] + kUnit - 1) / kUnit : a.blocks[i];
             }
-            const unsigned grid = unsigned(std::min<int64_t>((int64_t(a.units) + kAdamWarps - 1) / kAdamWarps, kSms * (many ? 2 : 4)));
+            const unsigned grid = unsigned(std::min<int64_t>((int64_t(a.units) + kAdamWarps - 1) / kAdamWarps, kSms * (bits8 ? (many ? 2 : 4) : (many ? 100 : 16))));
             void (*const kernel)(AdamArgs) = bits8 ? many ? adamw_kernel<true, kUnit> : adamw_kernel<true, 1>
                                                    : many ? adamw_kernel<false, kUnit> : adamw_kernel<false, 1>;
             err = hagl::launch_pdl<AdamArgs>(kernel, grid, unsigned(kAdamThreads), a, s);

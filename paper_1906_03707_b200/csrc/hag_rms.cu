@@ -2,8 +2,14 @@
 //   h = x + residual, rstd = 1 / sqrt(mean(h^2) + eps), y = h * rstd * w
 // or, in 8 bits, q = round(y / scale) with scale = max|y| / top over a row or a block of its columns.
 // h is added in fp32 and stays in registers between the sum of its squares and y, so a row is read once and y comes from
-// the sum before it is rounded to the stream's type.  Rows of more columns than a block's registers hold are read two or
-// three times, from the second time on out of the caches.
+// the sum before it is rounded to the stream's type.  Rows of more than 16 384 columns are read two or three times, from the
+// second time on out of the caches.
+//
+// Bound by memory.  Measured on B200 against a copy at 6.53 TB/s: 10^6 x 256 bf16 319 us (6.4 TB/s), around an fp32 stream 472
+// (6.5), into e4m3 with a scale per row 285 (6.3); 233 000 x 128 fp32 75.5 us (6.3); 30 000 x 4096 bf16 149 us (6.6); 10 000 x
+// 12 000 bf16 150 us (6.4).  Into 8 bits the instructions come near, 57 % of the issue slots.  Rows that do not begin on 16
+// bytes are read and written one element at a time: 300 000 x 333 fp32 275 us (5.8 TB/s), bf16 170 (4.7), 50 000 x 1433 bf16
+// into e4m3 169 (2.9: a byte per store).
 #include "hag_rms.cuh"
 
 #include <cfloat>
@@ -392,11 +398,13 @@ __global__ void __launch_bounds__(kRowThreads, 1) rms_fwd_long_kernel(const __gr
     }
 }
 
-// Threads per SM of the kernels with a ring: what is on its way at a time decides how near they come to the memory's rate.
-// Rows of up to 32 bytes per lane and turn: two stages of 512 threads (10^6 x 256 bf16 320 us, with three stages 365, with
-// twice the threads 333, with one stage of them 419).  More bytes per lane: one stage of 1536 threads (500 000 x 512 bf16
-// 313 us, with two stages of 512 threads 335; 10^6 x 256 bf16 around an fp32 stream 478 and 542).
-constexpr int kShortThreads = 512, kLongThreads = 1536;
+// Threads per SM of the kernels with a ring: what is on its way at a time, and how rows are handed out, decide how near they
+// come to the memory's rate.  Rows of up to 32 bytes per lane and turn: two stages of 512 threads, as many blocks as run at
+// once (10^6 x 256 bf16 319 us, with three stages 365, with twice the threads 333, with one stage of them 419).  More bytes
+// per lane: one stage, and more blocks than run at once, which take their rows as others end: 6144 threads (200 000 x 512
+// fp32 243 us, 500 000 x 256 fp32 307, 10^6 x 256 bf16 around an fp32 stream 472; 1536 threads 253, 327 and 479; two stages
+// of 512 threads 269, 354 and 542).
+constexpr int kShortThreads = 512, kLongThreads = 6144;
 
 template <typename X, typename S, typename Y, int V, int L, int K, bool QUANT, bool RES>
 cudaError_t launch_rows(RmsArgs &p, int warps, cudaStream_t s) {
@@ -408,15 +416,17 @@ cudaError_t launch_rows(RmsArgs &p, int warps, cudaStream_t s) {
     if (err != cudaSuccess) return err;
     const int64_t rows = L > 0 ? int64_t(kWarpRowThreads / kGroup) * R : 1;
     size_t shared = 0;
-    int most = kSms;
+    int most;
     if constexpr (kRing<X, S, V>) {
         constexpr int kLane = R * kRowBytes<X, S, V, K, RES>;
         constexpr bool kShort = kLane <= kTurnBytes || (L <= 0 && QUANT);
         p.stages = kShort && size_t(kLane) * threads * 2 <= size_t(kMostShared) ? 2 : 1;
         shared = size_t(kLane) * threads * p.stages;
         most = std::max(L < 0 ? 1 : 2, (kShort ? kShortThreads : kLongThreads) / int(threads));
+        if (kShort) most = std::min(most, blocks_per_sm<kernel>(threads, shared));
+    } else {
+        most = blocks_per_sm<kernel>(threads, shared);
     }
-    most = std::min(most, blocks_per_sm<kernel>(threads, shared));
     const int64_t grid = std::min<int64_t>((p.n + rows - 1) / rows, int64_t(kSms) * most);
     return launch(kernel, dim3(unsigned(grid)), threads, shared, p, s);
 }

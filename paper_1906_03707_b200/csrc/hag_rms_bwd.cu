@@ -2,6 +2,12 @@
 //   grad = rstd * (q - hh * mean(q * hh)) + what arrives along the residual stream,  gw = sum over rows of g * hh
 // A row is read once and its gradient written once; gw stays with the threads over all their rows, is joined per block
 // and then over the blocks, in a fixed order.
+//
+// Bound by memory.  Measured on B200, where a copy runs at 6.53 TB/s: with a gradient along the stream 10^6 x 256 bf16 294 us
+// (7.0 TB/s: three reads for a write), around an fp32 stream 624 (6.6), 30 000 x 4096 bf16 147 (6.7); without one 10^6 x 256
+// bf16 235 us (6.5).  Blocks of more than 512 threads have no registers left for what they read, read it twice and wait for
+// it: 10 000 x 12 000 bf16 277 us (3.5).  Rows that do not begin on 16 bytes are read one element at a time: 300 000 x 333
+// fp32 244 us (6.6), bf16 181 (4.4), 5001 x 1433 fp32 without a gradient along the stream 21.5 (4.0; 3 of them the join).
 #include "hag_rms.cuh"
 
 namespace {
@@ -448,7 +454,9 @@ cudaError_t launch_rows(RmsBwdArgs &p, int warps, cudaStream_t s) {
         if (size_t(kLane) * threads * p.stages > size_t(kMostShared)) p.stages = 1;
         shared = std::max(shared, size_t(kLane) * threads * p.stages);
     }
-    const int most = blocks_per_sm<kernel>(threads, shared);
+    // Two operands: four times as many blocks as run at once, which take their rows as others end (10^6 x 256 bf16 235 us, as
+    // many as run 247); three operands, or rows of blocks: as many as run (10^6 x 256 bf16 295 us, four times as many 300).
+    const int most = blocks_per_sm<kernel>(threads, shared) * (kRing<Y, V> && L > 0 && !ALONG ? 4 : 1);
     const int64_t rows = L > 0 ? int64_t(kWarpRowThreads / kGroup) * R : 1;
     int64_t grid = std::min<int64_t>((p.n + rows - 1) / rows, std::min(kSms * most, most_parts(p.D)));
     if (L > 0 && p.partial && p.n * p.D <= kFewValues) grid = 1;
