@@ -584,6 +584,7 @@ hag_status hag_rms_norm_bwd(int64_t n, int32_t D, const void *grad_y, hag_dtype 
  *                those of block b.  scale = largest finite magnitude / 448, at least 2^-126; each value is rounded to
  *                nearest after the step has been taken with the new m and v in fp32; a positive root is stored as 2^-9
  *                at least; a value that is not finite is stored as NaN and does not touch the rest of its block.
+ * In the step, and in the stored roots, a v below 2^-126 counts as 0, and so does an eps below 2^-126.
  * options: numbers that change from step to step may be given on the device, so that a captured call replays with new
  * ones: lr_device in the place of lr, step_device in the place of step (read by the call; who counts it up is the caller;
  * a step below 1 counts as 1).

@@ -1019,7 +1019,8 @@ def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
     ``step`` counts from 1, ``lr`` is the rate; either may be a device tensor of one value (int64, float32), which a
     captured call reads anew each time.  ``weight_decay`` is a number or a list of one per parameter.  With ``total_norm``
     (what ``grad_norm`` returned) the gradients are scaled as ``clip_grad_norm`` does for ``max_norm``, on the way.
-    ``copies``: a list of bfloat16 tensors (or None entries) that receive the new values.  Returns ``params``."""
+    ``copies``: a list of bfloat16 tensors (or None entries) that receive the new values.  Torch's own
+    differentiation does not notice that the parameters change: step after the backward pass.  Returns ``params``."""
     import torch
     if not params or not params[0].is_cuda:
         raise ValueError("parameters must be a list of device tensors, not empty")

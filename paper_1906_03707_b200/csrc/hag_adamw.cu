@@ -73,7 +73,7 @@ struct Coefficients {
 // What the gradient is multiplied with for m, and, before its square, for v.
 __device__ __forceinline__ float2 of_gradient(const AdamArgs &p, float norm) {
     if (!p.norm) return make_float2(p.rest1, p.root_rest2);
-    const float ratio = __fdividef(p.max_norm, norm + 1e-6f);
+    const float ratio = p.max_norm / (norm + 1e-6f);
     const float factor = ratio >= 1.0f ? 1.0f : ratio;         // a norm that is no number gives a factor that is none
     return make_float2(p.rest1 * factor, p.root_rest2 * factor);
 }
@@ -298,9 +298,8 @@ struct Piece {
 };
 
 template <typename P, typename G, bool BITS8, bool VEC>
-__device__ __forceinline__ void step_block(const AdamArgs &a, const Coefficients &c, float keep_, const Piece<P, G, BITS8, VEC> &in,
+__device__ __forceinline__ void step_block(const AdamArgs &a, const Coefficients &c, float keep_, float2 of_g, const Piece<P, G, BITS8, VEC> &in,
                                            const Arrays<P, G, BITS8> &to, int block, int lane, int count) {
-    const float2 of_g = of_gradient(a, c.norm);
     const float2 keep = both(keep_), of_m = both(of_g.x), of_v = both(of_g.y);
     const float2 of_old_m = both(BITS8 ? in.scale.x * a.b1 : a.b1), of_old_v = both(BITS8 ? in.scale.y * a.root2 : a.b2);
     float2 p[kPairs], m[kPairs], v[kPairs], r[kPairs];
@@ -341,8 +340,9 @@ __device__ __forceinline__ void step_unit(const AdamArgs &a, const Coefficients 
             Piece<P, G, BITS8, true> in[B];
 #pragma unroll
             for (int k = 0; k < B; ++k) in[k].load(at, i + k, lane, kAdamBlock);
+            const float2 of_g = of_gradient(a, c.norm);
 #pragma unroll
-            for (int k = 0; k < B; ++k) step_block<P, G, BITS8, true>(a, c, keep, in[k], at, i + k, lane, kAdamBlock);
+            for (int k = 0; k < B; ++k) step_block<P, G, BITS8, true>(a, c, keep, of_g, in[k], at, i + k, lane, kAdamBlock);
         }
     } else {
         const int n = int(min(uint32_t(T), a.blocks[t] - within));
@@ -351,12 +351,12 @@ __device__ __forceinline__ void step_unit(const AdamArgs &a, const Coefficients 
             if (T > 1 && within + i < a.whole[t]) {
                 Piece<P, G, BITS8, true> in;
                 in.load(at, i, lane, kAdamBlock);
-                step_block<P, G, BITS8, true>(a, c, keep, in, at, i, lane, kAdamBlock);
+                step_block<P, G, BITS8, true>(a, c, keep, of_gradient(a, c.norm), in, at, i, lane, kAdamBlock);
             } else {
                 const int count = int(min(int64_t(kAdamBlock), a.len[t] - int64_t(within + i) * kAdamBlock));
                 Piece<P, G, BITS8, false> in;
                 in.load(at, i, lane, count);
-                step_block<P, G, BITS8, false>(a, c, keep, in, at, i, lane, count);
+                step_block<P, G, BITS8, false>(a, c, keep, of_gradient(a, c.norm), in, at, i, lane, count);
             }
         }
     }

@@ -209,6 +209,32 @@ def test_values_that_are_not_finite_stay_alone(bits):
     assert case.params[0].isnan().all()
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("norm,max_norm", [(1e38, math.inf), (3e38, math.inf), (1e38, 1e38), (2.0, math.inf), (0.0, 0.0), (0.0, 1.0), (2.0, 0.0), (1e-30, 1e-30)])
+def test_ends_of_the_norm(bits, norm, max_norm):
+    """min(1, max_norm / (norm + 1e-6)) where a quotient may overflow or vanish."""
+    Case(10, [3000, 41], ("f32", "bf16"), bits).check(norm=torch.tensor(norm, device="cuda"), max_norm=max_norm)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_places_without_gradient_do_not_move_but_for_decay(bits):
+    """Rows of a table that no batch names: m and v stay zero, and p (1 - lr decay) is exact to 2 u and the rounding."""
+    p, g = torch.randn(5000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(11)), torch.zeros(5000, device="cuda")
+    g[700:900] = 0.5
+    state = hb.adamw_state([p], bits)
+    want = p.double()
+    for t in range(1, 6):
+        hb.adamw_step([p], [g], state, t, lr=1e-2, weight_decay=0.1)
+        want = want * (1 - 1e-3)
+    still = torch.ones(5000, dtype=torch.bool, device="cuda")
+    still[700:900] = False
+    assert ((p.double() - want).abs()[still] <= 5 * 3 * U * want.abs()[still]).all()
+    places = still.new_zeros(state.mean.shape).view(-1)
+    places[:5000] = still
+    for x in (state.mean, state.square):
+        assert not x.float().view(-1)[places].any() and (x.float().view(-1)[700:900] != 0).all()
+
+
 def test_runs_repeat_and_shapes():
     outs = []
     for _ in range(2):
