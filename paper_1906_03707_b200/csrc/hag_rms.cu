@@ -253,7 +253,8 @@ __global__ void __launch_bounds__(kThreadsOf<L>, L > 0 ? 2 : 1) rms_fwd_kernel(c
 #pragma unroll
                 for (int k = 0; k < K; ++k) h[i][k].mul(w[k]);
             } else {
-                constexpr int U = V > 1 ? 1 : 4;
+                constexpr int U = V > 1 ? 1 : K % 4 == 0 ? 4 : 2;
+                static_assert(K % U == 0, "");
 #pragma unroll
                 for (int k = 0; k < K; k += U) {
                     hagr::Pairs<V> some[U];

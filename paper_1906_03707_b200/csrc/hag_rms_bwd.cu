@@ -216,7 +216,8 @@ __global__ void __launch_bounds__(kThreadsOf<L>, L > 0 ? 2 : 1) rms_bwd_kernel(c
             static_assert(kHold || R == 1, "");
             const char *gr = static_cast<const char *>(p.g) + r0 * ld_g, *tr = static_cast<const char *>(p.total) + r0 * ld_total;
             const char *br = static_cast<const char *>(p.along) + r0 * ld_along, *from = raw + read;
-            constexpr int U = V >= 4 ? 1 : 4;                  // vectors at a time
+            constexpr int U = V >= 4 ? 1 : K % 4 == 0 ? 4 : 2; // vectors at a time
+            static_assert(K % U == 0, "");
             auto pass = [&](auto f) {
 #pragma unroll
                 for (int k0 = 0; k0 < K; k0 += U) {

@@ -112,7 +112,8 @@ def _inputs(seed, n, d, types):
 
 SHAPES = [(1, 1), (1, 4096), (1, 8193), (3, 2), (1000, 16), (257, 20), (5000, 64), (1001, 128), (777, 33), (640, 256), (300, 250), (129, 515),
           (90, 1024), (66, 1433), (40, 2048), (31, 4100), (12, 8192), (9, 16384), (5, 16386), (3, 50001), (2, 49153), (700, 8), (611, 31), (2, 70_001), (3, 131_072),
-          (4, 12_000), (300, 9999), (7, 32_800), (5, 65_536)]
+          (4, 12_000), (300, 9999), (7, 32_800), (5, 65_536),
+          (6, 8191), (6, 11_501), (161, 13_001), (155, 14_337), (4, 16_383)]
 
 
 @pytest.mark.parametrize("n,d", SHAPES)
