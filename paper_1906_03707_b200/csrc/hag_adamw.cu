@@ -13,8 +13,8 @@
 // and the codes are the hardware's.
 //
 // Bound by memory: 10 bytes per bf16 parameter with 8-bit states, 28 per fp32 one with fp32 states.  Measured on B200,
-// 24 to 40 tensors of 200 million parameters together: bf16 with 8-bit states 327 us (6.1 TB/s), fp32 with bf16 gradients and
-// copies and fp32 states 829 us (6.7 TB/s); 12 tensors of 50 000 values together 3.0 and 3.6 us.  A warp that copied its
+// 24 to 40 tensors of 200 million parameters together: bf16 with 8-bit states 319 us (6.3 TB/s), fp32 with bf16 gradients and
+// copies and fp32 states 825 us (6.8 TB/s); 12 tensors of 50 000 values together 3.5 and 3.0 us.  A warp that copied its
 // blocks into a ring in shared memory first took 415 us and 998, one that read the next block into registers 458 and 911.
 // Tensors that do not begin on four of their elements are read one element at a time: 7 million fp32 parameters with
 // 8-bit states 34 us, aligned 20.

@@ -424,7 +424,7 @@ cudaError_t launch_rows(RmsArgs &p, int warps, cudaStream_t s) {
         p.stages = kShort && size_t(kLane) * threads * 2 <= size_t(kMostShared) ? 2 : 1;
         shared = size_t(kLane) * threads * p.stages;
         most = std::max(L < 0 ? 1 : 2, (kShort ? kShortThreads : kLongThreads) / int(threads));
-        if (kShort) most = std::min(most, blocks_per_sm<kernel>(threads, shared));
+        if (kShort || L < 0) most = std::min(most, blocks_per_sm<kernel>(threads, shared));      // 10 000 x 12 000 bf16 150 us, else 163
     } else {
         most = blocks_per_sm<kernel>(threads, shared);
     }
