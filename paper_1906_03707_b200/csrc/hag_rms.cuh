@@ -30,7 +30,8 @@ struct Wide {
             uint32_t *w = v.raw.w;
             asm volatile("ld.global.cg.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                          : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-                         : "l"(static_cast<const char *>(row) + i * 32));
+                         : "l"(static_cast<const char *>(row) + i * 32)
+                         : "memory");
         } else {
             v.template load<hagr::kKeep>(row, size_t(i));
         }
@@ -53,9 +54,6 @@ __device__ __forceinline__ float load_one(const void *p, int64_t i) {
     v.template load<hagr::kKeep>(p, size_t(i));
     return v.get(0);
 }
-__device__ __forceinline__ float load_weight(const void *p, int bf16, int64_t i) {
-    return !p ? 1.0f : bf16 ? load_one<__nv_bfloat16>(p, i) : load_one<float>(p, i);
-}
 __device__ __forceinline__ void store_weight(void *p, int bf16, int64_t i, float f) {
     if (bf16) {
         hagr::Vec<__nv_bfloat16, 1> v;
@@ -65,8 +63,8 @@ __device__ __forceinline__ void store_weight(void *p, int bf16, int64_t i, float
         static_cast<float *>(p)[i] = f;
     }
 }
-// The weights of a thread's K vectors, zeros beyond the row; `vectors`: whether they can be read as such.  Without weights they are ones.  One
-// test of the type for all of them: loads behind a test of their own would wait for one another.
+// The weights of a thread's K vectors, zeros beyond the row; `vectors`: whether they can be read as such.  Without weights
+// they are ones.  One test of the type for all of them: loads behind a test of their own would wait for one another.
 template <int V, int K, typename At>
 __device__ __forceinline__ void load_all_weights(hagr::Pairs<V> (&w)[K], const void *p, int bf16, bool vectors, const At &at, int n_vec) {
     auto load = [&](auto type, auto width) {

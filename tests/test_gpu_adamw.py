@@ -307,3 +307,33 @@ def test_refusals():
         assert e.value.status == hb.HAG_ERR_ARG
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(p, before))
+
+
+@pytest.mark.parametrize("n,d", [(1, 256), (300, 256), (40, 9000), (700, 333), (64, 9001)])
+def test_steps_and_norms_behind_one_another(n, d):
+    """Kernels start while those before them still run: 100 steps whose norms read the weights that the step before wrote,
+    with nothing waited for, give the bits that they give with a wait after every call."""
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    x, start, table = _randn(gen, n, d), 1 + 0.1 * _randn(gen, d), _randn(gen, 50, d)
+    ids = torch.randint(0, 50, (n,), generator=gen, device="cuda")
+
+    def run(wait):
+        wait()
+        w, t, kept = start.clone(), table.clone(), []
+        state = hb.adamw_state([w, t], 8)
+        for k in range(1, 101):
+            for call in (lambda: hb.embedding_fwd(ids, t), lambda: hb.rms_norm_fwd(kept[-1], w, residual=x),
+                         lambda: hb.rms_norm_bwd(kept[-1][0], kept[-1][1], kept[-1][2], w, grad_total=x),
+                         lambda: hb.adamw_step([w, t], [kept[-1][2], hb.embedding_bwd(ids, kept[-1][0], 50)], state, k, lr=0.05,
+                                               total_norm=hb.grad_norm([kept[-1][2]]), max_norm=1.0)):
+                kept.append(call())
+                wait()
+            kept[-1] = w.clone()
+            wait()
+        return [u for v in kept for u in (v if isinstance(v, tuple) else (v,))] + [t, *state]
+
+    fast, slow = run(lambda: None), run(torch.cuda.synchronize)
+    torch.cuda.synchronize()
+    assert len(fast) == len(slow)
+    for a, b in zip(fast, slow):
+        assert torch.equal(a.float(), b.float())
