@@ -535,8 +535,9 @@ hag_status hag_clip_grad_norm(int32_t count, const void *const *grads, void *con
  *             h is added in fp32; rstd and y are those of the sum as it is, `total` receives it rounded to its type.
  *   forward with an 8-bit output: instead of y, q = round(y / scale) and the scales, one per `block` columns (32, 64 or
  *             128; the last one of a row may have fewer) or, with block 0, one per row: scale = max(|y|) / top, at least
- *             2^-126, top = 448 (HAG_E4M3) or 127 (HAG_I8).  scales: n x ceil(D / block), contiguous.  The quotient is
- *             good to 2^-21 before it is rounded.  A block with a y that is not finite gets a scale that is not finite.
+ *             2^-126, top = 448 (HAG_E4M3) or 127 (HAG_I8).  scales: n x ceil(D / block), contiguous.  max(|y|) is
+ *             multiplied with 1 / top as fp32 holds it; y / scale is the quotient of an fp32 division.  A block with a y that
+ *             is not finite gets a scale that is not finite.
  *   backward: with hh = total * rstd and t = grad_y * weight: grad = rstd * (t - hh * sum(t * hh) / D) + grad_total is the
  *             gradient of x and of the residual alike, grad_weight = sum over rows of grad_y * hh.  grad_total: what
  *             arrives along the residual stream (NULL: nothing).

@@ -1,6 +1,7 @@
 // Root-mean-square norm with the residual's addition, forward.
 //   h = x + residual, rstd = 1 / sqrt(mean(h^2) + eps), y = h * rstd * w
-// or, in 8 bits, q = round(y / scale) with scale = max|y| / top over a row or a block of its columns.
+// or, in 8 bits, q = round(y / scale) with scale = max|y| / top over a row or a block of its columns.  The quotient is that of an
+// fp32 division: the product with a reciprocal alone is off by a place or two, and moves one code in 10^5 to its neighbour.
 // h is added in fp32 and stays in registers between the sum of its squares and y, so a row is read once and y comes from
 // the sum before it is rounded to the stream's type.  Rows of more than 16 384 columns are read two or three times, from the
 // second time on out of the caches.
@@ -31,7 +32,7 @@ struct RmsArgs {
     int32_t block, n_scales;            // columns per scale (0: all), scales per row
     int32_t int8;
     int32_t stages;                     // of the ring
-    float top;
+    float inverse_top;                  // 1 / the type's largest value
 };
 
 // 8-bit codes of V quotients.
@@ -93,9 +94,9 @@ __device__ __forceinline__ float group_largest(float v, float *slot) {
     }
     return v;
 }
-// top is 448 or 127; a largest value that is not finite gives a scale that is none
+// the largest value's product with 1 / 448 or 1 / 127; one that is not finite gives a scale that is none
 __device__ __forceinline__ float scale_of(float largest, const RmsArgs &p) {
-    const float s = largest * (1.0f / p.top);
+    const float s = largest * p.inverse_top;
     return s < FLT_MIN ? FLT_MIN : s;
 }
 
@@ -115,7 +116,7 @@ __device__ __forceinline__ void quant_groups(hagr::Pairs<V> (&y)[K], const RmsAr
         if (!live) continue;
 #pragma unroll
         for (int k = k0; k < k0 + T && k < K; ++k) {
-            y[k].mul_all(inverse);
+            y[k].divide(scale, inverse);
             if (at.mine(k, n_vec)) store_codes<V>(y[k].v, q, at.vec(k), p.int8);
         }
         const int c = at.vec(k0) * V;
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(kThreadsOf<L>, L > 0 ? 2 : 1) rms_fwd_kernel(c
                 if (at.first()) p.scales[r] = scale;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    h[i][k].mul_all(inv);
+                    h[i][k].divide(scale, inv);
                     if (at.mine(k, n_vec)) store_codes<V>(h[i][k].v, to, at.vec(k), p.int8);
                 }
             }
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rms_fwd_long_kernel(const __gr
         }
         const float rstd = rsqrtf(group_sum<0>(s, slots[0]) / float(p.D) + p.eps);
         if (p.rstd && threadIdx.x == 0) p.rstd[r] = rstd;
-        float inv = 0.0f;
+        float scale = 0.0f, inv = 0.0f;
         if constexpr (QUANT) {
             if (!p.block) {
                 float top = 0.0f;
@@ -362,7 +363,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rms_fwd_long_kernel(const __gr
 #pragma unroll
                         for (int j = 0; j < V; ++j) top = larger(top, h[k].v[j]);
                 }
-                const float scale = scale_of(group_largest<0>(top, slots[1]), p);
+                scale = scale_of(group_largest<0>(top, slots[1]), p);
                 if (threadIdx.x == 0) p.scales[r] = scale;
                 inv = __fdividef(1.0f, scale);
             }
@@ -390,7 +391,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rms_fwd_long_kernel(const __gr
             } else {
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    h[k].mul_all(inv);
+                    h[k].divide(scale, inv);
                     if (at.mine(k, n_vec)) store_codes<V>(h[k].v, static_cast<char *>(p.y) + r * p.ld_y, at.vec(k), p.int8);
                 }
             }
@@ -571,7 +572,7 @@ extern "C" hag_status hag_rms_norm_quant_fwd(int64_t n, int32_t D, const void *x
     p.block = block >= D ? 0 : block;
     p.n_scales = p.block ? (D + block - 1) / block : 1;
     p.int8 = kind == HAG_I8;
-    p.top = kind == HAG_I8 ? 127.0f : 448.0f;
+    p.inverse_top = 1.0f / (kind == HAG_I8 ? 127.0f : 448.0f);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t err;
     if (x_dtype != stream_dtype) err = launch_typed<__nv_bfloat16, float, uint8_t, true>(p, m, s);

@@ -251,6 +251,17 @@ struct Pairs {
     __device__ __forceinline__ void add_scaled(const Pairs &a, float m) {                     // v += a * m
         each([&](int j) { put(j, __ffma2_rn(a.two(j), make_float2(m, m), two(j))); }, [&](int j) { v[j] = fmaf(a.v[j], m, v[j]); });
     }
+    // v = v / d, `inverse` an approximate reciprocal of d: the product's remainder, which a fused product gives exactly,
+    // corrects it to the rounded quotient (Markstein 1990); a zero keeps its sign.
+    __device__ __forceinline__ void divide(float d, float inverse) {
+        const Pairs a = *this;
+        mul_all(inverse);
+        each([&](int j) {
+                 const float2 rest = __ffma2_rn(two(j), make_float2(d, d), make_float2(-a.v[j], -a.v[j + 1]));
+                 put(j, __ffma2_rn(rest, make_float2(-inverse, -inverse), two(j)));
+             },
+             [&](int j) { v[j] = fmaf(fmaf(v[j], d, -a.v[j]), -inverse, v[j]); });
+    }
     __device__ __forceinline__ float sum() const {
         float2 s = make_float2(v[0], N > 1 ? v[N > 1] : 0.0f);
 #pragma unroll
