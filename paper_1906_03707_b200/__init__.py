@@ -868,7 +868,8 @@ def _rms_inputs(x, weight, residual, total_out, eps):
 def rms_norm_fwd(x, weight=None, residual=None, eps=1e-5, out=None, total_out=None, dtype=None, stats=True):
     """``hag_rms_norm_fwd`` over the columns of total = x + residual.  Returns (y, total, rstd): y is of ``dtype`` (default:
     x's type; bfloat16 is possible for float32), total of the residual's type, and x itself without a residual; rstd is
-    None where ``stats`` is false (no gradient wanted).  ``out`` and ``total_out`` may be x or the residual."""
+    None where ``stats`` is false (no gradient wanted).  ``out`` and ``total_out`` may be x or the residual; where y takes the
+    place of x and there is no residual, nothing is left that a gradient could be made from, and total is None."""
     import torch
     index, n, d, args, total, total_args = _rms_inputs(x, weight, residual, total_out, eps)
     if out is None:
@@ -876,6 +877,8 @@ def rms_norm_fwd(x, weight=None, residual=None, eps=1e-5, out=None, total_out=No
         ld_out = d
     else:
         ld_out = _rows(out, "out", (n, d), index, dtype)
+        if total is x and n and out.data_ptr() == args[0]:
+            total = None
     rstd = x.new_empty(n, dtype=torch.float32) if stats else None
     _call("hag_rms_norm_fwd", index, n, d, *args, out.data_ptr(), _code(out.dtype), ld_out, *total_args,
           None if rstd is None else rstd.data_ptr())
@@ -928,6 +931,8 @@ def rms_norm_bwd(grad_out, total, rstd, weight=None, grad_total=None, out=None, 
     stream.  grad_weight is of the weight's type (without a weight: ``param_dtype``, default float32), and None where
     ``param_grads`` is false.  ``out`` receives grad_residual; it may be grad_total, total or grad_out."""
     import torch
+    if total is None:
+        raise ValueError("the sum is missing: the forward pass wrote y in its place")
     ld = _rows(total, "total")
     index, stream, shape = total.get_device(), total.dtype, total.shape
     n, d = shape
