@@ -573,8 +573,8 @@ hag_status hag_rms_norm_bwd(int64_t n, int32_t D, const void *grad_y, hag_dtype 
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   p = p (1 - lr decay_i) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
  * params, param_dtypes, grads, grad_dtypes, copies, lengths, decays: HOST arrays of `count` entries (read during the call,
- * not kept); params[i] and grads[i]: DEVICE pointers to lengths[i] contiguous elements.  grads[i] NULL: tensor i and its
- * states stay as they are.  copies (may be NULL, and so may its entries): copies[i] receives the new parameters in bf16.
+ * not kept); params[i] and grads[i]: DEVICE pointers to lengths[i] contiguous elements.  grads[i] NULL: tensor i, its
+ * states and its copy stay as they are.  copies (may be NULL, and so may its entries): copies[i] receives the new parameters in bf16.
  * No two tensors may overlap, and no tensor may be named twice, but that grads may share memory.
  * The states of all tensors lie in one array of blocks of HAG_ADAMW_BLOCK elements, the blocks of tensor i behind those of
  * tensor i - 1, ceil(lengths[i] / HAG_ADAMW_BLOCK) of them; hag_adamw_state_blocks gives their number (-1 on bad

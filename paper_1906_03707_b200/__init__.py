@@ -991,23 +991,23 @@ def _one_value(t, what, index, dtype):
     return t.data_ptr()
 
 
-_dtype_of = attrgetter("dtype")
+_dtype_of, _shape_of = attrgetter("dtype"), attrgetter("shape")
 
 
 def _addresses(tensors, index, what):
-    """Addresses, lengths and type codes of a list of contiguous device tensors; AttributeError where an entry is None."""
+    """Addresses, shapes and type codes of a list of contiguous device tensors; AttributeError where an entry is None."""
     import torch
     T = torch.Tensor
     if not _codes:
         _runtime()
     kinds = list(map(_dtype_of, tensors))
-    try:
-        codes = list(map(_codes.__getitem__, kinds))
+    try:                                                        # most lists are of one type
+        codes = [_codes[kinds[0]]] * len(kinds) if kinds.count(kinds[0]) == len(kinds) else list(map(_codes.__getitem__, kinds))
     except KeyError as e:
         raise TypeError(f"{what} must be float32 or bfloat16, got {e.args[0]}") from None
     if not all(map(T.is_contiguous, tensors)) or set(map(T.get_device, tensors)) != {index}:
         raise ValueError(f"{what} must be contiguous tensors on cuda:{index}")
-    return list(map(T.data_ptr, tensors)), list(map(T.numel, tensors)), codes
+    return list(map(T.data_ptr, tensors)), list(map(_shape_of, tensors)), codes
 
 
 def _written_twice(params, copies, grads):
@@ -1019,12 +1019,13 @@ def _written_twice(params, copies, grads):
 def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, total_norm=None, max_norm=None,
                copies=None):
     """``hag_adamw_step``: one AdamW step over all ``params``, which it changes in place with their ``state``
-    (``adamw_state``).  An entry of ``grads`` may be None: that parameter stays as it is.
+    (``adamw_state``).  Gradients have their parameters' shapes; an entry of ``grads`` may be None: that parameter stays as it is,
+    and its copy is not written.
 
     ``step`` counts from 1, ``lr`` is the rate; either may be a device tensor of one value (int64, float32), which a
     captured call reads anew each time.  ``weight_decay`` is a number or a list of one per parameter.  With ``total_norm``
     (what ``grad_norm`` returned) the gradients are scaled as ``clip_grad_norm`` does for ``max_norm``, on the way.
-    ``copies``: a list of bfloat16 tensors (or None entries) that receive the new values.  Torch's own
+    ``copies``: a list of bfloat16 tensors (or None entries) of the same shapes that receive the new values.  Torch's own
     differentiation does not notice that the parameters change: step after the backward pass.  Returns ``params``."""
     import torch
     if not params or not params[0].is_cuda:
@@ -1032,22 +1033,23 @@ def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
     index, count = params[0].get_device(), len(params)
     if len(grads) != count:
         raise ValueError(f"{len(grads)} gradients for {count} parameters")
-    ptrs, lens, codes = _addresses(params, index, "parameters")
+    ptrs, shapes, codes = _addresses(params, index, "parameters")
+    lens = list(map(torch.Tensor.numel, params))
     try:
-        gptrs, glens, gcodes = _addresses(grads, index, "gradients")
+        gptrs, gshapes, gcodes = _addresses(grads, index, "gradients")
     except AttributeError:                                      # some are None
-        gptrs, glens, gcodes = _addresses([p if g is None else g for g, p in zip(grads, params)], index, "gradients")
+        gptrs, gshapes, gcodes = _addresses([p if g is None else g for g, p in zip(grads, params)], index, "gradients")
         gptrs = [0 if g is None else at for g, at in zip(grads, gptrs)]
-    if glens != lens:
-        raise ValueError("gradients must have the lengths of the parameters")
+    if gshapes != shapes:                                       # of equal length alone a transposed gradient would pass
+        raise ValueError("gradients must have the shapes of the parameters")
     cptrs, written = None, ptrs
     if copies is not None:
         if len(copies) != count:
             raise ValueError(f"{len(copies)} copies for {count} parameters")
         here = [c for c in copies if c is not None]
-        some, clens, ckinds = _addresses(here, index, "copies") if here else ([], [], [])
-        if clens != [m for m, c in zip(lens, copies) if c is not None] or any(k != HAG_BF16 for k in ckinds):
-            raise ValueError("copies must be bfloat16 tensors with the lengths of the parameters")
+        some, cshapes, ckinds = _addresses(here, index, "copies") if here else ([], [], [])
+        if cshapes != [m for m, c in zip(shapes, copies) if c is not None] or any(k != HAG_BF16 for k in ckinds):
+            raise ValueError("copies must be bfloat16 tensors with the shapes of the parameters")
         written = ptrs + some
         cptrs = array("Q", some if len(here) == count else [0 if c is None else c.data_ptr() for c in copies])
     names = set(written)
