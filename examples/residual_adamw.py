@@ -9,7 +9,8 @@ The batch of examples/graph_classification.py; a stream s carries the features f
     logits = p @ W2, cross entropy
 
 Backwards each norm's gradient meets the one that arrives along the stream (rms_norm_bwd, grad_total).  Then grad_norm and
-one adamw_step over all parameters: clipping included, no weight decay on gains, states in 32 or 8 bits.  With bf16 layers
+one adamw_step over all parameters: clipping included, no weight decay on gains, states in 32 or 8 bits (those rounded by
+chance, so that they follow gradients that shrink).  With bf16 layers
 the parameters stay in fp32 and the step writes the bf16 copies that the next pass reads.
 
     python examples/residual_adamw.py [--graphs 400] [--layers 3] [--steps 30] [--dtype f32|bf16] [--bits 32|8]
@@ -41,7 +42,7 @@ class Model:
         # what the passes read: the parameters, or their bf16 copies
         self.copies = None if dtype is torch.float32 else [p.to(dtype) for p in self.parameters()]
         self.state = hb.adamw_state(self.parameters(), bits)
-        self.steps = 0
+        self.steps, self.seed = 0, seed
 
     def parameters(self):
         return [self.table, *self.w, *self.gain, self.w2]
@@ -82,7 +83,7 @@ class Model:
         norm = hb.grad_norm(grads)
         self.steps += 1
         hb.adamw_step(self.parameters(), grads, self.state, self.steps, lr=rate, weight_decay=self.decay, total_norm=norm, max_norm=max_norm,
-                      copies=self.copies)
+                      copies=self.copies, seed=self.seed)
         return loss, norm
 
 

@@ -574,7 +574,8 @@ hag_status hag_rms_norm_bwd(int64_t n, int32_t D, const void *grad_y, hag_dtype 
  *   p = p (1 - lr decay_i) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
  * params, param_dtypes, grads, grad_dtypes, copies, lengths, decays: HOST arrays of `count` entries (read during the call,
  * not kept); params[i] and grads[i]: DEVICE pointers to lengths[i] contiguous elements.  grads[i] NULL: tensor i, its
- * states and its copy stay as they are.  copies (may be NULL, and so may its entries): copies[i] receives the new parameters in bf16.
+ * states and its copy stay as they are.  copies (may be NULL, and so may its entries): copies[i] receives the new
+ * parameters in bf16.
  * No two tensors may overlap, and no tensor may be named twice, but that grads may share memory.
  * The states of all tensors lie in one array of blocks of HAG_ADAMW_BLOCK elements, the blocks of tensor i behind those of
  * tensor i - 1, ceil(lengths[i] / HAG_ADAMW_BLOCK) of them; hag_adamw_state_blocks gives their number (-1 on bad
@@ -585,21 +586,34 @@ hag_status hag_rms_norm_bwd(int64_t n, int32_t D, const void *grad_y, hag_dtype 
  *                those of block b.  scale = largest finite magnitude / 448, at least 2^-126; each value is rounded to
  *                nearest after the step has been taken with the new m and v in fp32; a positive root is stored as 2^-9
  *                at least; a value that is not finite is stored as NaN and does not touch the rest of its block.
+ *                Rounding to nearest has a limit: codes are 6 to 12 % apart, but a root shrinks by a factor sqrt(beta2) a step
+ *                at most, so that no code ever falls by itself; it moves with its block's scale. The stored roots are right
+ *                (half to one and a half times the exact ones) while the gradients of a block grow and shrink together.  Where
+ *                half of a block's become 30 times larger, the other half's roots are 7 times too large after 3000 steps at
+ *                beta2 = 0.999, for good; where half become 30 times smaller, their own are 4 times too large by then, and 16
+ *                after 6000: steps are too short by as much.  A mean stays as it is in the same way where beta1 is above 0.94.
+ *   rounding   : HAG_CHANCE instead of HAG_NEAREST is free of that limit.  Each value of HAG_STATE8 goes to the code below or
+ *                above it, with the probability of its nearness (a positive root to 2^-9 at least), so that it is right on
+ *                average.  The random numbers are made from seed, the number of the step and the place among the states,
+ *                and from nothing else: equal calls give equal bits.  Lists that are trained together want seeds of their own.
  * In the step, and in the stored roots, a v below 2^-126 counts as 0, and so does an eps below 2^-126.
  * options: numbers that change from step to step may be given on the device, so that a captured call replays with new
  * ones: lr_device in the place of lr, step_device in the place of step (read by the call; who counts it up is the caller;
  * a step below 1 counts as 1).
  * Errors: NULL, ARG (count < 0, a negative length or decay, lr or max_norm negative or no number, a beta outside [0, 1), eps
- * negative or no number, step < 1), DTYPE, ALIGN (pointer not on its element; states or scales not on 16 bytes),
- * TOO_LARGE (a tensor of more than 2^39 - 256 elements), CUDA. */
+ * negative or no number, step < 1, a rounding that is none), DTYPE, ALIGN (pointer not on its element; states or scales
+ * not on 16 bytes), TOO_LARGE (a tensor of more than 2^39 - 256 elements), CUDA. */
 #define HAG_ADAMW_BLOCK 256
 typedef enum { HAG_STATE32 = 0, HAG_STATE8 = 1 } hag_state_type;
+typedef enum { HAG_NEAREST = 0, HAG_CHANCE = 1 } hag_rounding;
 typedef struct hag_adamw_options {
     double lr, beta1, beta2, eps, max_norm;
     int64_t step;
     const float *lr_device;
     const int64_t *step_device;
     const float *total_norm;
+    uint64_t seed;
+    int32_t rounding;
 } hag_adamw_options;
 int64_t hag_adamw_state_blocks(int32_t count, const int64_t *lengths);
 hag_status hag_adamw_step(int32_t count, void *const *params, const hag_dtype *param_dtypes, const void *const *grads,

@@ -22,7 +22,7 @@ from __future__ import annotations
 import ctypes
 import os
 from array import array
-from operator import attrgetter, eq
+from operator import attrgetter, eq, index as index_of
 from typing import NamedTuple, Optional
 
 import numpy as np
@@ -35,6 +35,7 @@ HAG_F32, HAG_BF16 = 0, 1
 HAG_ID32, HAG_ID64 = 0, 1
 HAG_E4M3, HAG_I8 = 0, 1
 HAG_STATE32, HAG_STATE8 = 0, 1
+HAG_NEAREST, HAG_CHANCE = 0, 1
 HAG_ADAMW_BLOCK = 256
 (HAG_OK, HAG_ERR_NULL, HAG_ERR_ARG, HAG_ERR_GRAPH, HAG_ERR_OOM_HOST, HAG_ERR_OOM_DEVICE, HAG_ERR_CUDA, HAG_ERR_DTYPE,
  HAG_ERR_ALIGN, HAG_ERR_WORKSPACE, HAG_ERR_TIMEOUT, HAG_ERR_NOT_ON_DEVICE, HAG_ERR_TOO_LARGE) = range(13)
@@ -90,7 +91,7 @@ class HagArrays(ctypes.Structure):
 
 class HagAdamwOptions(ctypes.Structure):
     _fields_ = [(k, ctypes.c_double) for k in ("lr", "beta1", "beta2", "eps", "max_norm")] + [("step", ctypes.c_int64)] + [
-        (k, ctypes.c_void_p) for k in ("lr_device", "step_device", "total_norm")]
+        (k, ctypes.c_void_p) for k in ("lr_device", "step_device", "total_norm")] + [("seed", ctypes.c_uint64), ("rounding", ctypes.c_int32)]
 
 
 _lib = None
@@ -972,7 +973,8 @@ class AdamWState(NamedTuple):
 
 
 def adamw_state(params, bits=32) -> AdamWState:
-    """Zero states for ``adamw_step``: float32, or float8_e4m3fn with a float32 scale per block for ``bits`` = 8."""
+    """Zero states for ``adamw_step``: float32, or float8_e4m3fn with a float32 scale per block for ``bits`` = 8 (see its
+    ``seed``)."""
     import torch
     if bits not in (8, 32):
         raise ValueError(f"bits must be 8 or 32, got {bits!r}")
@@ -1017,7 +1019,7 @@ def _written_twice(params, copies, grads):
 
 
 def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, total_norm=None, max_norm=None,
-               copies=None):
+               copies=None, seed=None):
     """``hag_adamw_step``: one AdamW step over all ``params``, which it changes in place with their ``state``
     (``adamw_state``).  Gradients have their parameters' shapes; an entry of ``grads`` may be None: that parameter stays as it is,
     and its copy is not written.
@@ -1025,8 +1027,14 @@ def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
     ``step`` counts from 1, ``lr`` is the rate; either may be a device tensor of one value (int64, float32), which a
     captured call reads anew each time.  ``weight_decay`` is a number or a list of one per parameter.  With ``total_norm``
     (what ``grad_norm`` returned) the gradients are scaled as ``clip_grad_norm`` does for ``max_norm``, on the way.
-    ``copies``: a list of bfloat16 tensors (or None entries) of the same shapes that receive the new values.  Torch's own
-    differentiation does not notice that the parameters change: step after the backward pass.  Returns ``params``."""
+    ``copies``: a list of bfloat16 tensors (or None entries) of the same shapes that receive the new values.
+
+    ``seed``: an integer, with which 8-bit states are rounded up or down by chance (another number each step, the same for
+    the same call) instead of to nearest.  Give one where a training run has more than some hundred steps: rounded to
+    nearest, the root of a parameter whose gradients shrink against those of its block's others stays too large.
+
+    Torch's own differentiation does not notice that the parameters change: step after the backward pass.  Returns
+    ``params``."""
     import torch
     if not params or not params[0].is_cuda:
         raise ValueError("parameters must be a list of device tensors, not empty")
@@ -1069,6 +1077,8 @@ def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
     if len(decays) != count:
         raise ValueError(f"{len(decays)} weight decays for {count} parameters")
     o = HagAdamwOptions(beta1=betas[0], beta2=betas[1], eps=eps)
+    if seed is not None:
+        o.seed, o.rounding = index_of(seed) & 0xffffffffffffffff, HAG_CHANCE
     if isinstance(lr, torch.Tensor):
         o.lr_device = _one_value(lr, "lr", index, torch.float32)
     else:
