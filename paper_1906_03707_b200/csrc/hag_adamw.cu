@@ -75,7 +75,6 @@ static_assert(sizeof(AdamArgs) <= 4096, "the list must fit in the parameters of 
 struct Coefficients {
     float lr, rate, root;
     float norm;                                 // as it was read: it arrives while the first blocks do
-    uint64_t key;                               // of the step's roundings by chance
 };
 // What the gradient is multiplied with for m, and, before its square, for v.
 __device__ __forceinline__ float2 of_gradient(const AdamArgs &p, float norm) {
@@ -94,12 +93,12 @@ __device__ double power(double base, int64_t n) {          // base^n by squaring
 
 // Random bits from a counter, so that a call's results depend on its arguments alone: products with odd numbers (the
 // fractions of the roots of 2 and 3 and of the golden ratio) carry low bits upwards, shifts bring high bits down again.
-__host__ __device__ __forceinline__ uint64_t mix64(uint64_t x) {
+__device__ __forceinline__ uint64_t mix64(uint64_t x) {
     x = (x ^ (x >> 32)) * 0x6a09e667f3bcc909ull;
     x = (x ^ (x >> 29)) * 0xbb67ae8584caa73bull;
     return x ^ (x >> 32);
 }
-__host__ __device__ __forceinline__ uint64_t step_key(uint64_t seed, int64_t step) { return mix64(mix64(seed + 0x9e3779b97f4a7c15ull) + uint64_t(step)); }
+__device__ __forceinline__ uint64_t step_key(uint64_t seed, int64_t step) { return mix64(mix64(seed + 0x9e3779b97f4a7c15ull) + uint64_t(step)); }
 // Of element `place` of a block with key `block`: 16 bits for the mean, 16 for the root.
 __device__ __forceinline__ uint32_t random_bits(uint64_t block, uint32_t place) {
     uint32_t x = uint32_t(block) + place * 0x9e3779b9u;
@@ -344,8 +343,8 @@ struct Piece {
 };
 
 template <typename P, typename G, bool BITS8, bool CHANCE, bool VEC>
-__device__ __forceinline__ void step_block(const AdamArgs &a, const Coefficients &c, float keep_, float2 of_g, const Piece<P, G, BITS8, VEC> &in,
-                                           const Arrays<P, G, BITS8> &to, int block, int lane, int count) {
+__device__ __forceinline__ void step_block(const AdamArgs &a, const Coefficients &c, uint64_t of_step, float keep_, float2 of_g,
+                                           const Piece<P, G, BITS8, VEC> &in, const Arrays<P, G, BITS8> &to, int block, int lane, int count) {
     const float2 keep = both(keep_), of_m = both(of_g.x), of_v = both(of_g.y);
     const float2 of_old_m = both(BITS8 ? in.scale.x * a.b1 : a.b1), of_old_v = both(BITS8 ? in.scale.y * a.root2 : a.b2);
     float2 p[kPairs], m[kPairs], v[kPairs], r[kPairs];
@@ -365,7 +364,7 @@ __device__ __forceinline__ void step_block(const AdamArgs &a, const Coefficients
     store8<P, VEC>(p, to.p + block * kAdamBlock, lane, count);
     if (to.copy) store8<__nv_bfloat16, VEC>(p, to.copy + block * kAdamBlock, lane, count);
     if constexpr (BITS8) {
-        const uint64_t key = CHANCE ? mix64(c.key + uint64_t(to.scales + block - a.scales)) : 0;
+        const uint64_t key = CHANCE ? mix64(of_step + uint64_t(to.scales + block - a.scales)) : 0;
         store_8_bits<VEC, CHANCE>(m, r, to.m + block * kAdamBlock, to.v + block * kAdamBlock, to.scales + block, lane, count, key);
     } else {
         store8<float, VEC>(m, to.m + block * kAdamBlock, lane, count);
@@ -375,7 +374,7 @@ __device__ __forceinline__ void step_block(const AdamArgs &a, const Coefficients
 
 // T blocks of a tensor from block `within` on; of the whole ones as many as the registers hold are read at once.
 template <typename P, typename G, bool BITS8, bool CHANCE, int T>
-__device__ __forceinline__ void step_unit(const AdamArgs &a, const Coefficients &c, int t, uint32_t within) {
+__device__ __forceinline__ void step_unit(const AdamArgs &a, const Coefficients &c, uint64_t key, int t, uint32_t within) {
     constexpr int kWords = 2 * int(sizeof(P) + sizeof(G)) + (BITS8 ? 4 : 16);          // per lane and block
     constexpr int B = kWords * T <= 48 ? T : kWords * 2 <= 64 && T > 1 ? 2 : 1;
     const int lane = threadIdx.x & 31;
@@ -389,7 +388,7 @@ __device__ __forceinline__ void step_unit(const AdamArgs &a, const Coefficients 
             for (int k = 0; k < B; ++k) in[k].load(at, i + k, lane, kAdamBlock);
             const float2 of_g = of_gradient(a, c.norm);
 #pragma unroll
-            for (int k = 0; k < B; ++k) step_block<P, G, BITS8, CHANCE, true>(a, c, keep, of_g, in[k], at, i + k, lane, kAdamBlock);
+            for (int k = 0; k < B; ++k) step_block<P, G, BITS8, CHANCE, true>(a, c, key, keep, of_g, in[k], at, i + k, lane, kAdamBlock);
         }
     } else {
         const int n = int(min(uint32_t(T), a.blocks[t] - within));
@@ -398,12 +397,12 @@ __device__ __forceinline__ void step_unit(const AdamArgs &a, const Coefficients 
             if (T > 1 && within + i < a.whole[t]) {
                 Piece<P, G, BITS8, true> in;
                 in.load(at, i, lane, kAdamBlock);
-                step_block<P, G, BITS8, CHANCE, true>(a, c, keep, of_gradient(a, c.norm), in, at, i, lane, kAdamBlock);
+                step_block<P, G, BITS8, CHANCE, true>(a, c, key, keep, of_gradient(a, c.norm), in, at, i, lane, kAdamBlock);
             } else {
                 const int count = int(min(int64_t(kAdamBlock), a.len[t] - int64_t(within + i) * kAdamBlock));
                 Piece<P, G, BITS8, false> in;
                 in.load(at, i, lane, count);
-                step_block<P, G, BITS8, CHANCE, false>(a, c, keep, of_gradient(a, c.norm), in, at, i, lane, count);
+                step_block<P, G, BITS8, CHANCE, false>(a, c, key, keep, of_gradient(a, c.norm), in, at, i, lane, count);
             }
         }
     }
@@ -418,12 +417,15 @@ __global__ void __launch_bounds__(kAdamThreads, T > 1 ? 2 : 4) adamw_kernel(cons
     if (threadIdx.x < kAdamList) first[threadIdx.x] = int(threadIdx.x) < a.tensors ? a.first[threadIdx.x] : 0xffffffffu;
     hagk::pdl_wait();
     Coefficients c{a.lr, a.rate, a.root};
-    if (CHANCE || a.step_at || a.lr_at) {
-        if (threadIdx.x == 0) {
-            if (a.step_at || a.lr_at) c = coefficients(a);
-            if (CHANCE) c.key = key_of(a);
-            shared = c;
-        }
+    uint64_t key = 0;
+    if constexpr (CHANCE) {
+        __shared__ uint64_t shared_key;
+        if (threadIdx.x == 0) shared_key = key_of(a);
+        __syncthreads();
+        key = shared_key;
+    }
+    if (a.step_at || a.lr_at) {
+        if (threadIdx.x == 0) shared = coefficients(a);
         __syncthreads();
         c = shared;
     } else {
@@ -437,11 +439,11 @@ __global__ void __launch_bounds__(kAdamThreads, T > 1 ? 2 : 4) adamw_kernel(cons
         const int t = __popc(__ballot_sync(0xffffffffu, first[lane] <= k)) + __popc(__ballot_sync(0xffffffffu, first[lane + 32] <= k)) - 1;
         const uint32_t within = (k - first[t]) * T;
         if (a.p_bf16[t]) {
-            if (a.g_bf16[t]) step_unit<__nv_bfloat16, __nv_bfloat16, BITS8, CHANCE, T>(a, c, t, within);
-            else step_unit<__nv_bfloat16, float, BITS8, CHANCE, T>(a, c, t, within);
+            if (a.g_bf16[t]) step_unit<__nv_bfloat16, __nv_bfloat16, BITS8, CHANCE, T>(a, c, key, t, within);
+            else step_unit<__nv_bfloat16, float, BITS8, CHANCE, T>(a, c, key, t, within);
         } else {
-            if (a.g_bf16[t]) step_unit<float, __nv_bfloat16, BITS8, CHANCE, T>(a, c, t, within);
-            else step_unit<float, float, BITS8, CHANCE, T>(a, c, t, within);
+            if (a.g_bf16[t]) step_unit<float, __nv_bfloat16, BITS8, CHANCE, T>(a, c, key, t, within);
+            else step_unit<float, float, BITS8, CHANCE, T>(a, c, key, t, within);
         }
     }
 }
