@@ -455,14 +455,18 @@ bool on(const void *p, int bytes) { return reinterpret_cast<uintptr_t>(p) % uint
 
 // Blocks that a warp takes at a time where a launch has more than kFewBlocks: four, all of whose data is read before the
 // first is worked on, so that what surrounds a block (its tensor, its addresses) is shared.  200 million bf16 parameters
-// with 8-bit states: four 327 us, two 364, eight 363; one, as a launch of few blocks takes them, 391.  Of few blocks one at
-// a time, for more warps: 5 million fp32 parameters with 8-bit states 16.2 us, four at a time 20.0; 8 million 24.9 and
-// 27.0; 16 million bf16 ones 36.5 and 30.8.
+// with 8-bit states: four 319 us, two 364, eight 363; one, as a launch of few blocks takes them, 391.  Of few blocks one at
+// a time, for more warps.  Both sides, us, one and four at a time, at 5, 8, 12 and 24 million parameters: fp32 with 8-bit states
+// 16.3 and 19.9, 25.0 and 26.8, 35.4 and 35.2, 67.4 and 65.1; fp32 with fp32 states 23.5 and 25.1, 35.7 and 36.4, 52.7 and 52.7,
+// 103.9 and 100.9; rounded by chance 19.5 and 21.9, 28.3 and 32.4, 41.9 and 41.1, 77.2 and 75.9; other types meet there too.
+// Where all is bf16 and 8 bits, a block has 2.5 KB and more of them have to be on their way: 12.8 and 13.1, 20.4 and 19.1,
+// 28.7 and 23.9, 53.2 and 43.6 (6 million 16.1 and 15.5).
 // The grid: with 8-bit states as many thread blocks as run at once (150 million fp32 parameters 377 us, a hundred per SM
 // 423); with fp32 states up to a hundred per SM, which take their units as others end (150 million fp32 parameters 611 us,
 // as many as run 690; of few blocks up to sixteen: 5 million 23.8 us, four 26.2).
 constexpr int kUnit = 4;
-constexpr int64_t kFewBlocks = kSms * 4 * kAdamWarps * 5;
+constexpr int64_t kFewBlocks = kSms * 304;             // 11.5 million elements
+constexpr int64_t kFewNarrowBlocks = kSms * 140;       // 5.3 million
 constexpr int64_t kMostBlocks = 0x7fffffffLL;   // of a tensor and of a launch
 }  // namespace
 
@@ -534,7 +538,9 @@ extern "C" hag_status hag_adamw_step(int32_t count, void *const *params, const h
     int64_t at = 0, blocks = 0;
     auto launch = [&]() {
         if (a.tensors > 0) {
-            const bool many = blocks > kFewBlocks;
+            bool narrow = bits8 && !chance;
+            for (int i = 0; i < a.tensors; ++i) narrow = narrow && a.p_bf16[i] && a.g_bf16[i];
+            const bool many = blocks > (narrow ? kFewNarrowBlocks : kFewBlocks);
             a.units = 0;
             for (int i = 0; i < a.tensors; ++i) {
                 a.first[i] = a.units;
