@@ -997,19 +997,23 @@ _dtype_of, _shape_of = attrgetter("dtype"), attrgetter("shape")
 
 
 def _addresses(tensors, index, what):
-    """Addresses, shapes and type codes of a list of contiguous device tensors; AttributeError where an entry is None."""
+    """Addresses and type codes (an array) of a list of contiguous device tensors; AttributeError where an entry is None."""
     import torch
     T = torch.Tensor
     if not _codes:
         _runtime()
     kinds = list(map(_dtype_of, tensors))
     try:                                                        # most lists are of one type
-        codes = [_codes[kinds[0]]] * len(kinds) if kinds.count(kinds[0]) == len(kinds) else list(map(_codes.__getitem__, kinds))
+        codes = array("i", [_codes[kinds[0]]]) * len(kinds) if kinds.count(kinds[0]) == len(kinds) else array("i", map(_codes.__getitem__, kinds))
     except KeyError as e:
         raise TypeError(f"{what} must be float32 or bfloat16, got {e.args[0]}") from None
     if not all(map(T.is_contiguous, tensors)) or set(map(T.get_device, tensors)) != {index}:
         raise ValueError(f"{what} must be contiguous tensors on cuda:{index}")
-    return list(map(T.data_ptr, tensors)), list(map(_shape_of, tensors)), codes
+    return list(map(T.data_ptr, tensors)), codes
+
+
+def _same_shapes(a, b):
+    return all(map(eq, map(_shape_of, a), map(_shape_of, b)))
 
 
 def _written_twice(params, copies, grads):
@@ -1041,22 +1045,23 @@ def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
     index, count = params[0].get_device(), len(params)
     if len(grads) != count:
         raise ValueError(f"{len(grads)} gradients for {count} parameters")
-    ptrs, shapes, codes = _addresses(params, index, "parameters")
-    lens = list(map(torch.Tensor.numel, params))
+    ptrs, codes = _addresses(params, index, "parameters")
+    there = grads
     try:
-        gptrs, gshapes, gcodes = _addresses(grads, index, "gradients")
+        gptrs, gcodes = _addresses(grads, index, "gradients")
     except AttributeError:                                      # some are None
-        gptrs, gshapes, gcodes = _addresses([p if g is None else g for g, p in zip(grads, params)], index, "gradients")
+        there = [p if g is None else g for g, p in zip(grads, params)]
+        gptrs, gcodes = _addresses(there, index, "gradients")
         gptrs = [0 if g is None else at for g, at in zip(grads, gptrs)]
-    if gshapes != shapes:                                       # of equal length alone a transposed gradient would pass
+    if not _same_shapes(there, params):                         # of equal length alone a transposed gradient would pass
         raise ValueError("gradients must have the shapes of the parameters")
     cptrs, written = None, ptrs
     if copies is not None:
         if len(copies) != count:
             raise ValueError(f"{len(copies)} copies for {count} parameters")
         here = [c for c in copies if c is not None]
-        some, cshapes, ckinds = _addresses(here, index, "copies") if here else ([], [], [])
-        if cshapes != [m for m, c in zip(shapes, copies) if c is not None] or any(k != HAG_BF16 for k in ckinds):
+        some, ckinds = _addresses(here, index, "copies") if here else ([], [])
+        if not _same_shapes(here, [p for p, c in zip(params, copies) if c is not None]) or any(k != HAG_BF16 for k in ckinds):
             raise ValueError("copies must be bfloat16 tensors with the shapes of the parameters")
         written = ptrs + some
         cptrs = array("Q", some if len(here) == count else [0 if c is None else c.data_ptr() for c in copies])
@@ -1065,7 +1070,8 @@ def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
         if _written_twice(params, copies, grads):
             raise ValueError("a tensor is named twice, or a gradient is written as a parameter or copy")
     mean, square, scales = state
-    blocks = sum([(m + (HAG_ADAMW_BLOCK - 1)) // HAG_ADAMW_BLOCK for m in lens])
+    lens = array("q", map(torch.Tensor.numel, params))
+    blocks = _lib.hag_adamw_state_blocks(count, lens.buffer_info()[0])
     bits8 = scales is not None
     sdt = torch.float8_e4m3fn if bits8 else torch.float32
     for t, what in ((mean, "mean"), (square, "square")):
@@ -1091,7 +1097,7 @@ def adamw_step(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
         raise ValueError("total_norm and max_norm go together")
     if total_norm is not None:
         o.total_norm, o.max_norm = _one_value(total_norm, "total_norm", index, torch.float32), max_norm
-    lists = [array("Q", ptrs), array("i", codes), array("Q", gptrs), array("i", gcodes), cptrs, array("q", lens), decays]
+    lists = [array("Q", ptrs), codes, array("Q", gptrs), gcodes, cptrs, lens, decays]
     _call("hag_adamw_step", index, count, *[None if x is None else x.buffer_info()[0] for x in lists], HAG_STATE8 if bits8 else HAG_STATE32,
           mean.data_ptr(), square.data_ptr(), scales.data_ptr() if bits8 else None, ctypes.byref(o))
     return params
