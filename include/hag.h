@@ -548,7 +548,7 @@ hag_status hag_clip_grad_norm(int32_t count, const void *const *grads, void *con
  * stream; else NULL.  grad_weight may be NULL; with n = 0 it is zeros.
  * In place (same pointer, type and row stride): y or total in the place of x or residual; grad_residual in the place of
  * grad_total, total or grad_y.
- * Squares are fp32: magnitudes above 1.8e19 give rstd = 0.
+ * Squares are fp32: magnitudes above 1.8e19 give rstd = 0 and, with eps = 0, a row of magnitudes below 1e-23 an infinite one.
  * hag_rms_norm_bwd_workspace_bytes: 16-byte aligned scratch, needed when grad_weight is wanted; carries nothing between
  * calls.
  * Errors: NULL, ARG (n < 0, D <= 0, eps negative or no number, a stride, block, kind), DTYPE, ALIGN (pointer not on its

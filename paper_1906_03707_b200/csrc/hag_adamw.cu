@@ -21,7 +21,7 @@
 // copies and fp32 states 825 us (6.8 TB/s); 12 tensors of 50 000 values together 3.5 and 3.0 us.  A warp that copied its
 // blocks into a ring in shared memory first took 415 us and 998, one that read the next block into registers 458 and 911.
 // Tensors that do not begin on four of their elements are read one element at a time: 7 million fp32 parameters with
-// 8-bit states 34 us, aligned 20.
+// 8-bit states, bf16 gradients and copies 35 us, aligned 23.
 #include <cuda_runtime.h>
 
 #include <algorithm>

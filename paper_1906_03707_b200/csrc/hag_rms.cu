@@ -8,9 +8,10 @@
 //
 // Bound by memory.  Measured on B200 against a copy at 6.53 TB/s: 10^6 x 256 bf16 319 us (6.4 TB/s), around an fp32 stream 472
 // (6.5), into e4m3 with a scale per row 285 (6.3); 233 000 x 128 fp32 75.5 us (6.3); 30 000 x 4096 bf16 149 us (6.6); 10 000 x
-// 12 000 bf16 150 us (6.4).  Into 8 bits the instructions come near, 57 % of the issue slots.  Rows that do not begin on 16
-// bytes are read and written one element at a time: 300 000 x 333 fp32 275 us (5.8 TB/s), bf16 170 (4.7), 50 000 x 1433 bf16
-// into e4m3 169 (2.9: a byte per store).
+// 12 000 bf16 150 us (6.4).  Into 8 bits the instructions come near, 59 % of the issue slots (30 000 x 4096 bf16 with a scale
+// per 128 columns 149 us, 5.8 TB/s; into int8, whose codes are converted one by one, 162).  Rows that do not begin on 16
+// bytes are read and written one element at a time: 300 000 x 333 fp32 275 us (5.8 TB/s), bf16 171 (4.7), 50 000 x 1433 bf16
+// into e4m3 173 (2.9: a byte per store).
 #include "hag_rms.cuh"
 
 #include <cfloat>

@@ -5,9 +5,11 @@
 //
 // Bound by memory.  Measured on B200, where a copy runs at 6.53 TB/s: with a gradient along the stream 10^6 x 256 bf16 294 us
 // (7.0 TB/s: three reads for a write), around an fp32 stream 624 (6.6), 30 000 x 4096 bf16 147 (6.7); without one 10^6 x 256
-// bf16 235 us (6.5).  Blocks of more than 512 threads have no registers left for what they read, read it twice and wait for
-// it: 10 000 x 12 000 bf16 277 us (3.5).  Rows that do not begin on 16 bytes are read one element at a time: 300 000 x 333
-// fp32 244 us (6.6), bf16 181 (4.4), 5001 x 1433 fp32 without a gradient along the stream 21.5 (4.0; 3 of them the join).
+// bf16 235 us (6.5).  Blocks of more than 512 threads have 64 registers each and no room for what they read: they read it twice,
+// convert it twice and wait for it, one block per SM: 10 000 x 12 000 bf16 277 us (3.5), at 54 % of the issue slots.  The 384 to
+// 464 bytes that a thread of these kernels spills are not it: reads and writes of them are 0.4 % of the
+// instructions.  Rows that do not begin on 16 bytes are read one element at a time: 300 000 x 333 fp32 244 us (6.6), bf16 183
+// (4.4), 5001 x 1433 fp32 without a gradient along the stream 21.6 (4.0; 3 of them the join).
 #include "hag_rms.cuh"
 
 namespace {
@@ -455,8 +457,10 @@ cudaError_t launch_rows(RmsBwdArgs &p, int warps, cudaStream_t s) {
         if (size_t(kLane) * threads * p.stages > size_t(kMostShared)) p.stages = 1;
         shared = std::max(shared, size_t(kLane) * threads * p.stages);
     }
-    // Two operands: four times as many blocks as run at once, which take their rows as others end (10^6 x 256 bf16 235 us, as
-    // many as run 247); three operands, or rows of blocks: as many as run (10^6 x 256 bf16 295 us, four times as many 300).
+    // Two operands: four times as many blocks as run at once, but no more than there are parts (eight per SM at most), which take
+    // their rows as others end (10^6 x 256 bf16 235 us, as many as run 247); three operands, or rows of blocks: as many as run
+    // (10^6 x 256 bf16 295 us, four times as many 300).  Without gw the number of parts binds nothing, and costs nothing: 2 000 000
+    // x 8 bf16 20.1 us, without that limit 20.7, 10^6 x 64 60.8 and 60.9.
     const int most = blocks_per_sm<kernel>(threads, shared) * (kRing<Y, V> && L > 0 && !ALONG ? 4 : 1);
     const int64_t rows = L > 0 ? int64_t(kWarpRowThreads / kGroup) * R : 1;
     int64_t grid = std::min<int64_t>((p.n + rows - 1) / rows, std::min(kSms * most, most_parts(p.D)));

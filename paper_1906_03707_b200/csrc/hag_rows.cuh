@@ -1,5 +1,5 @@
-// Row vectors shared by the kernels around the aggregation (embedding, layer norm, clipping): V elements of
-// type T as one load or store of V * sizeof(T) bytes (two of 16 bytes where that is 32), kept as raw words
+// Row vectors shared by the kernels around the aggregation (embedding, layer norm, clipping, root-mean-square norm, AdamW),
+// and sums and arithmetic on pairs of their elements: V elements of type T as one load or store of V * sizeof(T) bytes (two of 16 bytes where that is 32), kept as raw words
 // while in flight and widened to fp32 when used.  V is the largest power of two that the width, the row
 // strides and the pointers of a call allow (vector_elems), so any width and any element-aligned pointer works.
 // Loads are coherent (ld.global, never .nc): under programmatic dependent launch the kernel that wrote the
